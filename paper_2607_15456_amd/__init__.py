@@ -4,7 +4,7 @@ liblla.so holds the HIP kernels (gfx950) behind the C ABI of include/lla.h;
 ``paper_2607_15456_amd.lla`` is its thin ctypes binding.
 """
 
-from . import lla  # noqa: F401
+from . import kv, lla  # noqa: F401
 from .lla import (  # noqa: F401
     LLAError,
     alloc_cache,

@@ -1,0 +1,340 @@
+"""Binding of the paged K/V cache (include/lla_kv.h; argument marshalling only).
+
+The full-memory path beside the latent cache of ``lla``: keys and values of
+every token in pages of 64 positions that sequences share through a page table.
+A decode step of a batch, every call enqueued and none waiting for the host::
+
+    kv.reserve(pages, rows, add, start, pairs, result)     # room; copy on write
+    kv.copy_pages(k_pages, v_pages, pairs, result)         # all layers
+    ... per layer:
+    q = kv.rope(q, freq, pos=start)
+    kv.write(k, v, k_pages[l], v_pages[l], pages.table, start, rows=rows, freq=freq)
+    o = kv.decode_attn(q[:, 0], k_pages[l], v_pages[l], pages.table, pages.length, rows=rows, n_ctx=n)
+
+Pools: keys [n_pages, H_kv, 64, d], values [n_pages, H_kv, d, 64], with a leading
+layer dimension for the calls that take all layers at once.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple
+
+import torch
+
+from . import lla
+from .lla import PAGE, _c_f, _c_i64, _c_int, _c_sz, _c_vp, _check, _dt, _need, _out_code, _ptr
+
+ABI_VERSION = 1  # LLA_KV_ABI_VERSION of include/lla_kv.h this binding follows
+MAX_ROWS = 1024
+PAGES_OK, PAGES_FULL, PAGES_BAD = range(3)  # result[0] of the table calls
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+_c_d, _I64, _VP = ctypes.c_double, [_c_i64], [_c_vp]
+
+_SIGS = {
+    "lla_kv_abi_version": [],
+    "lla_rope_frequencies": [_c_int, _c_d, _c_int, _c_d, _c_d, _c_d, _c_d, _c_vp, ctypes.POINTER(_c_d)],
+    "lla_rope_positions": [_c_int] * 8 + _VP + _I64 * 3 + _VP + [_c_int] * 2 + _VP + [_c_f] + _VP + _I64 * 3 + _VP,
+    "lla_kv_write": [_c_int] * 7 + (_VP + _I64 * 2) * 2 + _VP + [_c_f] + [_c_int] * 3 + _VP * 7,
+    "lla_kv_decode_workspace_bytes": [_c_int] * 8 + [ctypes.POINTER(_c_sz)],
+    "lla_kv_decode_attn": [_c_int] * 12 + _VP * 6 + [_c_f] + _VP * 3 + [_c_sz] + _VP,
+    "lla_pages_reserve": [_c_int] + _VP * 2 + [_c_int] * 3 + _VP * 8,
+    "lla_pages_fork": [_c_int] + _VP * 2 + [_c_int] * 3 + _VP * 6,
+    "lla_pages_free": [_c_int] + _VP + [_c_int] * 3 + _VP * 6,
+    "lla_pages_copy": [_c_int] * 2 + (_VP + _I64) * 2 + _VP + [_c_int] + _VP * 2,
+    "lla_kv_gather": [_c_int] * 9 + _VP * 8,
+}
+
+_lib = None
+
+
+def lib() -> ctypes.CDLL:
+    """liblla.so with the entry points of lla_kv.h."""
+    global _lib
+    if _lib is None:
+        h = lla.lib()
+        for name, args in _SIGS.items():
+            fn = getattr(h, name)
+            fn.restype, fn.argtypes = _c_int, args
+        if h.lla_kv_abi_version() != ABI_VERSION:
+            raise RuntimeError(f"{lla.LIB_PATH} has K/V ABI version {h.lla_kv_abi_version()}, this binding "
+                               f"needs {ABI_VERSION}; rebuild it")
+        _lib = h
+    return _lib
+
+
+def _call(name, dev, *args):
+    """An entry point on dev's current stream, with dev the current device."""
+    fn = getattr(lib(), name)
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+
+
+def _ints(t, name, shape, dev):
+    _need(t, name, torch.int32, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}")
+
+
+def _rows_of(t, name, dev, dtype):
+    """Strides of t [B, M, heads, width] whose rows are dense (of a dimension of
+    one entry, which torch leaves as it happens to be, 0)."""
+    if not t.is_cuda or t.device != dev:
+        raise ValueError(f"{name} must be a tensor on {dev}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise ValueError(f"{name} must be [B, M, heads, width] with dense rows")
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape)]
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+
+def rope_frequencies(d_rot: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     original: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
+    """(float64 device tensor [d_rot / 2] of angles per position, magnitude) for
+    rope and write.  scaling: "none", "linear", "ntk" or "yarn" (with the trained
+    length ``original`` and its two turn counts)."""
+    if scaling not in SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(SCALINGS)}")
+    freq, mag = torch.empty(max(d_rot // 2, 1), dtype=torch.float64), _c_d()
+    _check(lib().lla_rope_frequencies(d_rot, base, SCALINGS[scaling], factor, original, beta_fast, beta_slow,
+                                      freq.data_ptr(), ctypes.byref(mag)))
+    return freq.to(device), mag.value
+
+
+def _freq(freq, width, dev):
+    _need(freq, "freq", torch.float64, dev)
+    if freq.dim() != 1 or 2 * freq.numel() > width:
+        raise ValueError("freq must be [d_rot / 2] with d_rot at most the rows' width")
+    return 2 * freq.numel()
+
+
+def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitude: float = 1.0,
+         transpose: bool = False, out=None):
+    """Rows x [B, M, H, d] (any strides, dense rows) turned to their positions:
+    pos0 + m, plus pos[b] (int32 [B]), or pos0 + pos[b, m] (int32 [B, M]).  The
+    first 2 * len(freq) features turn in pairs, half-split or ``interleaved``, and
+    are multiplied by ``magnitude``; the rest is copied.  ``transpose`` takes the
+    gradient of the result to the gradient of x.  ``out`` may be x (in place)."""
+    dev = x.device
+    xs = _rows_of(x, "x", dev, x.dtype)
+    B, M, H, d = x.shape
+    rot = _freq(freq, d, dev)
+    if pos is not None:
+        _ints(pos, "pos", (B, M) if pos.dim() == 2 else (B,), dev)
+    if out is None:
+        out = torch.empty((B, M, H, d), dtype=x.dtype, device=dev)
+    elif out.shape != x.shape:
+        raise ValueError("out must have x's shape")
+    ys = _rows_of(out, "out", dev, x.dtype)
+    _call("lla_rope_positions", dev, _dt(x), B, M, H, d, rot, int(interleaved), int(transpose), _ptr(x), *xs, _ptr(pos),
+          int(pos is not None and pos.dim() == 2), pos0, _ptr(freq), float(magnitude), _ptr(out), *ys)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Pools and tables
+# ---------------------------------------------------------------------------
+
+class PageTable(NamedTuple):
+    """Which pages the sequences hold (int32 device tensors; one for all layers)."""
+    table: torch.Tensor    # [n_seqs, max_pages]
+    length: torch.Tensor   # [n_seqs] tokens
+    refs: torch.Tensor     # [n_pages] holders
+    free: torch.Tensor     # [1 + n_pages] count, then a stack
+
+
+def new_page_table(n_seqs: int, max_pages: int, n_pages: int, device="cuda") -> PageTable:
+    """Empty sequences and a pool of free pages (page 0 is taken first)."""
+    free = torch.arange(n_pages, -1, -1, dtype=torch.int32, device=device)
+    free[0] = n_pages
+    free[1:] = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+    zeros = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
+    return PageTable(torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), zeros(n_seqs),
+                     zeros(n_pages), free)
+
+
+def alloc_pages(n_pages: int, H_kv: int, d: int, dtype=torch.bfloat16, device="cuda", layers: int | None = None):
+    """Key and value pools of one layer, or of ``layers`` in one piece."""
+    lead = (n_pages, H_kv) if layers is None else (layers, n_pages, H_kv)
+    return (torch.empty((*lead, PAGE, d), dtype=dtype, device=device),
+            torch.empty((*lead, d, PAGE), dtype=dtype, device=device))
+
+
+def _pools(k_pages, v_pages, layered=False):
+    """(layers, n_pages, H_kv, d) of a pair of pools."""
+    dev = k_pages.device
+    _need(k_pages, "k_pages", None, dev)
+    _need(v_pages, "v_pages", k_pages.dtype, dev)
+    if k_pages.dim() not in ((4, 5) if layered else (4,)):
+        raise ValueError("k_pages must be [n_pages, H_kv, 64, d]" + (", or with a layer dimension" if layered else ""))
+    *lead, P, H, page, d = k_pages.shape
+    if page != PAGE or v_pages.shape != (*lead, P, H, d, PAGE):
+        raise ValueError("k_pages must be [n_pages, H_kv, 64, d] and v_pages [n_pages, H_kv, d, 64]")
+    return (lead[0] if lead else 1), P, H, d
+
+
+def _page_table(p, dev):
+    n_seqs, max_pages = p.table.shape
+    _ints(p.table, "table", (n_seqs, max_pages), dev)
+    _ints(p.length, "length", (n_seqs,), dev)
+    _ints(p.refs, "refs", (p.refs.numel(),), dev)
+    _ints(p.free, "free", (1 + p.refs.numel(),), dev)
+    return n_seqs, max_pages, p.refs.numel()
+
+
+def reserve(pages: PageTable, rows, add, start, pairs, result):
+    """Room for add[i] new tokens of sequence rows[i]; start[i] gets its length
+    before (-1 where the call is refused), pairs the pages to copy (copy on write)
+    and result (status, number of pairs, pages taken, pages left).  All int32:
+    rows, add, start [n], pairs [n, 2], result [4]."""
+    dev, n = rows.device, rows.numel()
+    sizes = _page_table(pages, dev)
+    for t, name, shape in ((rows, "rows", (n,)), (add, "add", (n,)), (start, "start", (n,)), (pairs, "pairs", (n, 2)),
+                           (result, "result", (4,))):
+        _ints(t, name, shape, dev)
+    _call("lla_pages_reserve", dev, n, _ptr(rows), _ptr(add), *sizes, *map(_ptr, pages), _ptr(start), _ptr(pairs),
+          _ptr(result))
+
+
+def fork(pages: PageTable, src, dst, result):
+    """The empty sequences dst[i] become src[i], sharing its pages (int32 [n])."""
+    dev, n = dst.device, dst.numel()
+    sizes = _page_table(pages, dev)
+    for t, name, shape in ((src, "src", (n,)), (dst, "dst", (n,)), (result, "result", (4,))):
+        _ints(t, name, shape, dev)
+    _call("lla_pages_fork", dev, n, _ptr(src), _ptr(dst), *sizes, *map(_ptr, pages), _ptr(result))
+
+
+def free(pages: PageTable, rows, result):
+    """Empty the sequences rows (int32 [n]); pages without a holder become free."""
+    dev, n = rows.device, rows.numel()
+    sizes = _page_table(pages, dev)
+    for t, name, shape in ((rows, "rows", (n,)), (result, "result", (4,))):
+        _ints(t, name, shape, dev)
+    _call("lla_pages_free", dev, n, _ptr(rows), *sizes, *map(_ptr, pages), _ptr(result))
+
+
+def copy_pages(a, b, pairs, result=None):
+    """Copy pages pairs[i, 0] -> pairs[i, 1] of the pools a and b (b may be None),
+    [n_pages, ...] or [layers, n_pages, H, 64, d]-like (five dimensions: layers
+    first); with the result of reserve, only the pairs that it gave."""
+    dev, pools = a.device, []
+    lead = a.shape[:2] if a.dim() == 5 else (1, a.shape[0])
+    for t, name in ((a, "a"), (b, "b")):
+        if t is None:
+            pools += [None, 0]
+            continue
+        _need(t, name, None, dev)
+        if (t.shape[:2] if t.dim() == 5 else (1, t.shape[0])) != lead:
+            raise ValueError("a and b must have the same layers and pages")
+        pools += [_ptr(t), t.numel() // (lead[0] * lead[1]) * t.element_size()]
+    _ints(pairs, "pairs", (pairs.shape[0], 2), dev)
+    if result is not None:
+        _ints(result, "result", (4,), dev)
+    _call("lla_pages_copy", dev, *lead, *pools, _ptr(pairs), pairs.shape[0], None if result is None else _ptr(result) + 4)
+
+
+def gather(k_pages, v_pages, table, src, dst, keep, n_keep=None):
+    """Position i of sequence dst[j] becomes position keep[j, i] of sequence src[j],
+    for i < n_keep[j] (all of keep's columns without n_keep); int32 tensors."""
+    dev = k_pages.device
+    layers, P, H, d = _pools(k_pages, v_pages, layered=True)
+    n_seqs, max_pages = table.shape
+    B, most = keep.shape
+    for t, name, shape in ((table, "table", (n_seqs, max_pages)), (src, "src", (B,)), (dst, "dst", (B,)),
+                           (keep, "keep", (B, most))):
+        _ints(t, name, shape, dev)
+    if n_keep is not None:
+        _ints(n_keep, "n_keep", (B,), dev)
+    _call("lla_kv_gather", dev, _dt(k_pages), B, most, layers, H, d, n_seqs, max_pages, P, _ptr(table), _ptr(src),
+          _ptr(dst), _ptr(keep), _ptr(n_keep), _ptr(k_pages), _ptr(v_pages))
+
+
+# ---------------------------------------------------------------------------
+# Write and attention
+# ---------------------------------------------------------------------------
+
+def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, freq=None, interleaved: bool = False,
+          magnitude: float = 1.0):
+    """Write new tokens k, v [B, M, H_kv, d] (heads and rows dense, B and M of any
+    strides) at positions start[b] + m of sequences rows[b] (None: b), m < n_new[b]
+    (None: M), into one layer's pools; with freq, keys are turned to their
+    positions as by rope."""
+    dev = k_pages.device
+    _, P, H, d = _pools(k_pages, v_pages)
+    ks, vs = _rows_of(k, "k", dev, k_pages.dtype), _rows_of(v, "v", dev, k_pages.dtype)
+    B, M = k.shape[:2]
+    if k.shape != (B, M, H, d) or v.shape != k.shape:
+        raise ValueError("k and v must be [B, M, H_kv, d] with the pools' heads")
+    if H > 1 and (ks[2] != d or vs[2] != d):
+        raise ValueError("the heads of k and v must be dense")
+    rot = 0 if freq is None else _freq(freq, d, dev)
+    n_seqs, max_pages = table.shape
+    for t, name, shape in ((table, "table", (n_seqs, max_pages)), (start, "start", (B,))):
+        _ints(t, name, shape, dev)
+    for t, name in ((rows, "rows"), (n_new, "n_new")):
+        if t is not None:
+            _ints(t, name, (B,), dev)
+    if rows is None and B > n_seqs:
+        raise ValueError("more entries than sequences")
+    _call("lla_kv_write", dev, _dt(k_pages), B, M, H, d, rot, int(interleaved), _ptr(k), *ks[:2], _ptr(v), *vs[:2],
+          _ptr(freq), float(magnitude), n_seqs, max_pages, P, _ptr(table), _ptr(rows), _ptr(start), _ptr(n_new),
+          _ptr(k_pages), _ptr(v_pages))
+
+
+def decode_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int, n_ctx: int, sink: int = 0,
+                           window: int = 0) -> int:
+    """Workspace of decode_attn (0: no context is split over workgroups)."""
+    out = _c_sz()
+    _check(lib().lla_kv_decode_workspace_bytes(_out_code(dtype), B, H, H_kv, d, n_ctx, sink, window, ctypes.byref(out)))
+    return out.value
+
+
+def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, scale: float | None = None,
+                sink: int = 0, window: int = 0, out=None, out_dtype=torch.float32, lse=None, workspace=None):
+    """Attention of q [B, H, d] over the pages of sequences rows[b] (None: b) with
+    length[row] <= n_ctx tokens each: all of them, or with ``window`` the first
+    ``sink`` and the last ``window``.  H is a multiple of the pools' heads.  An
+    empty sequence or row -1 gives zeros.  lse: float32 [B, H] or None; workspace:
+    uint8 of decode_workspace_bytes(...) (allocated here if None).  Returns out
+    [B, H, d]."""
+    dev = q.device
+    _, P, Hkv, d = _pools(k_pages, v_pages)
+    B, H, width = q.shape
+    _need(q, "q", k_pages.dtype, dev)
+    if width != d or k_pages.device != dev or v_pages.device != dev:
+        raise ValueError("q must be [B, H, d] with the pools' width, on their device")
+    n_seqs, max_pages = table.shape
+    for t, name, shape in ((table, "table", (n_seqs, max_pages)), (length, "length", (n_seqs,))):
+        _ints(t, name, shape, dev)
+    if rows is not None:
+        _ints(rows, "rows", (B,), dev)
+    if out is None:
+        out = torch.empty((B, H, d), dtype=out_dtype, device=dev)
+    else:
+        _need(out, "out", None, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    if lse is not None:
+        _need(lse, "lse", torch.float32, dev)
+        if lse.shape != (B, H):
+            raise ValueError("lse must be [B, H]")
+    if workspace is None:
+        need = decode_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx, sink, window)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    else:
+        _need(workspace, "workspace", None, dev)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("lla_kv_decode_attn", dev, _dt(q), _out_code(out.dtype), B, H, Hkv, d, n_seqs, max_pages, P, n_ctx, sink,
+          window, _ptr(table), _ptr(length), _ptr(rows), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+          float(1.0 / math.sqrt(d) if scale is None else scale), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes)
+    return out
