@@ -3,10 +3,31 @@
 //
 //   s_n = scale q . k_n,  o = sum_n softmax(s)_n v_n
 //
-// One workgroup per (entry, query head); a wavefront takes every fourth page.
-// Scores: a lane per token, 16 bytes of its key row at a time.  Values: a lane
-// per feature row, 64 weights from LDS.  A wavefront keeps its own running
-// maximum and sum; the four are joined in LDS.
+// Every key and value is read once for all query heads of its group, so the
+// bytes of the attended pages bound it: 2 d elements a token and key head, 4 d
+// flops a token and query head.
+//
+// A workgroup takes up to 16 query heads of one (entry, key head) and a slice of
+// its pages; a wavefront takes steps of 16 to 64 tokens, every W-th of the
+// slice's, with both products on the matrix instructions and all operands
+// straight from memory to registers:
+//
+//   S^T [tokens x heads] = K Q^T      A: 16 bytes of a key row (token-major)
+//   O^T [features x heads] += V^T P^T A: 16 bytes of a value row (feature-major)
+//
+// In a 16 x 16 accumulator lane (c, g) = (lane % 16, lane / 16) holds rows 4g ..
+// 4g + 3 of column c, a query head: maximum and sum stay with the lane until the
+// end, and its weights are the next product's B operand without a lane exchange
+// once the token of each row is chosen so (bf16: rows 4g' + i of the two tiles of
+// 32 tokens are tokens 8g' + i and 8g' + 4 + i; fp32: row and token are the same,
+// and product e of a tile takes element e of every lane's 16 bytes).  Groups of
+// fewer than 16 heads leave columns empty: at 16 columns the products take about
+// a tenth of the time that their operands take to arrive.
+//
+// The running maximum is raised only when a step exceeds it by more than 2^8, so
+// the accumulator is rarely rescaled; bf16 weights enter as hi + lo (2^-17).
+
+#include <algorithm>
 
 #include "kv_internal.h"
 #include "lla_device.h"
@@ -15,13 +36,30 @@
 namespace lla {
 namespace {
 
-constexpr int kWaves = 4, kThreads = kWaves * kWave;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
-// Pages and tokens that an entry attends: tokens [0, first) and [last, n).
+constexpr int kTile = 16;     // query heads of a workgroup
+constexpr float kLazy = 8.f;  // log2 by which a step may exceed the running maximum
+constexpr float kLn2 = 0.69314718055994531f;
+
+__device__ __forceinline__ BufRsrc make_rsrc(const void* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
+}
+__device__ __forceinline__ uint4 buf_ld16(BufRsrc r, int voff, int soff) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0));
+}
+// Uniform read of an index array (nothing in a launch writes one).
+typedef const int __attribute__((address_space(4))) ConstInt;
+__device__ __forceinline__ int uniform(const int32_t* p, int64_t i) {
+  return reinterpret_cast<ConstInt*>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
+// Tokens that an entry attends, [0, first) and [last, n), and their pages: the
+// sequence's pages 0 .. lead - 1, then lead + skip .. .
 struct Span {
-  int n;                // tokens of the sequence
-  int first, last;      // first: the sinks
-  int lead, skip, pages;  // pages 0 .. lead-1, then lead + skip .. ; their number
+  int n, first, last, lead, skip, pages;
   __device__ __forceinline__ Span(int len, int sink, int window) {
     n = len;
     const bool cut = window > 0 && (int64_t)sink + window < n;
@@ -34,110 +72,422 @@ struct Span {
   }
   __device__ __forceinline__ int page(int i) const { return i < lead ? i : i + skip; }
   __device__ __forceinline__ bool seen(int t) const { return t < first || (t >= last && t < n); }
+  // all tokens t .. t + count - 1
+  __device__ __forceinline__ bool whole(int t, int count) const {
+    return t + count <= first || (t >= last && t + count <= n);
+  }
 };
 
-__device__ __forceinline__ void store_row(const KvDecodeArgs& a, int64_t i, float v) {
-  if (a.out_dtype == LLA_BF16) store_out(static_cast<bf16_t*>(a.out), i, v);
-  else store_out(static_cast<float*>(a.out), i, v);
+// Entry b's tokens: 0 for padding, -1 where its row or length is out of range.
+__device__ __forceinline__ int entry_tokens(const KvDecodeArgs& a, int b, int& row) {
+  row = a.rows ? uniform(a.rows, b) : b;
+  if (row < 0 || row >= a.p.n_seqs) return a.rows && row == -1 ? 0 : -1;
+  const int n = uniform(a.length, row);
+  return n < 0 || n > a.n_ctx ? -1 : n;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void decode_simple_kernel(KvDecodeArgs a) {
-  __shared__ float s_q[kMaxHead];
-  __shared__ float s_p[kWaves][kPage];
-  __shared__ float s_o[kWaves][kMaxHead];
-  __shared__ float s_m[kWaves], s_l[kWaves];
-  __shared__ int s_bad;
-  const int b = blockIdx.x / a.H, h = blockIdx.x % a.H, d = a.p.d;
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
-  const int64_t row_out = (int64_t)blockIdx.x * d;
-  const int row = a.rows ? a.rows[b] : b;
-  int n = row >= 0 && row < a.p.n_seqs ? a.length[row] : row == -1 ? 0 : -1;
-  if (n > a.n_ctx) n = -1;
-  if (n <= 0) {
-    for (int i = tid; i < d; i += kThreads) store_row(a, row_out + i, n < 0 ? __builtin_nanf("") : 0.f);
-    if (a.lse && tid == 0) a.lse[blockIdx.x] = n < 0 ? __builtin_nanf("") : neg_inf();
-    return;
+// ---- one step of a wavefront ----
+
+// bf16: 64 tokens, 32 where a page's operands would not fit the registers.
+template <int D>
+struct StepBf16 {
+  static constexpr int kTok = D <= 128 ? 64 : 32, kTiles = kTok / 16, kBytes = 2;
+  static constexpr int KS = D / 32, FT = D / 16, UU = kTok / 32, kQueryLds = 0;
+  uint4 q[KS], k[kTiles][KS], v[FT][UU];
+
+  __device__ __forceinline__ void load_q(const void* row, int g, bool in, f32x4*) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      q[s] = in ? ld16(static_cast<const bf16_t*>(row) + 32 * s + 8 * g) : uint4{0, 0, 0, 0};
   }
-  const Span sp(n, a.sink, a.window);
-  const int kvh = h / (a.H / a.p.Hkv);
-  for (int i = tid; i < d; i += kThreads) s_q[i] = Elem<T>::get(static_cast<const T*>(a.q), row_out + i) * a.qscale;
-  if (tid == 0) s_bad = 0;
-  __syncthreads();
-  float m_run = neg_inf(), l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = w; i < sp.pages; i += kWaves) {
-    const int pg = sp.page(i);
-    const int page = a.p.table[(int64_t)row * a.p.max_pages + pg];
-    if (page < 0 || page >= a.p.n_pages) {
-      s_bad = 1;
-      break;
+  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int c, int g) {
+    const int lane = ((8 * (c / 4) + c % 4) * D + 8 * g) * 2;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        k[t][s] = buf_ld16(r, lane, ((tok + 32 * (t / 2) + 4 * (t % 2)) * D + 32 * s) * 2);
+  }
+  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int c, int g) {
+    const int lane = (c * kPage + 8 * g) * 2;
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int u = 0; u < UU; ++u) v[f][u] = buf_ld16(r, lane, (16 * f * kPage + tok + 32 * u) * 2);
+  }
+  // token of register i of tile t in this lane, from the step's first
+  __device__ __forceinline__ static int token(int t, int i, int g) { return 32 * (t / 2) + 8 * g + 4 * (t % 2) + i; }
+  __device__ __forceinline__ void scores(f32x4 (&sc)[kTiles]) const {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      sc[t] = f32x4{0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][s]),
+                                                        __builtin_bit_cast(bf16x8, q[s]), sc[t], 0, 0, 0);
     }
-    const int64_t at = ((int64_t)page * a.p.Hkv + kvh) * kPage * d;
-    const T* k = static_cast<const T*>(a.p.k) + at + lane * d;
-    const T* v = static_cast<const T*>(a.p.v) + at;
-    const bool seen = sp.seen(pg * kPage + lane);
-    float s = 0.f;
-    constexpr int V = Elem<T>::kPer16B;
-    for (int j = 0; j < d; j += V) {
-      float f[V];
-      Elem<T>::unpack(ld16(k + j), f);
-      for (int e = 0; e < V; ++e) s += f[e] * s_q[j + e];
+  }
+  // values of tokens not attended to zero, whatever their slots hold
+  template <typename Seen>
+  __device__ __forceinline__ void mask_values(const Seen& seen, int g) {
+#pragma unroll
+    for (int u = 0; u < UU; ++u) {
+      uint32_t keep[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        keep[i] = (seen(32 * u + 8 * g + 2 * i) ? 0xffffu : 0u) | (seen(32 * u + 8 * g + 2 * i + 1) ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+        v[f][u] = uint4{v[f][u].x & keep[0], v[f][u].y & keep[1], v[f][u].z & keep[2], v[f][u].w & keep[3]};
     }
-    if (!seen) s = neg_inf();
-    float mx = s;
-    for (int x = 32; x; x >>= 1) mx = fmaxf(mx, xor_shfl(mx, x));
-    const float m_new = fmaxf(m_run, mx), m_use = m_new == neg_inf() ? 0.f : m_new;
-    const float alpha = exp2f(m_run - m_use), p = exp2f(s - m_use);
-    float ps = p;
-    for (int x = 32; x; x >>= 1) ps += xor_shfl(ps, x);
-    l_run = l_run * alpha + ps;
-    m_run = m_new;
-    s_p[w][lane] = p;
-    __builtin_amdgcn_wave_barrier();
-    for (int r = 0; r < 4; ++r) {
-      const int f = lane + r * kWave;
-      if (f < d) {
-        float acc = 0.f;
-        for (int t = 0; t < kPage; ++t)
-          if (sp.seen(pg * kPage + t)) acc += s_p[w][t] * Elem<T>::get(v, f * kPage + t);
-        o[r] = o[r] * alpha + acc;
+  }
+  __device__ __forceinline__ void values(const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+#pragma unroll
+    for (int u = 0; u < UU; ++u) {
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = p[2 * u + e / 4][e % 4];
+        hi[e] = (__bf16)x;
+        lo[e] = (__bf16)(x - (float)hi[e]);
+      }
+#pragma unroll
+      for (int f = 0; f < FT; ++f) {
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[f][u]), hi, o[f], 0, 0, 0);
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[f][u]), lo, o[f], 0, 0, 0);
       }
     }
-    __builtin_amdgcn_wave_barrier();
   }
-  for (int r = 0; r < 4; ++r)
-    if (lane + r * kWave < d) s_o[w][lane + r * kWave] = o[r];
-  if (lane == 0) {
-    s_m[w] = m_run;
-    s_l[w] = l_run;
+};
+
+// fp32: 32 tokens, 16 above a width of 128; above 192 the queries do not fit the
+// registers beside them and are read from LDS again for every step.
+template <int D>
+struct StepF32 {
+  static constexpr int kTok = D <= 128 ? 32 : 16, kTiles = kTok / 16, kBytes = 4;
+  static constexpr int KS = D / 16, FT = D / 16, kQueryLds = D > 192 ? KS * kWave : 0;  // LDS, in 16 bytes
+  f32x4 q[kQueryLds ? 1 : KS], k[kTiles][KS], v[FT][kTiles];
+  f32x4* sq;
+
+  // (every wavefront writes the same values, and reads after its own)
+  __device__ __forceinline__ void load_q(const void* row, int g, bool in, f32x4* lds) {
+    sq = lds;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const f32x4 x = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
+      if constexpr (kQueryLds) sq[s * kWave] = x;
+      else q[s] = x;
+    }
   }
-  __syncthreads();
+  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int c, int g) {
+    const int lane = (c * D + 4 * g) * 4;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        k[t][s] = __builtin_bit_cast(f32x4, buf_ld16(r, lane, ((tok + 16 * t) * D + 16 * s) * 4));
+  }
+  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int c, int g) {
+    const int lane = (c * kPage + 4 * g) * 4;
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+        v[f][t] = __builtin_bit_cast(f32x4, buf_ld16(r, lane, (16 * f * kPage + tok + 16 * t) * 4));
+  }
+  __device__ __forceinline__ static int token(int t, int i, int g) { return 16 * t + 4 * g + i; }
+  __device__ __forceinline__ void scores(f32x4 (&sc)[kTiles]) const {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      sc[t] = f32x4{0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        f32x4 x;
+        if constexpr (kQueryLds) x = sq[s * kWave];
+        else x = q[s];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][s][e], x[e], sc[t], 0, 0, 0);
+      }
+    }
+  }
+  template <typename Seen>
+  __device__ __forceinline__ void mask_values(const Seen& seen, int g) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = seen(16 * t + 4 * g + e);
+#pragma unroll
+        for (int f = 0; f < FT; ++f) v[f][t][e] = in ? v[f][t][e] : 0.f;
+      }
+  }
+  __device__ __forceinline__ void values(const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+          o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[f][t][e], p[t][e], o[f], 0, 0, 0);
+  }
+};
+
+// ---- output rows ----
+
+// Four features from f on of row i (d wide).
+__device__ __forceinline__ void store4(const KvDecodeArgs& a, int64_t i, int f, f32x4 v) {
+  const int64_t at = i * a.p.d + f;
+  if (a.out_dtype == LLA_BF16) {
+    uint2 w;
+    w.x = f32_to_bf16(v[0]) | (uint32_t(f32_to_bf16(v[1])) << 16);
+    w.y = f32_to_bf16(v[2]) | (uint32_t(f32_to_bf16(v[3])) << 16);
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + at) = w;
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
+  }
+}
+
+// Partial of a slice: d sums, the maximum (log2 units), the sum of weights, padding.
+__device__ __forceinline__ float* partial(const KvDecodeArgs& a, int64_t row, int slice) {
+  return a.part + (row * a.slices + slice) * (a.p.d + 4);
+}
+
+// One (m, l, o[]) into another: o2 and l2 were weighed by 2^-m2.
+template <int FT>
+__device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m2, float l2, const float* o2) {
+  const float to = fmaxf(m, m2), base = to == neg_inf() ? 0.f : to;
+  const float x = __builtin_amdgcn_exp2f(m - base), y = __builtin_amdgcn_exp2f(m2 - base);
+  m = to;
+  l = l * x + l2 * y;
+#pragma unroll
+  for (int f = 0; f < FT; ++f) {
+    const f32x4 w = *reinterpret_cast<const f32x4*>(o2 + 16 * f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[f][i] = o[f][i] * x + w[i] * y;
+  }
+}
+
+template <typename Step, int D, int W>
+__global__ __launch_bounds__(W* kWave, 2) void decode_kernel(KvDecodeArgs a) {
+  constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
+  constexpr int kRow = D + 4;
+  __shared__ __align__(16) float s_o[W / 2 * kTile * kRow];
+  __shared__ float s_ml[W / 2][2][kTile];
+  __shared__ f32x4 s_q[Step::kQueryLds ? Step::kQueryLds : 1];
+  const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int units = a.B * a.p.Hkv;
+  const int slice = blockIdx.x / units, unit = blockIdx.x - slice * units;
+  const int b = unit / a.p.Hkv, kvh = unit - b * a.p.Hkv;
+  const int group = a.H / a.p.Hkv;
+  const int h = blockIdx.y * kTile + c;  // of the group
+  const bool in = h < group;
+  const int64_t out_row = (int64_t)b * a.H + kvh * group + h;
+
+  int row;
+  const int n = entry_tokens(a, b, row);
+  const Span sp(max(n, 0), a.sink, a.window);
+  const int pb = slice * a.per, pe = min(sp.pages, pb + a.per);
+  if (n <= 0 || pb >= pe) {
+    if (n <= 0 && slice == 0 && w == 0 && in && a.slices == 1) {
+      const float x = n < 0 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+      for (int f = 0; f < FT; ++f) store4(a, out_row, 16 * f + 4 * g, f32x4{x, x, x, x});
+      if (a.lse && g == 0) a.lse[out_row] = n < 0 ? x : neg_inf();
+    }
+    return;
+  }
+
+  Step st;
+  constexpr int kHeadBytes = kPage * D * Step::kBytes;
+  const int32_t* table = a.p.table + (int64_t)row * a.p.max_pages;
+  bool bad = false;
+  // step t of the slice's: its page's keys and values, and its first token there
+  auto block = [&](int t) -> int64_t {
+    int page = uniform(table, sp.page(t / kSteps));
+    bad |= page < 0 || page >= a.p.n_pages;
+    page = page < 0 || page >= a.p.n_pages ? 0 : page;
+    return ((int64_t)page * a.p.Hkv + kvh) * kHeadBytes;
+  };
+  auto keys = [&](int64_t at) { return make_rsrc(static_cast<const char*>(a.p.k) + at, kHeadBytes); };
+  auto vals = [&](int64_t at) { return make_rsrc(static_cast<const char*>(a.p.v) + at, kHeadBytes); };
+
+  int t = pb * kSteps + w;
+  const int end = pe * kSteps;
   float m = neg_inf(), l = 0.f;
-  for (int x = 0; x < kWaves; ++x) m = fmaxf(m, s_m[x]);
-  const float m_use = m == neg_inf() ? 0.f : m;
-  for (int x = 0; x < kWaves; ++x) l += s_l[x] * exp2f(s_m[x] - m_use);
-  if (s_bad) l = __builtin_nanf("");
-  for (int i = tid; i < d; i += kThreads) {
-    float acc = 0.f;
-    for (int x = 0; x < kWaves; ++x) acc += s_o[x][i] * exp2f(s_m[x] - m_use);
-    store_row(a, row_out + i, acc / l);
+  f32x4 o[FT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f) o[f] = f32x4{0.f};
+  if (t < end) {
+    const int64_t at = block(t);
+    const int tok = t % kSteps * Step::kTok;
+    st.load_k(keys(at), tok, c, g);
+    st.load_v(vals(at), tok, c, g);
   }
-  if (a.lse && tid == 0) a.lse[blockIdx.x] = (m_use + log2f(l)) * 0.69314718055994531f;
+  st.load_q(static_cast<const char*>(a.q) + out_row * D * Step::kBytes, g, in, s_q + lane);
+  // A step's keys are requested as soon as the scores before have consumed
+  // theirs, its values once the products before are issued.
+  for (; t < end; t += W) {
+    const bool more = t + W < end;
+    const int tok = (t + W) % kSteps * Step::kTok;
+    const int64_t next = more ? block(t + W) : 0;
+    f32x4 sc[kTiles];
+    st.scores(sc);
+    if (more) st.load_k(keys(next), tok, c, g);
+    const int t0 = sp.page(t / kSteps) * kPage + t % kSteps * Step::kTok;
+    const bool whole = sp.whole(t0, Step::kTok);
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!sp.seen(t0 + Step::token(x, i, g))) sc[x][i] = neg_inf();
+    }
+    float pm = neg_inf();
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pm = fmaxf(pm, sc[x][i]);
+    pm = fmaxf(pm, xor_shfl(pm, 16));
+    pm = fmaxf(pm, xor_shfl(pm, 32)) * a.qscale;
+    if (__any(pm > m + kLazy)) {
+      const float to = fmaxf(m, pm);
+      const float alpha = m == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(m - to);
+      l *= alpha;
+#pragma unroll
+      for (int f = 0; f < FT; ++f) o[f] *= alpha;
+      m = to;
+    }
+    const float base = m == neg_inf() ? 0.f : m;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], a.qscale, -base));
+        l += sc[x][i];
+      }
+    if (!whole) st.mask_values([&](int k) { return sp.seen(t0 + k); }, g);
+    st.values(sc, o);
+    if (more) st.load_v(vals(next), tok, c, g);
+  }
+  l += xor_shfl(l, 16);
+  l += xor_shfl(l, 32);
+  if (bad) l = __builtin_nanf("");
+
+  // join the wavefronts, the upper half into the lower
+#pragma unroll
+  for (int half = W / 2; half >= 1; half /= 2) {
+    if (w >= half && w < 2 * half) {
+      float* so = s_o + ((w - half) * kTile + c) * kRow + 4 * g;
+#pragma unroll
+      for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(so + 16 * f) = o[f];
+      if (g == 0) {
+        s_ml[w - half][0][c] = m;
+        s_ml[w - half][1][c] = l;
+      }
+    }
+    __syncthreads();
+    if (w < half) join<FT>(m, l, o, s_ml[w][0][c], s_ml[w][1][c], s_o + (w * kTile + c) * kRow + 4 * g);
+    if (half > 1) __syncthreads();
+  }
+  if (w != 0 || !in) return;
+  if (a.slices > 1) {
+    float* part = partial(a, out_row, slice);
+#pragma unroll
+    for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(part + 16 * f + 4 * g) = o[f];
+    if (g == 0) {
+      part[D] = m;
+      part[D + 1] = l;
+    }
+    return;
+  }
+#pragma unroll
+  for (int f = 0; f < FT; ++f) store4(a, out_row, 16 * f + 4 * g, o[f] / l);
+  if (a.lse && g == 0) a.lse[out_row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the slices of one (entry, query head).  A thread holds four features of
+// every R-th slice; R is what 256 threads allow.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
+  __shared__ __align__(16) float s_o[kJoinThreads * 4];
+  __shared__ float s_l[kJoinThreads];
+  const int64_t row_out = blockIdx.x;
+  const int b = blockIdx.x / a.H, tid = threadIdx.x, lanes = a.p.d / 4;
+  int row;
+  const int n = entry_tokens(a, b, row);
+  const Span sp(max(n, 0), a.sink, a.window);
+  const int slices = (sp.pages + a.per - 1) / a.per;
+  const int R = kJoinThreads / lanes, r = tid / lanes, f = tid % lanes;
+  float m = neg_inf(), l = 0.f;
+  f32x4 o = f32x4{0.f};
+  if (r < R) {
+    for (int s = 0; s < slices; ++s) m = fmaxf(m, partial(a, row_out, s)[a.p.d]);
+    const float base = m == neg_inf() ? 0.f : m;
+    for (int s = r; s < slices; s += R) {
+      const float* part = partial(a, row_out, s);
+      const float x = __builtin_amdgcn_exp2f(part[a.p.d] - base);
+      l += part[a.p.d + 1] * x;
+      o += *reinterpret_cast<const f32x4*>(part + 4 * f) * x;
+    }
+  }
+  *reinterpret_cast<f32x4*>(&s_o[4 * tid]) = o;
+  s_l[tid] = l;
+  __syncthreads();
+  if (r == 0) {
+    for (int x = 1; x < R; ++x) {
+      o += *reinterpret_cast<const f32x4*>(&s_o[4 * (tid + x * lanes)]);
+      l += s_l[tid + x * lanes];
+    }
+    const float none = n < 0 ? __builtin_nanf("") : 0.f;
+    const bool empty = n <= 0;
+    store4(a, row_out, 4 * f, empty ? f32x4{none, none, none, none} : o / l);
+    if (a.lse && f == 0)
+      a.lse[row_out] = n < 0 ? none : empty ? neg_inf() : ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+template <int D>
+hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
+  constexpr int W = 4;
+  const dim3 grid(a.B * a.p.Hkv * a.slices, (a.H / a.p.Hkv + kTile - 1) / kTile);
+  if (a.p.dtype == LLA_BF16) hipLaunchKernelGGL((decode_kernel<StepBf16<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((decode_kernel<StepF32<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.slices == 1) return e;
+  hipLaunchKernelGGL(join_kernel, dim3(a.B * a.H), dim3(kJoinThreads), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 size_t kv_decode_shape(KvDecodeArgs& a) {
-  a.slices = 1;
-  a.per = (a.n_ctx + kPage - 1) / kPage;
-  return 0;
+  const int all = (a.n_ctx + kPage - 1) / kPage;
+  // most pages that an entry attends
+  const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
+  const int pages = a.window ? (int)std::min<int64_t>(all, budget) : all;
+  const int64_t units = (int64_t)a.B * a.p.Hkv * ((a.H / a.p.Hkv + kTile - 1) / kTile);
+  const int64_t want = std::max<int64_t>(1, (2 * device_cu_count() + units - 1) / units);
+  a.per = (int)std::max<int64_t>(8, (pages + want - 1) / want);
+  a.slices = (pages + a.per - 1) / a.per;
+  if (a.slices == 1) {
+    a.per = pages;
+    return 0;
+  }
+  return (size_t)a.B * a.H * a.slices * (a.p.d + 4) * sizeof(float);
 }
 
 hipError_t launch_kv_decode(const KvDecodeArgs& a, hipStream_t stream) {
-  const dim3 grid(a.B * a.H);
-  if (a.p.dtype == LLA_BF16) hipLaunchKernelGGL(decode_simple_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL(decode_simple_kernel<float>, grid, dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  switch (a.p.d) {
+    case 32: return launch<32>(a, stream);
+    case 64: return launch<64>(a, stream);
+    case 96: return launch<96>(a, stream);
+    case 128: return launch<128>(a, stream);
+    case 160: return launch<160>(a, stream);
+    case 192: return launch<192>(a, stream);
+    case 224: return launch<224>(a, stream);
+    default: return launch<256>(a, stream);
+  }
 }
 
 }  // namespace lla

@@ -761,7 +761,7 @@ def test_refusals_on_the_device():
                 lambda: kv.rope(q[None].transpose(2, 3), torch.ones(2, device=DEV, dtype=torch.float64)),
                 lambda: kv.gather(c.k, c.v, c.table, ints([0]), ints([0]), ints([0])),
                 lambda: kv.copy_pages(c.k, c.v[:1], ints([[0, 0]]))):
-        with pytest.raises((ValueError, TypeError)):
+        with pytest.raises((ValueError, TypeError, lla.LLAError)):
             bad()
     for bad in (dict(n_ctx=0), dict(n_ctx=65), dict(n_ctx=64, sink=2), dict(n_ctx=64, window=-1),
                 dict(n_ctx=64, scale=0.0)):

@@ -142,6 +142,11 @@ def test_workspace_refused():
     assert fn(*{**good, "workspace": None}.values()) == lla.LLA_ERR_WORKSPACE       # bytes without a buffer
     assert fn(*{**good, "ws_bytes": 0}.values()) == lla.LLA_ERR_WORKSPACE           # a buffer without bytes
     assert fn(*{**good, "workspace": P + 8}.values()) == lla.LLA_ERR_WORKSPACE
+    long = {**good, "B": 1, "n_ctx": 32768, "max_pages": 512, "H": 4}
+    need = kv.decode_workspace_bytes(torch.bfloat16, 1, 4, 4, 64, 32768)
+    assert need > 0
+    assert fn(*{**long, "ws_bytes": need - 1}.values()) == lla.LLA_ERR_WORKSPACE
+    assert fn(*{**long, "workspace": None, "ws_bytes": 0}.values()) == lla.LLA_ERR_WORKSPACE
     for bad in (dict(B=0), dict(n_ctx=0), dict(H=3, H_kv=2), dict(d=100), dict(window=-1), dict(sink=3)):
         args = {**dict(dtype=torch.float32, B=1, H=4, H_kv=4, d=64, n_ctx=100), **bad}
         with pytest.raises(lla.LLAError):
