@@ -1,9 +1,9 @@
 // Write of new tokens' keys and values into their sequences' pages, the keys
 // turned to their positions on the way.
 //
-// A workgroup takes the new tokens of one entry that fall into one page, for
-// one key head.  Keys are rows of the page as they are rows of the input; values
-// turn from token rows into the page's feature rows.
+// Bound by memory: every element is read and written once.  Keys are rows of the
+// page as they are rows of the input; values turn from token rows into the
+// page's feature rows.
 
 #include "kv_internal.h"
 #include "rotary.h"
@@ -14,63 +14,182 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T, bool Interleaved>
-__global__ __launch_bounds__(kThreads) void write_kernel(KvWriteArgs a, int blocks) {
-  const int b = blockIdx.x / blocks, h = blockIdx.y, d = a.p.d, tid = threadIdx.x;
-  const int row = a.rows ? a.rows[b] : b;
-  const int64_t first = a.start[b];
-  if (first < 0 || row < 0 || row >= a.p.n_seqs) return;
-  const int n = a.n_new ? max(0, min(a.n_new[b], a.M)) : a.M;
-  const int64_t slot = first / kPage + blockIdx.x % blocks;  // page of the sequence
-  if (slot >= a.p.max_pages) return;
-  // tokens [m0, m1) at positions t0 .. of the page
-  const int64_t base = slot * kPage - first;
-  const int m0 = (int)max((int64_t)0, base), m1 = (int)min((int64_t)n, base + kPage);
+// Where the tokens of entry b go: the first position and how many there are.
+struct Entry {
+  int row, n;
+  int64_t first;
+  __device__ __forceinline__ Entry(const KvWriteArgs& a, int b) {
+    row = a.rows ? a.rows[b] : b;
+    first = a.start[b];
+    n = a.n_new ? max(0, min(a.n_new[b], a.M)) : a.M;
+    if (first < 0 || row < 0 || row >= a.p.n_seqs) n = 0;
+  }
+  // page number of the sequence's page `slot`, -1 where it has none
+  __device__ __forceinline__ int page(const KvWriteArgs& a, int64_t slot) const {
+    if (slot >= a.p.max_pages) return -1;
+    const int p = a.p.table[(int64_t)row * a.p.max_pages + slot];
+    return p < a.p.n_pages ? p : -1;
+  }
+};
+
+// Few tokens: one thread per (token, head) and run of N key pairs, of 8 copied
+// key features, or of 8 value features (stored one by one: a token is one
+// element of every feature row).
+template <typename T, int N, bool Interleaved>
+__global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
+  const int d = a.p.d, half = a.rot / 2, turned = half / N, kept = (d - a.rot) / 8, units = turned + kept + d / 8;
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t at = idx / units;  // (b, m, h)
+  const int u = (int)(idx - at * units);
+  if (at >= (int64_t)a.B * a.M * a.p.Hkv) return;
+  const int h = (int)(at % a.p.Hkv), bm = (int)(at / a.p.Hkv), b = bm / a.M, m = bm - b * a.M;
+  const T* k = static_cast<const T*>(a.k) + b * a.kb + m * a.km + (int64_t)h * d;
+  const T* v = static_cast<const T*>(a.v) + b * a.vb + m * a.vm + (int64_t)h * d;
+  // the input is requested before the chain of entry, page and angle
+  Pairs<T, N, Interleaved> p;
+  Run<T, 8> r;
+  double freq[N];
+  if (u < turned) {
+    p.load(k, u * N, half);
+    load_freq(freq, a.freq + u * N);
+  } else {
+    r = Run<T, 8>::load(u < turned + kept ? k + a.rot + 8 * (u - turned) : v + 8 * (u - turned - kept));
+  }
+  const Entry e(a, b);
+  if (m >= e.n) return;
+  const int64_t pos = e.first + m;
+  const int page = e.page(a, pos / kPage), t = (int)(pos % kPage);
+  if (page < 0) return;
+  const int64_t unit = ((int64_t)page * a.p.Hkv + h) * kPage * d;
+  T* kp = static_cast<T*>(a.p.k) + unit + t * d;
+  T* vp = static_cast<T*>(a.p.v) + unit + t;
+  if (u < turned) {
+    Turn<N> turn;
+    turn.at((double)pos, freq, a.magnitude, 1.f);
+    p.turn(turn);
+    p.store(kp, u * N, half);
+  } else if (u < turned + kept) {
+    r.store(kp + a.rot + 8 * (u - turned));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) store_out(vp, (8 * (u - turned - kept) + i) * kPage, r.get(i));
+  }
+}
+
+// Prompts: a workgroup takes the tokens of one entry that fall into one page, for
+// `heads_per` key heads.  A thread turns a run of pairs of one token for all of
+// these heads; values go through LDS, up to 128 features of a head at a time, read
+// there by columns, 16 bytes of a feature row at a time.
+template <typename T, int N, bool Interleaved>
+__global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int blocks, int heads_per) {
+  constexpr int V = Elem<T>::kPer16B, HU = 4;
+  constexpr int kCols = 128, kRow = kCols + V;  // value features in LDS at a time
+  __shared__ __align__(16) T s_v[kPage * kRow];
+  const int b = blockIdx.x / blocks, d = a.p.d, tid = threadIdx.x;
+  const Entry e(a, b);
+  const int64_t slot = e.first / kPage + blockIdx.x % blocks;
+  // tokens [m0, m1), at positions t0 .. t1 - 1 of the page
+  const int64_t base = slot * kPage - e.first;
+  const int m0 = (int)max((int64_t)0, base), m1 = (int)min((int64_t)e.n, base + kPage);
   if (m0 >= m1) return;
-  const int t0 = (int)(m0 - base);
-  const int page = a.p.table[(int64_t)row * a.p.max_pages + slot];
-  if (page < 0 || page >= a.p.n_pages) return;
-  const int64_t at = ((int64_t)page * a.p.Hkv + h) * kPage * d;
-  T* kp = static_cast<T*>(a.p.k) + at;
-  T* vp = static_cast<T*>(a.p.v) + at;
-  const T* k = static_cast<const T*>(a.k) + b * a.kb + (int64_t)h * d;
-  const T* v = static_cast<const T*>(a.v) + b * a.vb + (int64_t)h * d;
-  const int half = a.rot / 2, turned = half / 4, units = turned + (d - a.rot) / 8;
-  for (int e = tid; e < (m1 - m0) * units; e += kThreads) {
-    const int i = e / units, u = e - i * units, m = m0 + i;
-    const T* x = k + m * a.km;
-    T* y = kp + (t0 + i) * d;
+  const int page = e.page(a, slot);
+  if (page < 0) return;
+  const int t0 = (int)(m0 - base), t1 = t0 + (m1 - m0), count = m1 - m0;
+  const int h0 = blockIdx.y * heads_per, h1 = min(a.p.Hkv, h0 + heads_per);
+  const int64_t head = (int64_t)kPage * d, unit = (int64_t)page * a.p.Hkv * head;
+  const T* k = static_cast<const T*>(a.k) + b * a.kb + m0 * a.km;
+  const T* v = static_cast<const T*>(a.v) + b * a.vb + m0 * a.vm;
+  T* kp = static_cast<T*>(a.p.k) + unit + t0 * d;
+  T* vp = static_cast<T*>(a.p.v) + unit;
+
+  const int half = a.rot / 2, turned = half / N, units = turned + (d - a.rot) / 8;
+  for (int x = tid; x < count * units; x += kThreads) {
+    const int i = x / units, u = x - i * units;
+    const T* from = k + i * a.km;
+    T* to = kp + i * d;
     if (u < turned) {
-      Turn<4> t;
-      t.at((double)(first + m), a.freq + 4 * u, a.magnitude, 1.f);
-      Pairs<T, 4, Interleaved> p;
-      p.load(x, 4 * u, half);
-      p.turn(t);
-      p.store(y, 4 * u, half);
+      Turn<N> t;
+      for (int h = h0; h < h1; h += HU) {
+        Pairs<T, N, Interleaved> p[HU];
+#pragma unroll
+        for (int y = 0; y < HU; ++y) p[y].load(from + (int64_t)min(h + y, h1 - 1) * d, u * N, half);
+        if (h == h0) {
+          double freq[N];
+          load_freq(freq, a.freq + u * N);
+          t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
+        }
+#pragma unroll
+        for (int y = 0; y < HU; ++y) {
+          p[y].turn(t);
+          if (h + y < h1) p[y].store(to + (h + y) * head, u * N, half);
+        }
+      }
     } else {
       const int f = a.rot + 8 * (u - turned);
-      Run<T, 8>::load(x + f).store(y + f);
+      for (int h = h0; h < h1; ++h) Run<T, 8>::load(from + (int64_t)h * d + f).store(to + h * head + f);
     }
   }
-  for (int e = tid; e < kPage * d; e += kThreads) {
-    const int f = e / kPage, t = e - f * kPage, m = m0 + t - t0;
-    if (m >= m0 && m < m1) vp[e] = v[m * a.vm + f];
+
+  for (int h = h0; h < h1; ++h) {
+    for (int f0 = 0; f0 < d; f0 += kCols) {
+      const int cols = min(kCols, d - f0), chunks = cols / V;
+      const T* from = v + (int64_t)h * d + f0;
+      for (int x = tid; x < count * chunks; x += kThreads) {
+        const int i = x / chunks, f = x - i * chunks;
+        *reinterpret_cast<uint4*>(s_v + (t0 + i) * kRow + f * V) = ld16(from + i * a.vm + f * V);
+      }
+      __syncthreads();
+      T* to = vp + h * head + f0 * kPage;
+      // 64 / V runs of a feature row side by side, so a row's lines are written together
+      constexpr int kRuns = kPage / V;
+      for (int x = tid; x < cols * kRuns; x += kThreads) {
+        const int f = x / kRuns, t = (x - f * kRuns) * V;
+        if (t + V <= t0 || t >= t1) continue;
+        if (t >= t0 && t + V <= t1) {
+          Run<T, V> r;
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[(t + i) * kRow + f]);
+            else if (i % 2 == 0) r.w[i / 2] = s_v[(t + i) * kRow + f] | (uint32_t(s_v[(t + i + 1) * kRow + f]) << 16);
+          }
+          r.store(to + f * kPage + t);
+        } else {
+          for (int i = max(t, t0); i < min(t + V, t1); ++i) to[f * kPage + i] = s_v[i * kRow + f];
+        }
+      }
+      __syncthreads();
+    }
   }
+}
+
+template <typename T, int N, bool Interleaved>
+hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
+  const int d = a.p.d;
+  if (a.M < 16) {
+    const int units = a.rot / 2 / N + (d - a.rot) / 8 + d / 8;
+    const int64_t runs = (int64_t)a.B * a.M * a.p.Hkv * units;
+    hipLaunchKernelGGL((write_few_kernel<T, N, Interleaved>), dim3((unsigned)((runs + kThreads - 1) / kThreads)),
+                       dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  const int blocks = (a.M + 2 * kPage - 2) / kPage;  // pages that M positions can touch
+  const int heads_per = 4;
+  hipLaunchKernelGGL((write_page_kernel<T, N, Interleaved>), dim3(a.B * blocks, (a.p.Hkv + heads_per - 1) / heads_per),
+                     dim3(kThreads), 0, stream, a, blocks, heads_per);
+  return hipGetLastError();
+}
+
+template <typename T, bool Interleaved>
+hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
+  if (sizeof(T) == 2 && a.rot % 16 == 0) return launch<T, 8, Interleaved>(a, stream);
+  return launch<T, 4, Interleaved>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t stream) {
-  const int blocks = (a.M + 2 * kPage - 2) / kPage;  // pages that M positions can touch
-  const dim3 grid(a.B * blocks, a.p.Hkv);
-  if (a.p.dtype == LLA_BF16) {
-    if (a.interleaved) hipLaunchKernelGGL((write_kernel<bf16_t, true>), grid, dim3(kThreads), 0, stream, a, blocks);
-    else hipLaunchKernelGGL((write_kernel<bf16_t, false>), grid, dim3(kThreads), 0, stream, a, blocks);
-  } else {
-    if (a.interleaved) hipLaunchKernelGGL((write_kernel<float, true>), grid, dim3(kThreads), 0, stream, a, blocks);
-    else hipLaunchKernelGGL((write_kernel<float, false>), grid, dim3(kThreads), 0, stream, a, blocks);
-  }
-  return hipGetLastError();
+  if (a.p.dtype == LLA_BF16) return a.interleaved ? launch<bf16_t, true>(a, stream) : launch<bf16_t, false>(a, stream);
+  return a.interleaved ? launch<float, true>(a, stream) : launch<float, false>(a, stream);
 }
 
 }  // namespace lla

@@ -2,9 +2,8 @@
 // pairs, shared by the embedding of queries (rotary.hip) and the write of keys
 // into their pages (kv_write.hip).
 //
-// A thread holds the N pairs of one token and turns them for one head after
-// another, so the angle (64-bit product and reduction, about 60 instructions a
-// pair with sine and cosine) is paid once per token, not once per head.
+// A thread holds the N pairs of one token and turns them for several heads, so
+// the angle (64-bit product and reduction, sine and cosine) is paid once.
 #pragma once
 
 #include "lla_device.h"
@@ -34,24 +33,49 @@ __device__ __forceinline__ void Run<T, N>::set(int i, float v) {
                         : (w[i / 2] & 0xffff0000u) | f32_to_bf16(v);
 }
 
-// magnitude * (cos, sin) of position * freq, the angle reduced to [-pi, pi] in
-// 64 bits (positions reach 2^31) and evaluated in 32.
+// cos and sin of an angle: in 64 bits the angle is brought to within pi/4 of a
+// multiple j of pi/2 (positions reach 2^31: the product is right to 2^-22 there),
+// in 32 their series about 0 are summed (the first terms left out are below
+// 2e-9) and go by j's quarter.  About 30 instructions, half of the library's
+// sincosf, which has to be ready for any argument.
+__device__ __forceinline__ void cos_sin(double angle, float& c, float& s) {
+  constexpr double kHalfPi = 1.5707963267948966192313216916398;
+  const double j = rint(angle * (1.0 / kHalfPi));
+  const float y = (float)__builtin_fma(-j, kHalfPi, angle), z = y * y;
+  const int quarter = (int)(j - 4.0 * rint(j * 0.25));  // -2 .. 2
+  float sn = __builtin_fmaf(z, 1.f / 362880.f, -1.f / 5040.f);
+  sn = __builtin_fmaf(sn, z, 1.f / 120.f);
+  sn = __builtin_fmaf(sn, z, -1.f / 6.f);
+  sn = __builtin_fmaf(sn * z, y, y);
+  float cs = __builtin_fmaf(z, -1.f / 3628800.f, 1.f / 40320.f);
+  cs = __builtin_fmaf(cs, z, -1.f / 720.f);
+  cs = __builtin_fmaf(cs, z, 1.f / 24.f);
+  cs = __builtin_fmaf(cs, z, -0.5f);
+  cs = __builtin_fmaf(cs, z, 1.f);
+  const float u = quarter & 1 ? sn : cs, v = quarter & 1 ? cs : sn;
+  c = (quarter + 1) & 2 ? -u : u;
+  s = quarter & 2 ? -v : v;
+}
+
+// magnitude * (cos, sin) of position * freq for N pairs.
 template <int N>
 struct Turn {
   float c[N], s[N];
-  __device__ __forceinline__ void at(double pos, const double* freq, float magnitude, float sign) {
-    constexpr double kTwoPi = 6.283185307179586476925286766559;
+  __device__ __forceinline__ void at(double pos, const double (&freq)[N], float magnitude, float sign) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const double ang = pos * freq[i];
-      const double r = ang - rint(ang * (1.0 / kTwoPi)) * kTwoPi;
       float sn, cs;
-      sincosf((float)r, &sn, &cs);
+      cos_sin(pos * freq[i], cs, sn);
       c[i] = magnitude * cs;
       s[i] = magnitude * sign * sn;
     }
   }
 };
+template <int N>
+__device__ __forceinline__ void load_freq(double (&f)[N], const double* p) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = p[i];
+}
 
 // The N pairs from pair p0 on of the row at x, turned, to the row at y (which
 // may be x): features (i, i + half), or (2i, 2i + 1) when interleaved.
