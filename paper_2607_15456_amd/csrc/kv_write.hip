@@ -77,15 +77,16 @@ __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
 }
 
 // Prompts: a workgroup takes the tokens of one entry that fall into one page, for
-// `heads_per` key heads.  A thread turns a run of pairs of one token for all of
-// these heads; values go through LDS, up to 128 features of a head at a time, read
-// there by columns, 16 bytes of a feature row at a time.
+// one key head, its keys or its values.  Values go through LDS, up to 128 features
+// at a time, read there by columns, 16 bytes of a feature row at a time.  Small
+// workgroups keep many loads in flight: prompts of 4001 to 2501 tokens, 16 heads of
+// 128, take 47 us (4.5 TB/s; a large copy runs at 4.8), with one angle for 2, 4 or
+// 16 heads of a workgroup 48, 51, 84; without non-temporal stores 6 us more.
 template <typename T, int N, bool Interleaved>
-__global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int blocks, int heads_per) {
-  constexpr int V = Elem<T>::kPer16B, HU = 4;
-  constexpr int kCols = 128, kRow = kCols + V;  // value features in LDS at a time
+__global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int blocks) {
+  constexpr int V = Elem<T>::kPer16B, kCols = 128, kRow = kCols + V;
   __shared__ __align__(16) T s_v[kPage * kRow];
-  const int b = blockIdx.x / blocks, d = a.p.d, tid = threadIdx.x;
+  const int b = blockIdx.x / blocks, h = blockIdx.y, d = a.p.d, tid = threadIdx.x;
   const Entry e(a, b);
   const int64_t slot = e.first / kPage + blockIdx.x % blocks;
   // tokens [m0, m1), at positions t0 .. t1 - 1 of the page
@@ -95,77 +96,69 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
   const int page = e.page(a, slot);
   if (page < 0) return;
   const int t0 = (int)(m0 - base), t1 = t0 + (m1 - m0), count = m1 - m0;
-  const int h0 = blockIdx.y * heads_per, h1 = min(a.p.Hkv, h0 + heads_per);
-  const int64_t head = (int64_t)kPage * d, unit = (int64_t)page * a.p.Hkv * head;
-  const T* k = static_cast<const T*>(a.k) + b * a.kb + m0 * a.km;
-  const T* v = static_cast<const T*>(a.v) + b * a.vb + m0 * a.vm;
-  T* kp = static_cast<T*>(a.p.k) + unit + t0 * d;
-  T* vp = static_cast<T*>(a.p.v) + unit;
+  const int64_t unit = ((int64_t)page * a.p.Hkv + h) * kPage * d;
 
-  const int half = a.rot / 2, turned = half / N, units = turned + (d - a.rot) / 8;
-  for (int x = tid; x < count * units; x += kThreads) {
-    const int i = x / units, u = x - i * units;
-    const T* from = k + i * a.km;
-    T* to = kp + i * d;
-    if (u < turned) {
-      Turn<N> t;
-      for (int h = h0; h < h1; h += HU) {
-        Pairs<T, N, Interleaved> p[HU];
-#pragma unroll
-        for (int y = 0; y < HU; ++y) p[y].load(from + (int64_t)min(h + y, h1 - 1) * d, u * N, half);
-        if (h == h0) {
-          double freq[N];
-          load_freq(freq, a.freq + u * N);
-          t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
-        }
-#pragma unroll
-        for (int y = 0; y < HU; ++y) {
-          p[y].turn(t);
-          if (h + y < h1) p[y].store(to + (h + y) * head, u * N, half);
-        }
+  if (blockIdx.z == 0) {
+    const T* k = static_cast<const T*>(a.k) + b * a.kb + m0 * a.km + (int64_t)h * d;
+    T* kp = static_cast<T*>(a.p.k) + unit + t0 * d;
+    const int half = a.rot / 2, turned = half / N, units = turned + (d - a.rot) / 8;
+    for (int x = tid; x < count * units; x += kThreads) {
+      const int i = x / units, u = x - i * units;
+      if (u < turned) {
+        Pairs<T, N, Interleaved> p;
+        p.load(k + i * a.km, u * N, half);
+        double freq[N];
+        load_freq(freq, a.freq + u * N);
+        Turn<N> t;
+        t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
+        p.turn(t);
+        p.template store<true>(kp + i * d, u * N, half);
+      } else {
+        const int f = a.rot + 8 * (u - turned);
+        Run<T, 8>::load(k + i * a.km + f).template store<true>(kp + i * d + f);
       }
-    } else {
-      const int f = a.rot + 8 * (u - turned);
-      for (int h = h0; h < h1; ++h) Run<T, 8>::load(from + (int64_t)h * d + f).store(to + h * head + f);
     }
+    return;
   }
 
-  for (int h = h0; h < h1; ++h) {
-    for (int f0 = 0; f0 < d; f0 += kCols) {
-      const int cols = min(kCols, d - f0), chunks = cols / V;
-      const T* from = v + (int64_t)h * d + f0;
-      for (int x = tid; x < count * chunks; x += kThreads) {
-        const int i = x / chunks, f = x - i * chunks;
-        *reinterpret_cast<uint4*>(s_v + (t0 + i) * kRow + f * V) = ld16(from + i * a.vm + f * V);
-      }
-      __syncthreads();
-      T* to = vp + h * head + f0 * kPage;
-      // 64 / V runs of a feature row side by side, so a row's lines are written together
-      constexpr int kRuns = kPage / V;
-      for (int x = tid; x < cols * kRuns; x += kThreads) {
-        const int f = x / kRuns, t = (x - f * kRuns) * V;
-        if (t + V <= t0 || t >= t1) continue;
-        if (t >= t0 && t + V <= t1) {
-          Run<T, V> r;
+  for (int f0 = 0; f0 < d; f0 += kCols) {
+    const int cols = min(kCols, d - f0), chunks = cols / V;
+    const T* v = static_cast<const T*>(a.v) + b * a.vb + m0 * a.vm + (int64_t)h * d + f0;
+    T* vp = static_cast<T*>(a.p.v) + unit + f0 * kPage;
+    if (f0) __syncthreads();
+    for (int x = tid; x < count * chunks; x += kThreads) {
+      const int i = x / chunks, f = x - i * chunks;
+      *reinterpret_cast<uint4*>(s_v + (t0 + i) * kRow + f * V) = ld16(v + i * a.vm + f * V);
+    }
+    __syncthreads();
+    // 64 / V runs of a feature row side by side, so a row's lines are written together
+    constexpr int kRuns = kPage / V;
+    for (int x = tid; x < cols * kRuns; x += kThreads) {
+      const int f = x / kRuns, t = (x - f * kRuns) * V;
+      if (t + V <= t0 || t >= t1) continue;
+      if (t >= t0 && t + V <= t1) {
+        Run<T, V> r;
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[(t + i) * kRow + f]);
-            else if (i % 2 == 0) r.w[i / 2] = s_v[(t + i) * kRow + f] | (uint32_t(s_v[(t + i + 1) * kRow + f]) << 16);
-          }
-          r.store(to + f * kPage + t);
-        } else {
-          for (int i = max(t, t0); i < min(t + V, t1); ++i) to[f * kPage + i] = s_v[i * kRow + f];
+        for (int i = 0; i < V; ++i) {
+          if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[(t + i) * kRow + f]);
+          else if (i % 2 == 0) r.w[i / 2] = s_v[(t + i) * kRow + f] | (uint32_t(s_v[(t + i + 1) * kRow + f]) << 16);
         }
+        r.template store<true>(vp + f * kPage + t);
+      } else {
+        for (int i = max(t, t0); i < min(t + V, t1); ++i) vp[f * kPage + i] = s_v[i * kRow + f];
       }
-      __syncthreads();
     }
   }
 }
 
+// From kPaged tokens an entry the page kernel is the faster one (32 entries, 16 heads of 128,
+// bf16, few / page: 2 tokens 6.0 / 6.5 us, 4 6.9 / 6.7, 8 9.6 / 6.2, 15 12.3 / 9.4).
+constexpr int kPaged = 4;
+
 template <typename T, int N, bool Interleaved>
 hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
   const int d = a.p.d;
-  if (a.M < 16) {
+  if (a.M < kPaged) {
     const int units = a.rot / 2 / N + (d - a.rot) / 8 + d / 8;
     const int64_t runs = (int64_t)a.B * a.M * a.p.Hkv * units;
     hipLaunchKernelGGL((write_few_kernel<T, N, Interleaved>), dim3((unsigned)((runs + kThreads - 1) / kThreads)),
@@ -173,9 +166,8 @@ hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
     return hipGetLastError();
   }
   const int blocks = (a.M + 2 * kPage - 2) / kPage;  // pages that M positions can touch
-  const int heads_per = 4;
-  hipLaunchKernelGGL((write_page_kernel<T, N, Interleaved>), dim3(a.B * blocks, (a.p.Hkv + heads_per - 1) / heads_per),
-                     dim3(kThreads), 0, stream, a, blocks, heads_per);
+  hipLaunchKernelGGL((write_page_kernel<T, N, Interleaved>), dim3(a.B * blocks, a.p.Hkv, 2), dim3(kThreads), 0, stream, a,
+                     blocks);
   return hipGetLastError();
 }
 

@@ -22,9 +22,8 @@ __device__ __forceinline__ int64_t position(const RotaryArgs& a, int b, int m) {
 }
 
 // One thread per (token, run of N pairs or of 8 copied features) and chunk of
-// heads (blockIdx.y), HU heads' rows in flight at a time: their loads are issued
-// before any store (y may be x), the first ones before the angle is formed.
-template <typename T, int N, bool Interleaved, int HU>
+// heads (blockIdx.y).
+template <typename T, int N, bool Interleaved, bool Past>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int units, int heads_per) {
   const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t tok = idx / units;
@@ -36,52 +35,41 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int unit
   T* y = static_cast<T*>(a.y) + b * a.yb + m * a.ym;
   const int half = a.rot / 2, turned = half / N;
   if (u < turned) {
+    Pairs<T, N, Interleaved> p;
+    p.load(x + h0 * a.xh, u * N, half);  // on its way while the angle is formed
+    double freq[N];
+    load_freq(freq, a.freq + u * N);
     Turn<N> t;
-    for (int h = h0; h < h1; h += HU) {
-      Pairs<T, N, Interleaved> p[HU];
-#pragma unroll
-      for (int k = 0; k < HU; ++k) p[k].load(x + min(h + k, h1 - 1) * a.xh, u * N, half);
-      if (h == h0) {
-        double freq[N];
-        load_freq(freq, a.freq + u * N);
-        t.at((double)position(a, b, m), freq, a.magnitude, a.sign);
-      }
-#pragma unroll
-      for (int k = 0; k < HU; ++k) {
-        p[k].turn(t);
-        if (h + k < h1) p[k].store(y + (h + k) * a.yh, u * N, half);
-      }
+    t.at((double)position(a, b, m), freq, a.magnitude, a.sign);
+    for (int h = h0;;) {
+      p.turn(t);
+      p.template store<Past>(y + h * a.yh, u * N, half);
+      if (++h >= h1) break;
+      p.load(x + h * a.xh, u * N, half);
     }
   } else {
     const int f = a.rot + 8 * (u - turned);
-    for (int h = h0; h < h1; h += HU) {
-      Run<T, 8> p[HU];
-#pragma unroll
-      for (int k = 0; k < HU; ++k) p[k] = Run<T, 8>::load(x + min(h + k, h1 - 1) * a.xh + f);
-#pragma unroll
-      for (int k = 0; k < HU; ++k)
-        if (h + k < h1) p[k].store(y + (h + k) * a.yh + f);
-    }
+    for (int h = h0; h < h1; ++h) Run<T, 8>::load(x + h * a.xh + f).template store<Past>(y + h * a.yh + f);
   }
 }
 
+// Few rows get a thread for each head, so that they spread over the device; from
+// kMany runs on a thread turns two heads with one angle and stores past the
+// caches, which the result no longer fits (4 x 8192 tokens of 16 heads of 128,
+// bf16: one head 57 us, two 45, four 47; two without the non-temporal stores 53;
+// 3 x 1501 tokens of 16 heads of 96, fp32, 64 turned: one head 14.0, two 15.0).
+constexpr int64_t kMany = 1 << 21;
+
 template <typename T, int N, bool Interleaved>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
-  constexpr int kHeads = 4;
   const int units = a.rot / 2 / N + (a.x == a.y ? 0 : (a.d - a.rot) / 8);
   const int64_t runs = (int64_t)a.B * a.M * units;
   const unsigned blocks = (unsigned)((runs + kThreads - 1) / kThreads);
-  // heads of a thread: as many as leave the device kOccupy threads, so that few
-  // tokens spread over it and many form each angle once
-  const int64_t kOccupy = (int64_t)device_cu_count() * 1024;
-  const int64_t want = runs * a.H / kOccupy;
-  if (want < kHeads) {
-    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, 1>), dim3(blocks, a.H), dim3(kThreads), 0, stream, a, units, 1);
-  } else {
-    const int per = (int)(want < a.H ? want : a.H);
-    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, kHeads>), dim3(blocks, (a.H + per - 1) / per), dim3(kThreads), 0,
-                       stream, a, units, per);
-  }
+  if (runs * a.H < kMany)
+    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, false>), dim3(blocks, a.H), dim3(kThreads), 0, stream, a, units, 1);
+  else
+    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, true>), dim3(blocks, (a.H + 1) / 2), dim3(kThreads), 0, stream, a,
+                       units, 2);
   return hipGetLastError();
 }
 
