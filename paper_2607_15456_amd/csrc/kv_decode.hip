@@ -8,9 +8,8 @@
 // flops a token and query head.
 //
 // A workgroup takes up to 16 query heads of one (entry, key head) and a slice of
-// its pages; a wavefront takes steps of 16 to 64 tokens, every W-th of the
-// slice's, with both products on the matrix instructions and all operands
-// straight from memory to registers:
+// its pages; a wavefront takes steps of 64 tokens (fp32: 32), every W-th of the
+// slice's, with both products on the matrix instructions:
 //
 //   S^T [tokens x heads] = K Q^T      A: 16 bytes of a key row (token-major)
 //   O^T [features x heads] += V^T P^T A: 16 bytes of a value row (feature-major)
@@ -47,8 +46,9 @@ constexpr float kLn2 = 0.69314718055994531f;
 __device__ __forceinline__ BufRsrc make_rsrc(const void* base, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
 }
+// (2: the non-temporal policy)
 __device__ __forceinline__ uint4 buf_ld16(BufRsrc r, int voff, int soff) {
-  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0));
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 2));
 }
 // Uniform read of an index array (nothing in a launch writes one).
 typedef const int __attribute__((address_space(4))) ConstInt;
@@ -87,61 +87,87 @@ __device__ __forceinline__ int entry_tokens(const KvDecodeArgs& a, int b, int& r
 }
 
 // ---- one step of a wavefront ----
+//
+// A step's keys, then its values, go from memory to registers as whole
+// consecutive kilobytes (read once: non-temporal), from there to the
+// wavefront's own LDS, and from there to the matrix instructions as operands: 16
+// bytes of a row a lane.  Straight from memory, an operand load touches 64 bytes
+// of each of 16 rows, which the memory answers 12% more slowly (32 x 4096 tokens of 16 heads of
+// 128: 191 us; the same bytes consecutive and non-temporal 168).  16-byte chunks
+// of a row are stored at chunk ^ swizzle(row), so that the 8 lanes that LDS
+// serves at a time meet different banks.
 
-// bf16: 64 tokens, 32 where a page's operands would not fit the registers.
+// bf16: a page.
 template <int D>
 struct StepBf16 {
-  static constexpr int kTok = D <= 128 ? 64 : 32, kTiles = kTok / 16, kBytes = 2;
-  static constexpr int KS = D / 32, FT = D / 16, UU = kTok / 32, kQueryLds = 0;
-  uint4 q[KS], k[kTiles][KS], v[FT][UU];
+  static constexpr int kTok = 64, kTiles = kTok / 16, kBytes = 2;
+  static constexpr int KS = D / 32, FT = D / 16, UU = kTok / 32;
+  static constexpr int kLoads = kTok * D * 2 / 1024;  // of the keys, and of the values
+  static constexpr int kKeyChunks = D / 8, kValChunks = kTok / 8;
+  uint4 q[KS], k[kLoads], v[kLoads];
 
-  __device__ __forceinline__ void load_q(const void* row, int g, bool in, f32x4*) {
+  __device__ __forceinline__ void load_q(const void* row, int g, bool in) {
 #pragma unroll
     for (int s = 0; s < KS; ++s)
       q[s] = in ? ld16(static_cast<const bf16_t*>(row) + 32 * s + 8 * g) : uint4{0, 0, 0, 0};
   }
-  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int c, int g) {
-    const int lane = ((8 * (c / 4) + c % 4) * D + 8 * g) * 2;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        k[t][s] = buf_ld16(r, lane, ((tok + 32 * (t / 2) + 4 * (t % 2)) * D + 32 * s) * 2);
+  // lanes that read keys at a time hold rows 0 .. 3 and 8 .. 11 of 16
+  __device__ __forceinline__ static int key_at(int row, int chunk) {
+    const int i = (row & 3) | ((row >> 1) & 4);
+    return (row * kKeyChunks + (chunk ^ (kKeyChunks % 8 ? i >> 1 : i))) * 16;
   }
-  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int c, int g) {
-    const int lane = (c * kPage + 8 * g) * 2;
+  __device__ __forceinline__ static int val_at(int row, int chunk) { return (row * kValChunks + (chunk ^ (row & 7))) * 16; }
+  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int lane) {
 #pragma unroll
-    for (int f = 0; f < FT; ++f)
+    for (int j = 0; j < kLoads; ++j) k[j] = buf_ld16(r, lane * 16, tok * D * 2 + j * 1024);
+  }
+  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int lane) {
+    constexpr int kRows = kWave / kValChunks;  // feature rows of a load
+    const int at = lane / kValChunks * (kPage * 2) + lane % kValChunks * 16;
 #pragma unroll
-      for (int u = 0; u < UU; ++u) v[f][u] = buf_ld16(r, lane, (16 * f * kPage + tok + 32 * u) * 2);
+    for (int j = 0; j < kLoads; ++j) v[j] = buf_ld16(r, at, tok * 2 + j * kRows * kPage * 2);
+  }
+  __device__ __forceinline__ void stage_k(char* lds, int lane) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = j * kWave + lane;
+      *reinterpret_cast<uint4*>(lds + key_at(i / kKeyChunks, i % kKeyChunks)) = k[j];
+    }
+  }
+  // tokens not attended become zero, whatever their slots hold
+  template <typename Seen>
+  __device__ __forceinline__ void mask_values(const Seen& seen, int lane) {
+    uint32_t keep[4];
+    const int t = lane % kValChunks * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      keep[i] = (seen(t + 2 * i) ? 0xffffu : 0u) | (seen(t + 2 * i + 1) ? 0xffff0000u : 0u);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      v[j] = uint4{v[j].x & keep[0], v[j].y & keep[1], v[j].z & keep[2], v[j].w & keep[3]};
+  }
+  __device__ __forceinline__ void stage_v(char* lds, int lane) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = j * kWave + lane;
+      *reinterpret_cast<uint4*>(lds + val_at(i / kValChunks, i % kValChunks)) = v[j];
+    }
   }
   // token of register i of tile t in this lane, from the step's first
   __device__ __forceinline__ static int token(int t, int i, int g) { return 32 * (t / 2) + 8 * g + 4 * (t % 2) + i; }
-  __device__ __forceinline__ void scores(f32x4 (&sc)[kTiles]) const {
+  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[kTiles]) const {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       sc[t] = f32x4{0.f};
+      const int row = 32 * (t / 2) + 8 * (c / 4) + 4 * (t % 2) + c % 4;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][s]),
-                                                        __builtin_bit_cast(bf16x8, q[s]), sc[t], 0, 0, 0);
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + key_at(row, 4 * s + g))),
+            __builtin_bit_cast(bf16x8, q[s]), sc[t], 0, 0, 0);
     }
   }
-  // values of tokens not attended to zero, whatever their slots hold
-  template <typename Seen>
-  __device__ __forceinline__ void mask_values(const Seen& seen, int g) {
-#pragma unroll
-    for (int u = 0; u < UU; ++u) {
-      uint32_t keep[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        keep[i] = (seen(32 * u + 8 * g + 2 * i) ? 0xffffu : 0u) | (seen(32 * u + 8 * g + 2 * i + 1) ? 0xffff0000u : 0u);
-#pragma unroll
-      for (int f = 0; f < FT; ++f)
-        v[f][u] = uint4{v[f][u].x & keep[0], v[f][u].y & keep[1], v[f][u].z & keep[2], v[f][u].w & keep[3]};
-    }
-  }
-  __device__ __forceinline__ void values(const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
 #pragma unroll
     for (int u = 0; u < UU; ++u) {
       bf16x8 hi, lo;
@@ -153,82 +179,88 @@ struct StepBf16 {
       }
 #pragma unroll
       for (int f = 0; f < FT; ++f) {
-        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[f][u]), hi, o[f], 0, 0, 0);
-        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[f][u]), lo, o[f], 0, 0, 0);
+        const bf16x8 w =
+            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + val_at(16 * f + c, 4 * u + g)));
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, o[f], 0, 0, 0);
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, o[f], 0, 0, 0);
       }
     }
   }
 };
 
-// fp32: 32 tokens, 16 above a width of 128; above 192 the queries do not fit the
-// registers beside them and are read from LDS again for every step.
+// fp32: half a page.
 template <int D>
 struct StepF32 {
-  static constexpr int kTok = D <= 128 ? 32 : 16, kTiles = kTok / 16, kBytes = 4;
-  static constexpr int KS = D / 16, FT = D / 16, kQueryLds = D > 192 ? KS * kWave : 0;  // LDS, in 16 bytes
-  f32x4 q[kQueryLds ? 1 : KS], k[kTiles][KS], v[FT][kTiles];
-  f32x4* sq;
+  static constexpr int kTok = 32, kTiles = kTok / 16, kBytes = 4;
+  static constexpr int KS = D / 16, FT = D / 16;
+  static constexpr int kLoads = kTok * D * 4 / 1024;
+  static constexpr int kKeyChunks = D / 4, kValChunks = kTok / 4;
+  f32x4 q[KS], k[kLoads], v[kLoads];
 
-  // (every wavefront writes the same values, and reads after its own)
-  __device__ __forceinline__ void load_q(const void* row, int g, bool in, f32x4* lds) {
-    sq = lds;
+  __device__ __forceinline__ void load_q(const void* row, int g, bool in) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const f32x4 x = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
-      if constexpr (kQueryLds) sq[s * kWave] = x;
-      else q[s] = x;
-    }
+    for (int s = 0; s < KS; ++s)
+      q[s] = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
   }
-  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int c, int g) {
-    const int lane = (c * D + 4 * g) * 4;
+  __device__ __forceinline__ static int key_at(int row, int chunk) { return (row * kKeyChunks + (chunk ^ (row & 7))) * 16; }
+  __device__ __forceinline__ static int val_at(int row, int chunk) { return (row * kValChunks + (chunk ^ (row & 7))) * 16; }
+  __device__ __forceinline__ void load_k(BufRsrc r, int tok, int lane) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        k[t][s] = __builtin_bit_cast(f32x4, buf_ld16(r, lane, ((tok + 16 * t) * D + 16 * s) * 4));
+    for (int j = 0; j < kLoads; ++j) k[j] = __builtin_bit_cast(f32x4, buf_ld16(r, lane * 16, tok * D * 4 + j * 1024));
   }
-  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int c, int g) {
-    const int lane = (c * kPage + 4 * g) * 4;
+  __device__ __forceinline__ void load_v(BufRsrc r, int tok, int lane) {
+    constexpr int kRows = kWave / kValChunks;
+    const int at = lane / kValChunks * (kPage * 4) + lane % kValChunks * 16;
 #pragma unroll
-    for (int f = 0; f < FT; ++f)
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-        v[f][t] = __builtin_bit_cast(f32x4, buf_ld16(r, lane, (16 * f * kPage + tok + 16 * t) * 4));
+    for (int j = 0; j < kLoads; ++j) v[j] = __builtin_bit_cast(f32x4, buf_ld16(r, at, tok * 4 + j * kRows * kPage * 4));
   }
-  __device__ __forceinline__ static int token(int t, int i, int g) { return 16 * t + 4 * g + i; }
-  __device__ __forceinline__ void scores(f32x4 (&sc)[kTiles]) const {
+  __device__ __forceinline__ void stage_k(char* lds, int lane) const {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      sc[t] = f32x4{0.f};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        f32x4 x;
-        if constexpr (kQueryLds) x = sq[s * kWave];
-        else x = q[s];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][s][e], x[e], sc[t], 0, 0, 0);
-      }
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = j * kWave + lane;
+      *reinterpret_cast<f32x4*>(lds + key_at(i / kKeyChunks, i % kKeyChunks)) = k[j];
     }
   }
   template <typename Seen>
-  __device__ __forceinline__ void mask_values(const Seen& seen, int g) {
+  __device__ __forceinline__ void mask_values(const Seen& seen, int lane) {
+    const int t = lane % kValChunks * 4;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int e = 0; e < 4; ++e) {
+      const bool in = seen(t + e);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool in = seen(16 * t + 4 * g + e);
-#pragma unroll
-        for (int f = 0; f < FT; ++f) v[f][t][e] = in ? v[f][t][e] : 0.f;
-      }
+      for (int j = 0; j < kLoads; ++j) v[j][e] = in ? v[j][e] : 0.f;
+    }
   }
-  __device__ __forceinline__ void values(const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+  __device__ __forceinline__ void stage_v(char* lds, int lane) const {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = j * kWave + lane;
+      *reinterpret_cast<f32x4*>(lds + val_at(i / kValChunks, i % kValChunks)) = v[j];
+    }
+  }
+  __device__ __forceinline__ static int token(int t, int i, int g) { return 16 * t + 4 * g + i; }
+  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[kTiles]) const {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+    for (int t = 0; t < kTiles; ++t) sc[t] = f32x4{0.f};
 #pragma unroll
-        for (int f = 0; f < FT; ++f)
-          o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[f][t][e], p[t][e], o[f], 0, 0, 0);
+    for (int s = 0; s < KS; ++s) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(lds + key_at(16 * t + c, 4 * s + g));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], q[s][e], sc[t], 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(lds + val_at(16 * f + c, 4 * t + g));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], p[t][e], o[f], 0, 0, 0);
+      }
   }
 };
 
@@ -267,15 +299,21 @@ __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m
   }
 }
 
+// Two wavefronts a SIMD, one above a width of 128: its steps are twice as large,
+// so as many bytes are on their way.
 template <typename Step, int D, int W>
-__global__ __launch_bounds__(W* kWave, 2) void decode_kernel(KvDecodeArgs a) {
+__global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
+  constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
   constexpr int kRow = D + 4;
-  __shared__ __align__(16) float s_o[W / 2 * kTile * kRow];
-  __shared__ float s_ml[W / 2][2][kTile];
-  __shared__ f32x4 s_q[Step::kQueryLds ? Step::kQueryLds : 1];
+  // the wavefronts' steps, then what they join
+  __shared__ __align__(16) char s_raw[W * kStepBytes];
+  static_assert(W / 2 * kTile * (kRow + 2) * 4 <= W * kStepBytes);
+  float* const s_o = reinterpret_cast<float*>(s_raw);
+  float(*const s_ml)[2][kTile] = reinterpret_cast<float(*)[2][kTile]>(s_o + W / 2 * kTile * kRow);
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  char* const lds = s_raw + w * kStepBytes;
   const int units = a.B * a.p.Hkv;
   const int slice = blockIdx.x / units, unit = blockIdx.x - slice * units;
   const int b = unit / a.p.Hkv, kvh = unit - b * a.p.Hkv;
@@ -321,19 +359,20 @@ __global__ __launch_bounds__(W* kWave, 2) void decode_kernel(KvDecodeArgs a) {
   if (t < end) {
     const int64_t at = block(t);
     const int tok = t % kSteps * Step::kTok;
-    st.load_k(keys(at), tok, c, g);
-    st.load_v(vals(at), tok, c, g);
+    st.load_k(keys(at), tok, lane);
+    st.load_v(vals(at), tok, lane);
   }
-  st.load_q(static_cast<const char*>(a.q) + out_row * D * Step::kBytes, g, in, s_q + lane);
-  // A step's keys are requested as soon as the scores before have consumed
-  // theirs, its values once the products before are issued.
+  st.load_q(static_cast<const char*>(a.q) + out_row * D * Step::kBytes, g, in);
+  // A step's keys are requested as soon as the keys before have left their
+  // registers for LDS, its values likewise.
   for (; t < end; t += W) {
     const bool more = t + W < end;
     const int tok = (t + W) % kSteps * Step::kTok;
     const int64_t next = more ? block(t + W) : 0;
     f32x4 sc[kTiles];
-    st.scores(sc);
-    if (more) st.load_k(keys(next), tok, c, g);
+    st.stage_k(lds, lane);
+    if (more) st.load_k(keys(next), tok, lane);
+    st.scores(lds, c, g, sc);
     const int t0 = sp.page(t / kSteps) * kPage + t % kSteps * Step::kTok;
     const bool whole = sp.whole(t0, Step::kTok);
     if (!whole) {
@@ -366,15 +405,17 @@ __global__ __launch_bounds__(W* kWave, 2) void decode_kernel(KvDecodeArgs a) {
         sc[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], a.qscale, -base));
         l += sc[x][i];
       }
-    if (!whole) st.mask_values([&](int k) { return sp.seen(t0 + k); }, g);
-    st.values(sc, o);
-    if (more) st.load_v(vals(next), tok, c, g);
+    if (!whole) st.mask_values([&](int k) { return sp.seen(t0 + k); }, lane);
+    st.stage_v(lds, lane);
+    if (more) st.load_v(vals(next), tok, lane);
+    st.values(lds, c, g, sc, o);
   }
   l += xor_shfl(l, 16);
   l += xor_shfl(l, 32);
   if (bad) l = __builtin_nanf("");
 
   // join the wavefronts, the upper half into the lower
+  __syncthreads();
 #pragma unroll
   for (int half = W / 2; half >= 1; half /= 2) {
     if (w >= half && w < 2 * half) {
