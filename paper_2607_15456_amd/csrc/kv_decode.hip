@@ -40,6 +40,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
 constexpr int kTile = 16;     // query heads of a workgroup
+constexpr int kWaves = 4;
 constexpr float kLazy = 8.f;  // log2 by which a step may exceed the running maximum
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -447,50 +448,73 @@ __global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDe
   if (a.lse && g == 0) a.lse[out_row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins the slices of one (entry, query head).  A thread holds four features of
-// every R-th slice; R is what 256 threads allow.
-constexpr int kJoinThreads = 256;
+// Joins the slices of one (entry, query head): their weights 2^(m_s - m) first, a
+// slice a thread, then four features a thread of every R-th slice.
+constexpr int kJoinThreads = 256, kMaxSlices = 512;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
+  constexpr int kJoinWaves = kJoinThreads / kWave;
   __shared__ __align__(16) float s_o[kJoinThreads * 4];
-  __shared__ float s_l[kJoinThreads];
+  __shared__ float s_w[kMaxSlices], s_red[2][kJoinWaves];
   const int64_t row_out = blockIdx.x;
-  const int b = blockIdx.x / a.H, tid = threadIdx.x, lanes = a.p.d / 4;
+  const int b = blockIdx.x / a.H, tid = threadIdx.x, d = a.p.d, lanes = d / 4;
   int row;
   const int n = entry_tokens(a, b, row);
   const Span sp(max(n, 0), a.sink, a.window);
   const int slices = (sp.pages + a.per - 1) / a.per;
+  float ms[kMaxSlices / kJoinThreads], ls[kMaxSlices / kJoinThreads], m = neg_inf(), l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxSlices / kJoinThreads; ++i) {
+    const int s = tid + i * kJoinThreads;
+    ms[i] = neg_inf();
+    ls[i] = 0.f;
+    if (s < slices) {
+      ms[i] = partial(a, row_out, s)[d];
+      ls[i] = partial(a, row_out, s)[d + 1];
+    }
+    m = fmaxf(m, ms[i]);
+  }
+#pragma unroll
+  for (int x = kWave / 2; x; x >>= 1) m = fmaxf(m, xor_shfl(m, x));
+  if (tid % kWave == 0) s_red[0][tid / kWave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kJoinWaves; ++x) m = fmaxf(m, s_red[0][x]);
+  const float base = m == neg_inf() ? 0.f : m;
+#pragma unroll
+  for (int i = 0; i < kMaxSlices / kJoinThreads; ++i) {
+    const float w = __builtin_amdgcn_exp2f(ms[i] - base);
+    s_w[tid + i * kJoinThreads] = w;
+    l += ls[i] * w;
+  }
+#pragma unroll
+  for (int x = kWave / 2; x; x >>= 1) l += xor_shfl(l, x);
+  if (tid % kWave == 0) s_red[1][tid / kWave] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int x = 0; x < kJoinWaves; ++x) l += s_red[1][x];
+
   const int R = kJoinThreads / lanes, r = tid / lanes, f = tid % lanes;
-  float m = neg_inf(), l = 0.f;
   f32x4 o = f32x4{0.f};
   if (r < R) {
-    for (int s = 0; s < slices; ++s) m = fmaxf(m, partial(a, row_out, s)[a.p.d]);
-    const float base = m == neg_inf() ? 0.f : m;
-    for (int s = r; s < slices; s += R) {
-      const float* part = partial(a, row_out, s);
-      const float x = __builtin_amdgcn_exp2f(part[a.p.d] - base);
-      l += part[a.p.d + 1] * x;
-      o += *reinterpret_cast<const f32x4*>(part + 4 * f) * x;
-    }
+    const float* part = partial(a, row_out, 0) + 4 * f;
+#pragma unroll 4
+    for (int s = r; s < slices; s += R) o += *reinterpret_cast<const f32x4*>(part + (int64_t)s * (d + 4)) * s_w[s];
   }
   *reinterpret_cast<f32x4*>(&s_o[4 * tid]) = o;
-  s_l[tid] = l;
   __syncthreads();
   if (r == 0) {
-    for (int x = 1; x < R; ++x) {
-      o += *reinterpret_cast<const f32x4*>(&s_o[4 * (tid + x * lanes)]);
-      l += s_l[tid + x * lanes];
-    }
+    for (int x = 1; x < R; ++x) o += *reinterpret_cast<const f32x4*>(&s_o[4 * (tid + x * lanes)]);
     const float none = n < 0 ? __builtin_nanf("") : 0.f;
     const bool empty = n <= 0;
     store4(a, row_out, 4 * f, empty ? f32x4{none, none, none, none} : o / l);
-    if (a.lse && f == 0)
-      a.lse[row_out] = n < 0 ? none : empty ? neg_inf() : ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+    if (a.lse && f == 0) a.lse[row_out] = n < 0 ? none : empty ? neg_inf() : (base + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
 
 template <int D>
 hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
-  constexpr int W = 4;
+  constexpr int W = kWaves;
   const dim3 grid(a.B * a.p.Hkv * a.slices, (a.H / a.p.Hkv + kTile - 1) / kTile);
   if (a.p.dtype == LLA_BF16) hipLaunchKernelGGL((decode_kernel<StepBf16<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
   else hipLaunchKernelGGL((decode_kernel<StepF32<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
@@ -502,20 +526,31 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Slices of a context.  Long ones: as many as give each compute unit two
+// workgroups, if a slice keeps kLong pages; otherwise one workgroup a unit, since
+// a join costs a launch (4 us) and has to save more.  Measured (width 128, bf16
+// but for the first; unsplit / split, us):
+//   1 x 512 tokens, fp32, 16 key heads 20.8 / 10.6 (a page a slice), bf16 11.7 / 8.6
+//   1 x 32,768, 2 key heads            299 / 15.6 (4 pages; 2 pages 17.6, one 25)
+//   4 x 4096, 16 key heads             49.6 / 29.6 (16 pages; 8 pages 29.1)
+//   24 of 17 pages, 8 key heads of 64  16.2 / 18.6
+//   20 x 1024 .. 4096, 16 key heads    89 / 80;  12 x 2250 .. 9000, 8 key heads 100 / 59
+//   40 x 4096, 16 key heads (640 workgroups) 209 / 208 .. 214
 size_t kv_decode_shape(KvDecodeArgs& a) {
+  constexpr int kLong = 16;
   const int all = (a.n_ctx + kPage - 1) / kPage;
   // most pages that an entry attends
   const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
   const int pages = a.window ? (int)std::min<int64_t>(all, budget) : all;
   const int64_t units = (int64_t)a.B * a.p.Hkv * ((a.H / a.p.Hkv + kTile - 1) / kTile);
-  const int64_t want = std::max<int64_t>(1, (2 * device_cu_count() + units - 1) / units);
-  a.per = (int)std::max<int64_t>(8, (pages + want - 1) / want);
+  const int64_t cus = device_cu_count();
+  int64_t want = (2 * cus + units - 1) / units;
+  if (pages < want * kLong) want = std::max<int64_t>(1, cus / units);
+  if (pages <= (a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2)) want = 1;  // a step a wavefront
+  a.per = (int)((pages + want - 1) / want);
+  a.per = std::max(a.per, (pages + kMaxSlices - 1) / kMaxSlices);
   a.slices = (pages + a.per - 1) / a.per;
-  if (a.slices == 1) {
-    a.per = pages;
-    return 0;
-  }
-  return (size_t)a.B * a.H * a.slices * (a.p.d + 4) * sizeof(float);
+  return a.slices == 1 ? 0 : (size_t)a.B * a.H * a.slices * (a.p.d + 4) * sizeof(float);
 }
 
 hipError_t launch_kv_decode(const KvDecodeArgs& a, hipStream_t stream) {
