@@ -7,7 +7,7 @@
 // bytes of the attended pages bound it: 2 d elements a token and key head, 4 d
 // flops a token and query head.
 //
-// A workgroup takes up to 16 query heads of one (entry, key head) and a slice of
+// A workgroup takes up to 32 query heads of one (entry, key head) and a slice of
 // its pages; a wavefront takes steps of 64 tokens (fp32: 32), every W-th of the
 // slice's, with both products on the matrix instructions:
 //
@@ -39,7 +39,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
-constexpr int kTile = 16;     // query heads of a workgroup
+constexpr int kTile = 16;     // columns of a product: query heads
 constexpr int kWaves = 4;
 constexpr float kLazy = 8.f;  // log2 by which a step may exceed the running maximum
 constexpr float kLn2 = 0.69314718055994531f;
@@ -99,18 +99,18 @@ __device__ __forceinline__ int entry_tokens(const KvDecodeArgs& a, int b, int& r
 // serves at a time meet different banks.
 
 // bf16: a page.
-template <int D>
+template <int D, int NT>
 struct StepBf16 {
   static constexpr int kTok = 64, kTiles = kTok / 16, kBytes = 2;
   static constexpr int KS = D / 32, FT = D / 16, UU = kTok / 32;
   static constexpr int kLoads = kTok * D * 2 / 1024;  // of the keys, and of the values
   static constexpr int kKeyChunks = D / 8, kValChunks = kTok / 8;
-  uint4 q[KS], k[kLoads], v[kLoads];
+  uint4 q[NT][KS], k[kLoads], v[kLoads];
 
-  __device__ __forceinline__ void load_q(const void* row, int g, bool in) {
+  __device__ __forceinline__ void load_q(int n, const void* row, int g, bool in) {
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      q[s] = in ? ld16(static_cast<const bf16_t*>(row) + 32 * s + 8 * g) : uint4{0, 0, 0, 0};
+      q[n][s] = in ? ld16(static_cast<const bf16_t*>(row) + 32 * s + 8 * g) : uint4{0, 0, 0, 0};
   }
   // lanes that read keys at a time hold rows 0 .. 3 and 8 .. 11 of 16
   __device__ __forceinline__ static int key_at(int row, int chunk) {
@@ -156,52 +156,62 @@ struct StepBf16 {
   }
   // token of register i of tile t in this lane, from the step's first
   __device__ __forceinline__ static int token(int t, int i, int g) { return 32 * (t / 2) + 8 * g + 4 * (t % 2) + i; }
-  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[kTiles]) const {
+  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[NT][kTiles]) const {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      sc[t] = f32x4{0.f};
+#pragma unroll
+      for (int n = 0; n < NT; ++n) sc[n][t] = f32x4{0.f};
       const int row = 32 * (t / 2) + 8 * (c / 4) + 4 * (t % 2) + c % 4;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + key_at(row, 4 * s + g))),
-            __builtin_bit_cast(bf16x8, q[s]), sc[t], 0, 0, 0);
+      for (int s = 0; s < KS; ++s) {
+        const bf16x8 x =
+            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + key_at(row, 4 * s + g)));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, q[n][s]), sc[n][t], 0, 0, 0);
+      }
     }
   }
-  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[NT][kTiles],
+                                         f32x4 (&o)[NT][FT]) const {
 #pragma unroll
     for (int u = 0; u < UU; ++u) {
-      bf16x8 hi, lo;
+      bf16x8 hi[NT], lo[NT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = p[2 * u + e / 4][e % 4];
-        hi[e] = (__bf16)x;
-        lo[e] = (__bf16)(x - (float)hi[e]);
-      }
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = p[n][2 * u + e / 4][e % 4];
+          hi[n][e] = (__bf16)x;
+          lo[n][e] = (__bf16)(x - (float)hi[n][e]);
+        }
 #pragma unroll
       for (int f = 0; f < FT; ++f) {
         const bf16x8 w =
             __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + val_at(16 * f + c, 4 * u + g)));
-        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, o[f], 0, 0, 0);
-        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, o[f], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          o[n][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi[n], o[n][f], 0, 0, 0);
+          o[n][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo[n], o[n][f], 0, 0, 0);
+        }
       }
     }
   }
 };
 
 // fp32: half a page.
-template <int D>
+template <int D, int NT>
 struct StepF32 {
   static constexpr int kTok = 32, kTiles = kTok / 16, kBytes = 4;
   static constexpr int KS = D / 16, FT = D / 16;
   static constexpr int kLoads = kTok * D * 4 / 1024;
   static constexpr int kKeyChunks = D / 4, kValChunks = kTok / 4;
-  f32x4 q[KS], k[kLoads], v[kLoads];
+  f32x4 q[NT][KS], k[kLoads], v[kLoads];
 
-  __device__ __forceinline__ void load_q(const void* row, int g, bool in) {
+  __device__ __forceinline__ void load_q(int n, const void* row, int g, bool in) {
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      q[s] = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
+      q[n][s] = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
   }
   __device__ __forceinline__ static int key_at(int row, int chunk) { return (row * kKeyChunks + (chunk ^ (row & 7))) * 16; }
   __device__ __forceinline__ static int val_at(int row, int chunk) { return (row * kValChunks + (chunk ^ (row & 7))) * 16; }
@@ -240,27 +250,35 @@ struct StepF32 {
     }
   }
   __device__ __forceinline__ static int token(int t, int i, int g) { return 16 * t + 4 * g + i; }
-  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[kTiles]) const {
+  __device__ __forceinline__ void scores(const char* lds, int c, int g, f32x4 (&sc)[NT][kTiles]) const {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) sc[t] = f32x4{0.f};
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
+      for (int t = 0; t < kTiles; ++t) sc[n][t] = f32x4{0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const f32x4 y = *reinterpret_cast<const f32x4*>(lds + key_at(16 * t + c, 4 * s + g));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], q[s][e], sc[t], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], q[n][s][e], sc[n][t], 0, 0, 0);
       }
-    }
   }
-  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[kTiles], f32x4 (&o)[FT]) const {
+  __device__ __forceinline__ void values(const char* lds, int c, int g, const f32x4 (&p)[NT][kTiles],
+                                         f32x4 (&o)[NT][FT]) const {
 #pragma unroll
     for (int f = 0; f < FT; ++f)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const f32x4 y = *reinterpret_cast<const f32x4*>(lds + val_at(16 * f + c, 4 * t + g));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], p[t][e], o[f], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            o[n][f] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], p[n][t][e], o[n][f], 0, 0, 0);
       }
   }
 };
@@ -300,18 +318,20 @@ __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m
   }
 }
 
-// Two wavefronts a SIMD, one above a width of 128: its steps are twice as large,
-// so as many bytes are on their way.
-template <typename Step, int D, int W>
-__global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
+// NT tiles of 16 query heads.  Two wavefronts a SIMD; one above a width of 128,
+// where steps are twice as large, so as many bytes are on their way, and with two
+// tiles, whose accumulators need the registers.
+template <template <int, int> class StepOf, int D, int NT, int W>
+__global__ __launch_bounds__(W* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
+  typedef StepOf<D, NT> Step;
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
-  constexpr int kRow = D + 4;
+  constexpr int kRow = D + 4, kCols = NT * kTile;
   // the wavefronts' steps, then what they join
   __shared__ __align__(16) char s_raw[W * kStepBytes];
-  static_assert(W / 2 * kTile * (kRow + 2) * 4 <= W * kStepBytes);
+  static_assert(W / 2 * kCols * (kRow + 2) * 4 <= W * kStepBytes);
   float* const s_o = reinterpret_cast<float*>(s_raw);
-  float(*const s_ml)[2][kTile] = reinterpret_cast<float(*)[2][kTile]>(s_o + W / 2 * kTile * kRow);
+  float(*const s_ml)[2][kCols] = reinterpret_cast<float(*)[2][kCols]>(s_o + W / 2 * kCols * kRow);
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   char* const lds = s_raw + w * kStepBytes;
@@ -319,20 +339,23 @@ __global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDe
   const int slice = blockIdx.x / units, unit = blockIdx.x - slice * units;
   const int b = unit / a.p.Hkv, kvh = unit - b * a.p.Hkv;
   const int group = a.H / a.p.Hkv;
-  const int h = blockIdx.y * kTile + c;  // of the group
-  const bool in = h < group;
-  const int64_t out_row = (int64_t)b * a.H + kvh * group + h;
+  const int h0 = blockIdx.y * kCols + c;  // tile x's column: head h0 + 16 x of the group
+  const int64_t out_row = (int64_t)b * a.H + kvh * group + h0;
 
   int row;
   const int n = entry_tokens(a, b, row);
   const Span sp(max(n, 0), a.sink, a.window);
   const int pb = slice * a.per, pe = min(sp.pages, pb + a.per);
   if (n <= 0 || pb >= pe) {
-    if (n <= 0 && slice == 0 && w == 0 && in && a.slices == 1) {
-      const float x = n < 0 ? __builtin_nanf("") : 0.f;
+    if (n <= 0 && slice == 0 && w == 0 && a.slices == 1) {
+      const float none = n < 0 ? __builtin_nanf("") : 0.f;
 #pragma unroll
-      for (int f = 0; f < FT; ++f) store4(a, out_row, 16 * f + 4 * g, f32x4{x, x, x, x});
-      if (a.lse && g == 0) a.lse[out_row] = n < 0 ? x : neg_inf();
+      for (int x = 0; x < NT; ++x) {
+        if (h0 + x * kTile >= group) continue;
+#pragma unroll
+        for (int f = 0; f < FT; ++f) store4(a, out_row + x * kTile, 16 * f + 4 * g, f32x4{none, none, none, none});
+        if (a.lse && g == 0) a.lse[out_row + x * kTile] = n < 0 ? none : neg_inf();
+      }
     }
     return;
   }
@@ -341,7 +364,7 @@ __global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDe
   constexpr int kHeadBytes = kPage * D * Step::kBytes;
   const int32_t* table = a.p.table + (int64_t)row * a.p.max_pages;
   bool bad = false;
-  // step t of the slice's: its page's keys and values, and its first token there
+  // step t of the slice's: where its page's keys and values are
   auto block = [&](int t) -> int64_t {
     int page = uniform(table, sp.page(t / kSteps));
     bad |= page < 0 || page >= a.p.n_pages;
@@ -353,24 +376,31 @@ __global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDe
 
   int t = pb * kSteps + w;
   const int end = pe * kSteps;
-  float m = neg_inf(), l = 0.f;
-  f32x4 o[FT];
+  float m[NT], l[NT];
+  f32x4 o[NT][FT];
 #pragma unroll
-  for (int f = 0; f < FT; ++f) o[f] = f32x4{0.f};
+  for (int x = 0; x < NT; ++x) {
+    m[x] = neg_inf();
+    l[x] = 0.f;
+#pragma unroll
+    for (int f = 0; f < FT; ++f) o[x][f] = f32x4{0.f};
+  }
   if (t < end) {
     const int64_t at = block(t);
     const int tok = t % kSteps * Step::kTok;
     st.load_k(keys(at), tok, lane);
     st.load_v(vals(at), tok, lane);
   }
-  st.load_q(static_cast<const char*>(a.q) + out_row * D * Step::kBytes, g, in);
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+    st.load_q(x, static_cast<const char*>(a.q) + (out_row + x * kTile) * D * Step::kBytes, g, h0 + x * kTile < group);
   // A step's keys are requested as soon as the keys before have left their
   // registers for LDS, its values likewise.
   for (; t < end; t += W) {
     const bool more = t + W < end;
     const int tok = (t + W) % kSteps * Step::kTok;
     const int64_t next = more ? block(t + W) : 0;
-    f32x4 sc[kTiles];
+    f32x4 sc[NT][kTiles];
     st.stage_k(lds, lane);
     if (more) st.load_k(keys(next), tok, lane);
     st.scores(lds, c, g, sc);
@@ -378,74 +408,98 @@ __global__ __launch_bounds__(W* kWave, D <= 128 ? 2 : 1) void decode_kernel(KvDe
     const bool whole = sp.whole(t0, Step::kTok);
     if (!whole) {
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x)
+      for (int y = 0; y < kTiles; ++y)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!sp.seen(t0 + Step::token(x, i, g))) sc[x][i] = neg_inf();
+          if (!sp.seen(t0 + Step::token(y, i, g))) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) sc[x][y][i] = neg_inf();
+          }
     }
-    float pm = neg_inf();
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
+    for (int x = 0; x < NT; ++x) {
+      float pm = neg_inf();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pm = fmaxf(pm, sc[x][i]);
-    pm = fmaxf(pm, xor_shfl(pm, 16));
-    pm = fmaxf(pm, xor_shfl(pm, 32)) * a.qscale;
-    if (__any(pm > m + kLazy)) {
-      const float to = fmaxf(m, pm);
-      const float alpha = m == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(m - to);
-      l *= alpha;
+      for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-      for (int f = 0; f < FT; ++f) o[f] *= alpha;
-      m = to;
-    }
-    const float base = m == neg_inf() ? 0.f : m;
+        for (int i = 0; i < 4; ++i) pm = fmaxf(pm, sc[x][y][i]);
+      pm = fmaxf(pm, xor_shfl(pm, 16));
+      pm = fmaxf(pm, xor_shfl(pm, 32)) * a.qscale;
+      if (__any(pm > m[x] + kLazy)) {
+        const float to = fmaxf(m[x], pm);
+        const float alpha = m[x] == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(m[x] - to);
+        l[x] *= alpha;
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], a.qscale, -base));
-        l += sc[x][i];
+        for (int f = 0; f < FT; ++f) o[x][f] *= alpha;
+        m[x] = to;
       }
+      const float base = m[x] == neg_inf() ? 0.f : m[x];
+#pragma unroll
+      for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[x][y][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][y][i], a.qscale, -base));
+          l[x] += sc[x][y][i];
+        }
+    }
     if (!whole) st.mask_values([&](int k) { return sp.seen(t0 + k); }, lane);
     st.stage_v(lds, lane);
     if (more) st.load_v(vals(next), tok, lane);
     st.values(lds, c, g, sc, o);
   }
-  l += xor_shfl(l, 16);
-  l += xor_shfl(l, 32);
-  if (bad) l = __builtin_nanf("");
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    l[x] += xor_shfl(l[x], 16);
+    l[x] += xor_shfl(l[x], 32);
+    if (bad) l[x] = __builtin_nanf("");
+  }
 
   // join the wavefronts, the upper half into the lower
   __syncthreads();
 #pragma unroll
   for (int half = W / 2; half >= 1; half /= 2) {
     if (w >= half && w < 2 * half) {
-      float* so = s_o + ((w - half) * kTile + c) * kRow + 4 * g;
 #pragma unroll
-      for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(so + 16 * f) = o[f];
-      if (g == 0) {
-        s_ml[w - half][0][c] = m;
-        s_ml[w - half][1][c] = l;
+      for (int x = 0; x < NT; ++x) {
+        const int col = x * kTile + c;
+        float* so = s_o + ((w - half) * kCols + col) * kRow + 4 * g;
+#pragma unroll
+        for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(so + 16 * f) = o[x][f];
+        if (g == 0) {
+          s_ml[w - half][0][col] = m[x];
+          s_ml[w - half][1][col] = l[x];
+        }
       }
     }
     __syncthreads();
-    if (w < half) join<FT>(m, l, o, s_ml[w][0][c], s_ml[w][1][c], s_o + (w * kTile + c) * kRow + 4 * g);
+    if (w < half) {
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const int col = x * kTile + c;
+        join<FT>(m[x], l[x], o[x], s_ml[w][0][col], s_ml[w][1][col], s_o + (w * kCols + col) * kRow + 4 * g);
+      }
+    }
     if (half > 1) __syncthreads();
   }
-  if (w != 0 || !in) return;
-  if (a.slices > 1) {
-    float* part = partial(a, out_row, slice);
+  if (w != 0) return;
 #pragma unroll
-    for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(part + 16 * f + 4 * g) = o[f];
-    if (g == 0) {
-      part[D] = m;
-      part[D + 1] = l;
+  for (int x = 0; x < NT; ++x) {
+    if (h0 + x * kTile >= group) continue;
+    const int64_t at = out_row + x * kTile;
+    if (a.slices > 1) {
+      float* part = partial(a, at, slice);
+#pragma unroll
+      for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(part + 16 * f + 4 * g) = o[x][f];
+      if (g == 0) {
+        part[D] = m[x];
+        part[D + 1] = l[x];
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < FT; ++f) store4(a, at, 16 * f + 4 * g, o[x][f] / l[x]);
+      if (a.lse && g == 0) a.lse[at] = ((m[x] == neg_inf() ? 0.f : m[x]) + __builtin_amdgcn_logf(l[x])) * kLn2;
     }
-    return;
   }
-#pragma unroll
-  for (int f = 0; f < FT; ++f) store4(a, out_row, 16 * f + 4 * g, o[f] / l);
-  if (a.lse && g == 0) a.lse[out_row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Joins the slices of one (entry, query head): their weights 2^(m_s - m) first, a
@@ -512,12 +566,34 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
   }
 }
 
+// Tiles of a workgroup: two from 17 query heads a group on, where their registers
+// suffice (16 x 4096 tokens, 8 key heads, bf16, one tile / two: 20 heads a group 94
+// / 64 us, 64 131 / 115).
+constexpr int kTwoTiles = 192;  // widest head of two tiles
+int query_tiles(int group, int d) { return group > kTile && d <= kTwoTiles ? 2 : 1; }
+int query_blocks(int group, int d) {
+  const int cols = kTile * query_tiles(group, d);
+  return (group + cols - 1) / cols;
+}
+
+template <template <int, int> class StepOf, int D>
+void launch_step(const KvDecodeArgs& a, hipStream_t stream) {
+  constexpr int W = kWaves;
+  const int group = a.H / a.p.Hkv;
+  const dim3 grid(a.B * a.p.Hkv * a.slices, query_blocks(group, D));
+  if constexpr (D <= kTwoTiles) {
+    if (query_tiles(group, D) == 2) {
+      hipLaunchKernelGGL((decode_kernel<StepOf, D, 2, W>), grid, dim3(W * kWave), 0, stream, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((decode_kernel<StepOf, D, 1, W>), grid, dim3(W * kWave), 0, stream, a);
+}
+
 template <int D>
 hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
-  constexpr int W = kWaves;
-  const dim3 grid(a.B * a.p.Hkv * a.slices, (a.H / a.p.Hkv + kTile - 1) / kTile);
-  if (a.p.dtype == LLA_BF16) hipLaunchKernelGGL((decode_kernel<StepBf16<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
-  else hipLaunchKernelGGL((decode_kernel<StepF32<D>, D, W>), grid, dim3(W * kWave), 0, stream, a);
+  if (a.p.dtype == LLA_BF16) launch_step<StepBf16, D>(a, stream);
+  else launch_step<StepF32, D>(a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.slices == 1) return e;
   hipLaunchKernelGGL(join_kernel, dim3(a.B * a.H), dim3(kJoinThreads), 0, stream, a);
@@ -542,7 +618,7 @@ size_t kv_decode_shape(KvDecodeArgs& a) {
   // most pages that an entry attends
   const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
   const int pages = a.window ? (int)std::min<int64_t>(all, budget) : all;
-  const int64_t units = (int64_t)a.B * a.p.Hkv * ((a.H / a.p.Hkv + kTile - 1) / kTile);
+  const int64_t units = (int64_t)a.B * a.p.Hkv * query_blocks(a.H / a.p.Hkv, a.p.d);
   const int64_t cus = device_cu_count();
   int64_t want = (2 * cus + units - 1) / units;
   if (pages < want * kLong) want = std::max<int64_t>(1, cus / units);
