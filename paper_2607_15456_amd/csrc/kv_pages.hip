@@ -4,7 +4,10 @@
 // The three table calls each run in one workgroup of up to 1024 sequences: the
 // rows' needs are a prefix sum, so the outcome is that of one row after another
 // in any run, with no lock and no order of atomics that shows.  They move a few
-// words a page; what they cost is a launch and a chain of dependent loads.
+// words a page; a launch and a chain of dependent reads bound them (16 rows of 36
+// pages dropped, forked and given room: 16.5 us for the three calls, 256 rows 71),
+// for thousands of pages the scattered words that one compute unit can ask for
+// (1000 rows of 32 pages 420).
 
 #include "kv_internal.h"
 #include "lla_device.h"
@@ -39,11 +42,22 @@ __device__ __forceinline__ int prefix(int v, int* s_wave, int& total) {
 }
 
 // A sequence number in range, named once in s_row[0 .. n).
-__device__ __forceinline__ bool sound(const int* s_row, int n, int i, int n_seqs) {
+__device__ __forceinline__ bool sound(const int* s_row, int i, int n_seqs) {
   const int r = s_row[i];
   bool ok = r >= 0 && r < n_seqs;
   for (int j = 0; j < i; ++j) ok &= s_row[j] != r;
   return ok;
+}
+
+// Row of entry e, where row i has the entries s_at[i] .. s_at[i + 1] - 1.
+__device__ __forceinline__ int row_of(const int* s_at, int n, int e) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (s_at[mid] <= e) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
 }
 
 __device__ __forceinline__ void report(const TableArgs& a, int status, int pairs, int pages, int left) {
@@ -54,12 +68,12 @@ __device__ __forceinline__ void report(const TableArgs& a, int status, int pairs
 }
 
 __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
-  __shared__ int s_row[kRows], s_open[kRows], s_wave[kThreads / kWave];
+  __shared__ int s_row[kRows], s_open[kRows], s_at[kRows], s_have[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
   const bool mine = i < a.n;
   s_row[i] = mine ? a.rows[i] : -1;
   __syncthreads();
-  bool ok = !mine || sound(s_row, a.n, i, a.n_seqs);
+  bool ok = !mine || sound(s_row, i, a.n_seqs);
   const int row = mine && ok ? s_row[i] : -1;
   const int add = row >= 0 ? a.more[i] : 0;
   const int len = row >= 0 ? a.length[row] : 0;
@@ -96,21 +110,24 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
     if (i == 0) report(a, LLA_PAGES_FULL, 0, 0, n_free);
     return;
   }
+  s_at[i] = at;
+  s_have[i] = have;
   if (row >= 0) {
-    for (int k = 0; k < need; ++k) {
-      const int page = a.free_pages[n_free - (at + k)];
-      table[have + k] = page;
-      if (page >= 0 && page < a.n_pages) a.refs[page] = 1;
-    }
     if (copy) {
       atomicSub(&a.refs[open], 1);
       a.pairs[2 * pair] = open;
-      a.pairs[2 * pair + 1] = table[have];
+      a.pairs[2 * pair + 1] = a.free_pages[n_free - at];  // the row's first
     }
     a.start[i] = len;
     a.length[row] = (int)end;
   }
   __syncthreads();
+  for (int e = i; e < total; e += kThreads) {
+    const int r = row_of(s_at, a.n, e);
+    const int page = a.free_pages[n_free - e];
+    a.table[(int64_t)s_row[r] * a.max_pages + s_have[r] + e - s_at[r]] = page;
+    if (page >= 0 && page < a.n_pages) a.refs[page] = 1;
+  }
   if (i == 0) {
     a.free_pages[0] = n_free - total;
     report(a, LLA_PAGES_OK, pairs, total, n_free - total);
@@ -118,42 +135,48 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
 }
 
 __global__ __launch_bounds__(kThreads) void fork_kernel(TableArgs a) {
-  __shared__ int s_row[kRows];
+  __shared__ int s_row[kRows], s_src[kRows], s_at[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
   const bool mine = i < a.n;
   s_row[i] = mine ? a.rows[i] : -1;
+  s_src[i] = mine ? a.more[i] : -1;
   __syncthreads();
   bool ok = true;
-  int src = -1;
+  int len = 0;
   if (mine) {
-    src = a.more[i];
-    ok = sound(s_row, a.n, i, a.n_seqs) && src >= 0 && src < a.n_seqs;
+    const int src = s_src[i];
+    ok = sound(s_row, i, a.n_seqs) && src >= 0 && src < a.n_seqs;
     for (int j = 0; j < a.n; ++j) ok &= s_row[j] != src;
-    if (ok) ok = a.length[s_row[i]] == 0 && a.length[src] >= 0 && a.length[src] <= (int64_t)a.max_pages * kPage;
+    if (ok) {
+      len = a.length[src];
+      ok = a.length[s_row[i]] == 0 && len >= 0 && len <= (int64_t)a.max_pages * kPage;
+    }
   }
   if (!__syncthreads_and(ok)) {
     if (i == 0) report(a, LLA_PAGES_BAD, 0, 0, a.free_pages[0]);
     return;
   }
-  if (mine) {
-    const int len = a.length[src];
-    const int32_t* from = a.table + (int64_t)src * a.max_pages;
-    int32_t* to = a.table + (int64_t)s_row[i] * a.max_pages;
-    for (int k = 0; k < pages_of(len); ++k) {
-      const int page = from[k];
-      to[k] = page;
-      if (page >= 0 && page < a.n_pages) atomicAdd(&a.refs[page], 1);
-    }
-    a.length[s_row[i]] = len;
+  int entries;
+  s_at[i] = prefix(pages_of(len), s_wave, entries);
+  if (mine) a.length[s_row[i]] = len;
+  __syncthreads();
+  for (int e = i; e < entries; e += kThreads) {
+    const int r = row_of(s_at, a.n, e), k = e - s_at[r];
+    const int page = a.table[(int64_t)s_src[r] * a.max_pages + k];
+    a.table[(int64_t)s_row[r] * a.max_pages + k] = page;
+    if (page >= 0 && page < a.n_pages) atomicAdd(&a.refs[page], 1);
   }
   if (i == 0) report(a, LLA_PAGES_OK, 0, 0, a.free_pages[0]);
 }
 
-// Freeing in three steps over all (row, page) entries: holders are counted
-// down; of the entries whose page has none left, the first names it (its rank,
-// lowered by 2^31, is the least that lands in refs); the named pages are laid
-// onto the stack, the last first.
+// Freeing goes over all (row, page) entries.  Holders are counted down; the
+// entry that takes the last one gives the page back, unless several entries of
+// the call name that page: then the first of them does, which is found by the
+// least rank, lowered by 2^31, that lands in refs.  Pages given back are laid onto
+// the stack, the last first.
 __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
+  constexpr int kHeld = 8;   // entries of a thread whose pages it keeps
+  constexpr int kNamed = (int)0x80000000;
   __shared__ int s_row[kRows], s_at[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
   const bool mine = i < a.n;
@@ -163,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
   int len = 0;
   const int n_free = a.free_pages[0];
   if (mine) {
-    ok = sound(s_row, a.n, i, a.n_seqs);
+    ok = sound(s_row, i, a.n_seqs);
     if (ok) len = a.length[s_row[i]];
     ok = ok && len >= 0 && len <= (int64_t)a.max_pages * kPage;
   }
@@ -173,66 +196,88 @@ __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
     return;
   }
   int entries;
-  s_at[i] = prefix(mine ? pages_of(len) : 0, s_wave, entries);
+  s_at[i] = prefix(pages_of(len), s_wave, entries);
   __syncthreads();
-  // entry e of all: its row (the last whose first entry is at or before e) and page
   auto entry = [&](int e) -> int32_t* {
-    int lo = 0, hi = a.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (s_at[mid] <= e) lo = mid;
-      else hi = mid - 1;
-    }
-    return a.table + (int64_t)s_row[lo] * a.max_pages + (e - s_at[lo]);
+    const int r = row_of(s_at, a.n, e);
+    return a.table + (int64_t)s_row[r] * a.max_pages + (e - s_at[r]);
   };
   auto page_at = [&](int e) {
-    const int page = *entry(e);
+    const int page = e < entries ? *entry(e) : -1;
     return page >= 0 && page < a.n_pages ? page : -1;
   };
-  for (int e = i; e < entries; e += kThreads) {
-    const int page = page_at(e);
-    if (page >= 0) atomicSub(&a.refs[page], 1);
-  }
-  wait_stores_in_l2();
-  __syncthreads();
-  constexpr int kNamed = (int)0x80000000;
-  for (int e = i; e < entries; e += kThreads) {
-    const int page = page_at(e);
-    if (page >= 0 && __hip_atomic_load(&a.refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0)
-      atomicMin(&a.refs[page], kNamed + e);
-  }
-  wait_stores_in_l2();
-  __syncthreads();
-  int back = 0;  // pages given back by earlier rounds
-  for (int e0 = 0; e0 < entries; e0 += kThreads) {
-    const int e = e0 + i;
-    const int page = e < entries ? page_at(e) : -1;
-    const bool named =
-        page >= 0 && __hip_atomic_load(&a.refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == kNamed + e;
-    int round;
-    const int at = back + prefix(named ? 1 : 0, s_wave, round);
-    (void)at;
-    back += round;
-  }
-  const int total = min(back, a.n_pages - n_free);
+  auto each = [&](auto f) {
+    for (int e = i; e < entries; e += kThreads) {
+      const int page = page_at(e);
+      if (page >= 0) f(e, page);
+    }
+  };
+  auto holders = [&](int page) {
+    return __hip_atomic_load(&a.refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  // lays down the pages of this round's threads that give one back (the last
+  // first, so the first is on top once all `total` are there)
   int done = 0;
-  for (int e0 = 0; e0 < entries; e0 += kThreads) {
-    const int e = e0 + i;
-    const int page = e < entries ? page_at(e) : -1;
-    const bool named =
-        page >= 0 && __hip_atomic_load(&a.refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == kNamed + e;
+  auto lay = [&](int page, bool back, int total) {
     int round;
-    const int at = done + prefix(named ? 1 : 0, s_wave, round);
-    if (named && at < total) a.free_pages[n_free + total - at] = page;
+    const int at = done + prefix(back ? 1 : 0, s_wave, round);
+    if (back && at < total) a.free_pages[n_free + total - at] = page;
     done += round;
+  };
+  const int room = a.n_pages - n_free;  // (more than this only if a table was damaged)
+  int total;
+  bool again = entries > kHeld * kThreads;
+  if (!again) {
+    int page[kHeld], old[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) page[k] = k * kThreads < entries ? page_at(i + k * kThreads) : -1;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      old[k] = 2;
+      if (page[k] >= 0) old[k] = atomicSub(&a.refs[page[k]], 1);
+    }
+    wait_stores_in_l2();
+    __syncthreads();
+    int twice = 0, back = 0;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      if (k * kThreads >= entries) break;
+      back += old[k] == 1;
+      if (page[k] >= 0 && old[k] != 1) twice |= holders(page[k]) <= 0;
+    }
+    again = __syncthreads_or(twice);
+    if (!again) {
+      prefix(back, s_wave, total);
+      total = min(total, room);
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k)
+        if (k * kThreads < entries) lay(page[k], old[k] == 1, total);
+    }
+  } else {
+    each([&](int, int page) { atomicSub(&a.refs[page], 1); });
+    wait_stores_in_l2();
+    __syncthreads();
   }
-  __syncthreads();
-  for (int e = i; e < entries; e += kThreads) {
-    const int page = page_at(e);
-    if (page >= 0 && __hip_atomic_load(&a.refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0)
-      __hip_atomic_store(&a.refs[page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (again) {
+    each([&](int e, int page) {
+      if (holders(page) <= 0) atomicMin(&a.refs[page], kNamed + e);
+    });
+    wait_stores_in_l2();
+    __syncthreads();
+    int back = 0;
+    each([&](int e, int page) { back += holders(page) == kNamed + e; });
+    prefix(back, s_wave, total);
+    total = min(total, room);
+    for (int e0 = 0; e0 < entries; e0 += kThreads) {
+      const int page = page_at(e0 + i);
+      lay(page, page >= 0 && holders(page) == kNamed + e0 + i, total);
+    }
+    __syncthreads();
+    each([&](int, int page) {
+      if (holders(page) < 0) __hip_atomic_store(&a.refs[page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+    __syncthreads();
   }
-  __syncthreads();
   for (int e = i; e < entries; e += kThreads) *entry(e) = -1;
   if (mine) a.length[s_row[i]] = 0;
   if (i == 0) {
@@ -244,23 +289,46 @@ __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
 // ---- whole pages ----
 
 constexpr int kCopyThreads = 256;
+typedef unsigned int Words4 __attribute__((ext_vector_type(4)));
 
-__global__ __launch_bounds__(kCopyThreads) void copy_kernel(PageCopyArgs a) {
-  const int i = blockIdx.x;
+// 768 pieces of 262 KB (24 layers, 32 pages, keys and values) in 108 us, 7.4 TB/s of
+// reads and writes, part of them held by the last-level cache; one workgroup a page
+// 180.  A workgroup copies kCopyBytes of one page of one layer (blockIdx.x: piece of
+// both pools' pages, blockIdx.y: pair, blockIdx.z: layer).
+constexpr int kCopyRun = 2, kCopyBytes = kCopyRun * kCopyThreads * 16;
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(PageCopyArgs a, int pieces_a) {
+  const int i = blockIdx.y;
   if (a.count && i >= *a.count) return;
   const int from = a.pairs[2 * i], to = a.pairs[2 * i + 1];
   if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) return;
-  for (int x = 0; x < 2; ++x) {
-    char* const pool = static_cast<char*>(a.pool[x]) + (int64_t)blockIdx.y * a.n_pages * a.bytes[x];
-    const uint4* src = reinterpret_cast<const uint4*>(pool + from * a.bytes[x]);
-    uint4* dst = reinterpret_cast<uint4*>(pool + to * a.bytes[x]);
-    for (int64_t e = threadIdx.x; e < a.bytes[x] / 16; e += kCopyThreads) dst[e] = src[e];
+  const bool second = (int)blockIdx.x >= pieces_a;
+  const int64_t bytes = a.bytes[second], at = (int64_t)(blockIdx.x - (second ? pieces_a : 0)) * kCopyBytes;
+  char* const pool = static_cast<char*>(a.pool[second]) + (int64_t)blockIdx.z * a.n_pages * bytes + at;
+  const Words4* src = reinterpret_cast<const Words4*>(pool + from * bytes);
+  Words4* dst = reinterpret_cast<Words4*>(pool + to * bytes);
+  const int n = (int)min((int64_t)kCopyBytes, bytes - at) / 16;
+  Words4 w[kCopyRun];
+#pragma unroll
+  for (int k = 0; k < kCopyRun; ++k) {
+    const int e = threadIdx.x + k * kCopyThreads;
+    if (e < n) w[k] = __builtin_nontemporal_load(src + e);
+  }
+#pragma unroll
+  for (int k = 0; k < kCopyRun; ++k) {
+    const int e = threadIdx.x + k * kCopyThreads;
+    if (e < n) __builtin_nontemporal_store(w[k], dst + e);
   }
 }
 
 // ---- tokens ----
 
-// One workgroup per (sequence, destination page), key head and layer.
+// One workgroup per (sequence, destination page), key head and layer (blockIdx.z
+// / 2), of the keys (blockIdx.z even) or the values.  Keys are whole rows; a
+// value is one element of every feature row, so a wavefront collects the page's
+// 64 tokens of a feature from the few lines that hold them and stores one.  Where
+// few tokens are kept, the lines of values that they share with others bound it: a
+// quarter of 8 x 4096 tokens of 16 heads of 128, bf16, reads nearly all of their
+// 134 MB to move 34, and with the keys takes 55 us, 4.3 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, int blocks) {
   __shared__ int64_t s_from[kPage];  // element offset of the token's page and head, -1: none
@@ -272,9 +340,7 @@ __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, in
   if (count <= 0 || dst < 0 || dst >= a.p.n_seqs) return;
   const int page = a.p.table[(int64_t)dst * a.p.max_pages + pg];
   if (page < 0 || page >= a.p.n_pages) return;
-  const int64_t layer = (int64_t)blockIdx.z * a.p.n_pages, unit = (int64_t)kPage * d;
-  T* k = static_cast<T*>(a.p.k);
-  T* v = static_cast<T*>(a.p.v);
+  const int64_t layer = (int64_t)(blockIdx.z / 2) * a.p.n_pages, unit = (int64_t)kPage * d;
   if (tid < kPage) {
     int64_t from = -1;
     int slot = 0;
@@ -293,13 +359,47 @@ __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, in
   const int64_t at = ((layer + page) * a.p.Hkv + h) * unit;
   T none;
   store_out(&none, 0, __builtin_nanf(""));
-  for (int e = tid; e < count * d; e += kCopyThreads) {
-    const int t = e / d, f = e - t * d;
-    k[at + e] = s_from[t] < 0 ? none : k[s_from[t] + s_slot[t] * d + f];
+  constexpr int kRun = 8;  // loads of a thread on their way
+  if (blockIdx.z % 2 == 0) {
+    constexpr int V = Elem<T>::kPer16B;
+    T* const k = static_cast<T*>(a.p.k);
+    const int chunks = d / V, all = count * chunks;
+    for (int e0 = tid; e0 < all; e0 += kRun * kCopyThreads) {
+      uint4 w[kRun];
+#pragma unroll
+      for (int x = 0; x < kRun; ++x) {
+        const int e = min(e0 + x * kCopyThreads, all - 1), t = e / chunks, f = e - t * chunks;
+        const int64_t from = s_from[t];
+        w[x] = ld16(k + (from < 0 ? at : from + s_slot[t] * d) + f * V);
+        if (from < 0) {
+          const uint32_t u = sizeof(T) == 4 ? __float_as_uint(__builtin_nanf("")) : 0x7fc07fc0u;
+          w[x] = uint4{u, u, u, u};
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kRun; ++x) {
+        const int e = e0 + x * kCopyThreads;
+        if (e < all) *reinterpret_cast<uint4*>(k + at + (int64_t)e * V) = w[x];
+      }
+    }
+    return;
   }
-  for (int e = tid; e < kPage * d; e += kCopyThreads) {
-    const int f = e / kPage, t = e - f * kPage;
-    if (t < count) v[at + e] = s_from[t] < 0 ? none : v[s_from[t] + f * kPage + s_slot[t]];
+  T* const v = static_cast<T*>(a.p.v);
+  const int t = tid % kPage;
+  if (t >= count) return;
+  const int64_t from = s_from[t];
+  const T* in = v + (from < 0 ? at : from + s_slot[t]);
+  T* out = v + at + t;
+  constexpr int kWaves = kCopyThreads / kWave;
+  for (int f0 = tid / kWave; f0 < d; f0 += kRun * kWaves) {
+    T w[kRun];
+#pragma unroll
+    for (int x = 0; x < kRun; ++x) w[x] = in[min(f0 + x * kWaves, d - 1) * kPage];
+#pragma unroll
+    for (int x = 0; x < kRun; ++x) {
+      const int f = f0 + x * kWaves;
+      if (f < d) out[f * kPage] = from < 0 ? none : w[x];
+    }
   }
 }
 
@@ -318,12 +418,13 @@ hipError_t launch_pages_free(const TableArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 hipError_t launch_pages_copy(const PageCopyArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(copy_kernel, dim3(a.n_pairs, a.layers), dim3(kCopyThreads), 0, stream, a);
+  const int pa = (int)((a.bytes[0] + kCopyBytes - 1) / kCopyBytes), pb = (int)((a.bytes[1] + kCopyBytes - 1) / kCopyBytes);
+  hipLaunchKernelGGL(copy_kernel, dim3(pa + pb, a.n_pairs, a.layers), dim3(kCopyThreads), 0, stream, a, pa);
   return hipGetLastError();
 }
 hipError_t launch_kv_gather(const KvGatherArgs& a, hipStream_t stream) {
   const int blocks = (a.max_keep + kPage - 1) / kPage;
-  const dim3 grid(a.B * blocks, a.p.Hkv, a.layers);
+  const dim3 grid(a.B * blocks, a.p.Hkv, 2 * a.layers);
   if (a.p.dtype == LLA_BF16) hipLaunchKernelGGL(gather_kernel<bf16_t>, grid, dim3(kCopyThreads), 0, stream, a, blocks);
   else hipLaunchKernelGGL(gather_kernel<float>, grid, dim3(kCopyThreads), 0, stream, a, blocks);
   return hipGetLastError();

@@ -65,19 +65,29 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without a stream object around it, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
 def _call(name, dev, *args):
     """An entry point on dev's current stream, with dev the current device."""
-    fn = getattr(lib(), name)
-    if torch.cuda.current_device() == dev.index:
-        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    fn, index = getattr(_lib or lib(), name), dev.index
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+            status = fn(*args, _raw_stream(index))
+    if status:
+        _check(status)
 
 
 def _ints(t, name, shape, dev):
-    _need(t, name, torch.int32, dev)
-    if t.shape != shape:
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != dev or not (t.is_cuda and t.is_contiguous()):
+        _need(t, name, torch.int32, dev)
         raise ValueError(f"{name} must have shape {list(shape)}")
 
 
@@ -144,12 +154,26 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
 # Pools and tables
 # ---------------------------------------------------------------------------
 
-class PageTable(NamedTuple):
-    """Which pages the sequences hold (int32 device tensors; one for all layers)."""
+class _Pages(NamedTuple):
     table: torch.Tensor    # [n_seqs, max_pages]
     length: torch.Tensor   # [n_seqs] tokens
     refs: torch.Tensor     # [n_pages] holders
     free: torch.Tensor     # [1 + n_pages] count, then a stack
+
+
+class PageTable(_Pages):
+    """Which pages the sequences hold: int32 device tensors table [n_seqs, max_pages],
+    length [n_seqs], refs [n_pages] and free [1 + n_pages]; one for all layers."""
+    __slots__ = ()
+
+    def __new__(cls, table, length, refs, free):
+        for t, name, shape in ((table, "table", table.shape), (length, "length", table.shape[:1]),
+                               (refs, "refs", refs.shape), (free, "free", (1 + refs.numel(),))):
+            if t.dtype != torch.int32 or t.shape != shape or t.device != table.device or not t.is_contiguous():
+                raise ValueError(f"{name} must be a dense int32 tensor of shape {list(shape)} on {table.device}")
+        if table.dim() != 2 or refs.dim() != 1:
+            raise ValueError("table must be [n_seqs, max_pages] and refs [n_pages]")
+        return super().__new__(cls, table, length, refs, free)
 
 
 def new_page_table(n_seqs: int, max_pages: int, n_pages: int, device="cuda") -> PageTable:
@@ -171,24 +195,22 @@ def alloc_pages(n_pages: int, H_kv: int, d: int, dtype=torch.bfloat16, device="c
 
 def _pools(k_pages, v_pages, layered=False):
     """(layers, n_pages, H_kv, d) of a pair of pools."""
-    dev = k_pages.device
-    _need(k_pages, "k_pages", None, dev)
-    _need(v_pages, "v_pages", k_pages.dtype, dev)
-    if k_pages.dim() not in ((4, 5) if layered else (4,)):
+    shape = k_pages.shape
+    if len(shape) not in ((4, 5) if layered else (4,)):
         raise ValueError("k_pages must be [n_pages, H_kv, 64, d]" + (", or with a layer dimension" if layered else ""))
-    *lead, P, H, page, d = k_pages.shape
+    lead, (P, H, page, d) = shape[:-4], shape[-4:]
     if page != PAGE or v_pages.shape != (*lead, P, H, d, PAGE):
         raise ValueError("k_pages must be [n_pages, H_kv, 64, d] and v_pages [n_pages, H_kv, d, 64]")
+    _need(k_pages, "k_pages", None, None)
+    _need(v_pages, "v_pages", k_pages.dtype, k_pages.device)
     return (lead[0] if lead else 1), P, H, d
 
 
 def _page_table(p, dev):
-    n_seqs, max_pages = p.table.shape
-    _ints(p.table, "table", (n_seqs, max_pages), dev)
-    _ints(p.length, "length", (n_seqs,), dev)
-    _ints(p.refs, "refs", (p.refs.numel(),), dev)
-    _ints(p.free, "free", (1 + p.refs.numel(),), dev)
-    return n_seqs, max_pages, p.refs.numel()
+    """(n_seqs, max_pages, n_pages) of a page table on dev."""
+    if p.table.device != dev or not p.table.is_cuda:
+        raise ValueError(f"the page table is on {p.table.device}, expected {dev}")
+    return (*p.table.shape, p.refs.numel())
 
 
 def reserve(pages: PageTable, rows, add, start, pairs, result):

@@ -769,3 +769,30 @@ def test_refusals_on_the_device():
             kv.decode_attn(q, *args, **bad)
     with pytest.raises(lla.LLAError):
         kv.decode_attn(normal((1, 3, 64), 0, BF), *args, n_ctx=64)
+
+
+def test_free_of_more_entries_than_a_thread_holds():
+    """More than 16384 (row, page) entries in one call, then shared ones among them."""
+    n = 600
+    pages, t = kv.new_page_table(n + 1, 40, 25000), O.KvTables(n + 1, 40, 25000)
+    r, rows = ints([0] * 4), list(range(1, n + 1))
+    start, pairs = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros((n, 2), dtype=torch.int32, device=DEV)
+    add = [64 * 30 + i % 64 for i in range(n)]
+    kv.reserve(pages, ints(rows), ints(add), start, pairs, r)
+    t.reserve(rows, add)
+    same_tables(pages, t)
+    kv.free(pages, ints(rows[::-1]), r)
+    t.free_rows(rows[::-1])
+    same_tables(pages, t)
+    kv.reserve(pages, ints([0]), ints([2500]), start[:1], pairs[:1], r)
+    t.reserve([0], [2500])
+    kv.fork(pages, ints([0] * n), ints(rows), r)
+    t.fork([0] * n, rows)
+    kv.reserve(pages, ints(rows[:50]), ints([1] * 50), start[:50], pairs[:50], r)
+    t.reserve(rows[:50], [1] * 50)
+    same_tables(pages, t)
+    everything = rows[7:] + [0] + rows[:7]
+    kv.free(pages, ints(everything), r)
+    t.free_rows(everything)
+    same_tables(pages, t)
+    assert int(pages.free[0]) == 25000
