@@ -134,7 +134,7 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
  * n_new[b] counts as at most M and no less than 0.  Slots of other positions
  * are not touched.  Pages written must have one holder, and a position must
  * occur once in a call.
- * Requires B, M, H_kv >= 1; B*M <= 2^30; B*ceil((M+63)/64) <= 2^31 - 1; sizes as above.
+ * Requires B, M >= 1; 1 <= H_kv <= 65535; B*M*H_kv <= 2^31 - 1; d_rot as above, or 0.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot, int interleaved,

@@ -161,7 +161,7 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream) {
-  if (!dtype_ok(dtype) || B < 1 || M < 1 || (int64_t)B * M > (1 << 30) || H_kv < 1 || H_kv > 65535 ||
+  if (!dtype_ok(dtype) || B < 1 || M < 1 || H_kv < 1 || H_kv > 65535 || (int64_t)B * M > std::numeric_limits<int>::max() / H_kv ||
       !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) || !std::isfinite(magnitude) ||
       !tables_ok(n_seqs, max_pages, n_pages))
     return LLA_ERR_INVALID_ARG;

@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(PageCopyArgs a, int 
 #pragma unroll
   for (int k = 0; k < kCopyRun; ++k) {
     const int e = threadIdx.x + k * kCopyThreads;
-    if (e < n) w[k] = __builtin_nontemporal_load(src + e);
+    if (e < n) w[k] = src[e];
   }
 #pragma unroll
   for (int k = 0; k < kCopyRun; ++k) {
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, in
   const int64_t at = ((layer + page) * a.p.Hkv + h) * unit;
   T none;
   store_out(&none, 0, __builtin_nanf(""));
-  constexpr int kRun = 8;  // loads of a thread on their way
+  constexpr int kRun = 4;  // loads of a thread on their way
   if (blockIdx.z % 2 == 0) {
     constexpr int V = Elem<T>::kPer16B;
     T* const k = static_cast<T*>(a.p.k);
@@ -379,7 +379,8 @@ __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, in
 #pragma unroll
       for (int x = 0; x < kRun; ++x) {
         const int e = e0 + x * kCopyThreads;
-        if (e < all) *reinterpret_cast<uint4*>(k + at + (int64_t)e * V) = w[x];
+        if (e < all)
+          __builtin_nontemporal_store(__builtin_bit_cast(Words4, w[x]), reinterpret_cast<Words4*>(k + at + (int64_t)e * V));
       }
     }
     return;
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kCopyThreads) void gather_kernel(KvGatherArgs a, in
 #pragma unroll
     for (int x = 0; x < kRun; ++x) {
       const int f = f0 + x * kWaves;
-      if (f < d) out[f * kPage] = from < 0 ? none : w[x];
+      if (f < d) __builtin_nontemporal_store(from < 0 ? none : w[x], &out[f * kPage]);
     }
   }
 }

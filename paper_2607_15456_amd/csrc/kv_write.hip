@@ -80,25 +80,26 @@ __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
 // one key head, its keys or its values.  Values go through LDS, up to 128 features
 // at a time, read there by columns, 16 bytes of a feature row at a time.  Small
 // workgroups keep many loads in flight: prompts of 4001 to 2501 tokens, 16 heads of
-// 128, take 47 us (4.5 TB/s; a large copy runs at 4.8), with one angle for 2, 4 or
-// 16 heads of a workgroup 48, 51, 84; without non-temporal stores 6 us more.
+// 128, not in a cache take 47 us (4.4 TB/s; a large copy runs at 5.0); a workgroup with
+// one angle for 2, 4 or 16 heads takes 1, 5, 40 us more, plain stores 2.
 template <typename T, int N, bool Interleaved>
 __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int blocks) {
   constexpr int V = Elem<T>::kPer16B, kCols = 128, kRow = kCols + V;
   __shared__ __align__(16) T s_v[kPage * kRow];
-  const int b = blockIdx.x / blocks, h = blockIdx.y, d = a.p.d, tid = threadIdx.x;
+  // heads side by side, as a token's rows are (52 -> 47 us against pages side by side)
+  const int h = blockIdx.x % a.p.Hkv, wg = blockIdx.x / a.p.Hkv;
+  const int b = wg / blocks, d = a.p.d, tid = threadIdx.x;
   const Entry e(a, b);
-  const int64_t slot = e.first / kPage + blockIdx.x % blocks;
+  const int64_t slot = e.first / kPage + wg % blocks;
   // tokens [m0, m1), at positions t0 .. t1 - 1 of the page
   const int64_t base = slot * kPage - e.first;
   const int m0 = (int)max((int64_t)0, base), m1 = (int)min((int64_t)e.n, base + kPage);
   if (m0 >= m1) return;
-  const int page = e.page(a, slot);
-  if (page < 0) return;
+  const int page = e.page(a, slot);  // (needed by the stores: the rows are requested beside it)
   const int t0 = (int)(m0 - base), t1 = t0 + (m1 - m0), count = m1 - m0;
   const int64_t unit = ((int64_t)page * a.p.Hkv + h) * kPage * d;
 
-  if (blockIdx.z == 0) {
+  if (blockIdx.y == 0) {
     const T* k = static_cast<const T*>(a.k) + b * a.kb + m0 * a.km + (int64_t)h * d;
     T* kp = static_cast<T*>(a.p.k) + unit + t0 * d;
     const int half = a.rot / 2, turned = half / N, units = turned + (d - a.rot) / 8;
@@ -112,10 +113,11 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
         Turn<N> t;
         t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
         p.turn(t);
-        p.template store<true>(kp + i * d, u * N, half);
+        if (page >= 0) p.store_past(kp + i * d, u * N, half);
       } else {
         const int f = a.rot + 8 * (u - turned);
-        Run<T, 8>::load(k + i * a.km + f).template store<true>(kp + i * d + f);
+        const Run<T, 8> r = Run<T, 8>::load(k + i * a.km + f);
+        if (page >= 0) r.store_past(kp + i * d + f);
       }
     }
     return;
@@ -131,6 +133,7 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
       *reinterpret_cast<uint4*>(s_v + (t0 + i) * kRow + f * V) = ld16(v + i * a.vm + f * V);
     }
     __syncthreads();
+    if (page < 0) return;
     // 64 / V runs of a feature row side by side, so a row's lines are written together
     constexpr int kRuns = kPage / V;
     for (int x = tid; x < cols * kRuns; x += kThreads) {
@@ -143,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
           if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[(t + i) * kRow + f]);
           else if (i % 2 == 0) r.w[i / 2] = s_v[(t + i) * kRow + f] | (uint32_t(s_v[(t + i + 1) * kRow + f]) << 16);
         }
-        r.template store<true>(vp + f * kPage + t);
+        r.store_past(vp + f * kPage + t);
       } else {
         for (int i = max(t, t0); i < min(t + V, t1); ++i) vp[f * kPage + i] = s_v[i * kRow + f];
       }
@@ -166,7 +169,7 @@ hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
     return hipGetLastError();
   }
   const int blocks = (a.M + 2 * kPage - 2) / kPage;  // pages that M positions can touch
-  hipLaunchKernelGGL((write_page_kernel<T, N, Interleaved>), dim3(a.B * blocks, a.p.Hkv, 2), dim3(kThreads), 0, stream, a,
+  hipLaunchKernelGGL((write_page_kernel<T, N, Interleaved>), dim3((unsigned)a.B * blocks * a.p.Hkv, 2), dim3(kThreads), 0, stream, a,
                      blocks);
   return hipGetLastError();
 }

@@ -17,12 +17,9 @@ struct Run {
   typedef uint32_t Words __attribute__((ext_vector_type(kBytes / 4)));
   Words w;
   __device__ __forceinline__ static Run load(const void* p) { return Run{*static_cast<const Words*>(p)}; }
-  // Past: the non-temporal policy, for results that leave the caches anyway
-  template <bool Past = false>
-  __device__ __forceinline__ void store(void* p) const {
-    if constexpr (Past) __builtin_nontemporal_store(w, static_cast<Words*>(p));
-    else *static_cast<Words*>(p) = w;
-  }
+  __device__ __forceinline__ void store(void* p) const { *static_cast<Words*>(p) = w; }
+  // with the non-temporal policy
+  __device__ __forceinline__ void store_past(void* p) const { __builtin_nontemporal_store(w, static_cast<Words*>(p)); }
   __device__ __forceinline__ float get(int i) const;
   __device__ __forceinline__ void set(int i, float v);
 };
@@ -112,10 +109,13 @@ struct Pairs {
       }
     }
   }
-  template <bool Past = false>
   __device__ __forceinline__ void store(T* y, int p0, int half) const {
-    a.template store<Past>(y + first(p0));
-    b.template store<Past>(y + second(p0, half));
+    a.store(y + first(p0));
+    b.store(y + second(p0, half));
+  }
+  __device__ __forceinline__ void store_past(T* y, int p0, int half) const {
+    a.store_past(y + first(p0));
+    b.store_past(y + second(p0, half));
   }
 };
 

@@ -23,7 +23,7 @@ __device__ __forceinline__ int64_t position(const RotaryArgs& a, int b, int m) {
 
 // One thread per (token, run of N pairs or of 8 copied features) and chunk of
 // heads (blockIdx.y).
-template <typename T, int N, bool Interleaved, bool Past>
+template <typename T, int N, bool Interleaved>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int units, int heads_per) {
   const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t tok = idx / units;
@@ -43,33 +43,33 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int unit
     t.at((double)position(a, b, m), freq, a.magnitude, a.sign);
     for (int h = h0;;) {
       p.turn(t);
-      p.template store<Past>(y + h * a.yh, u * N, half);
+      p.store(y + h * a.yh, u * N, half);
       if (++h >= h1) break;
       p.load(x + h * a.xh, u * N, half);
     }
   } else {
     const int f = a.rot + 8 * (u - turned);
-    for (int h = h0; h < h1; ++h) Run<T, 8>::load(x + h * a.xh + f).template store<Past>(y + h * a.yh + f);
+    for (int h = h0; h < h1; ++h) Run<T, 8>::load(x + h * a.xh + f).store(y + h * a.yh + f);
   }
 }
 
 // Few rows get a thread for each head, so that they spread over the device; from
-// kMany runs on a thread turns two heads with one angle and stores past the
-// caches, which the result no longer fits (4 x 8192 tokens of 16 heads of 128,
-// bf16: one head 57 us, two 45, four 47; two without the non-temporal stores 53;
-// 3 x 1501 tokens of 16 heads of 96, fp32, 64 turned: one head 14.0, two 15.0).
+// kMany runs on a thread turns kHeads heads with one angle.  4 x 8192 tokens of 16
+// heads of 128, bf16, not in a cache: one head 71 us, two 50, four 50 (5.2 TB/s; a
+// large copy runs at 5.0), four with two or four of them loaded together 51, 52,
+// non-temporal stores 69; 3 x 1501 tokens of 16 heads of 96, fp32, 64 turned: one 13.8,
+// four 15.3.
 constexpr int64_t kMany = 1 << 21;
+constexpr int kHeads = 4;
 
 template <typename T, int N, bool Interleaved>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
   const int units = a.rot / 2 / N + (a.x == a.y ? 0 : (a.d - a.rot) / 8);
   const int64_t runs = (int64_t)a.B * a.M * units;
-  const unsigned blocks = (unsigned)((runs + kThreads - 1) / kThreads);
-  if (runs * a.H < kMany)
-    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, false>), dim3(blocks, a.H), dim3(kThreads), 0, stream, a, units, 1);
-  else
-    hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved, true>), dim3(blocks, (a.H + 1) / 2), dim3(kThreads), 0, stream, a,
-                       units, 2);
+  const int heads_per = runs * a.H < kMany ? 1 : kHeads;
+  hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved>),
+                     dim3((unsigned)((runs + kThreads - 1) / kThreads), (a.H + heads_per - 1) / heads_per), dim3(kThreads), 0,
+                     stream, a, units, heads_per);
   return hipGetLastError();
 }
 
