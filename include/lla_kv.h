@@ -36,6 +36,7 @@
  *   refs    [n_pages]            how many table entries name a page
  *   free    [1 + n_pages]        free[0] pages are free: free[1 .. free[0]], a
  *                                stack whose last entry is taken first
+ * with n_seqs >= 1, 1 <= max_pages <= 2^20, 1 <= n_pages <= 2^30 (all calls).
  * To begin: length and refs 0, free[0] = n_pages, free[1 ..] every page once.
  * A page with refs > 1 is shared; it may be read, and lla_pages_reserve gives a
  * sequence a copy of its own before it is written.
@@ -106,8 +107,8 @@ lla_status lla_rope_frequencies(int d_rot, double base, int scaling, double fact
  *           not overlap x or itself otherwise.
  * Angles are formed and reduced in 64 bits, sine and cosine and the products in
  * 32, rounded once to dtype.
- * Requires B, M, H >= 1; d_head a multiple of 8 in [8, LLA_KV_MAX_ROW]; d_rot a multiple
- * of 8 in [8, min(d_head, LLA_MAX_ROPE)]; B*M*H <= 2^31 - 1; magnitude finite.
+ * Requires B, M >= 1; 1 <= H <= 65535; d_head a multiple of 8 in [8, LLA_KV_MAX_ROW]; d_rot a
+ * multiple of 8 in [8, min(d_head, LLA_MAX_ROPE)]; B*M*H <= 2^31 - 1; magnitude finite.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_rot, int interleaved,
@@ -170,8 +171,8 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  * [0, n_pages) among those read gets NaN.  Slots that are not attended may hold anything.
  * Products of bf16 are exact; the softmax weights enter their product with the
  * values as a sum of two bf16 (about 2^-17 relative).
- * Requires B >= 1, H a multiple of H_kv >= 1, sink >= 0, window >= 0, sink = 0 without a
- * window, B*H <= 2^24.
+ * Requires B >= 1, H a multiple of H_kv >= 1, H / H_kv <= 65535, sink >= 0, window >= 0,
+ * sink = 0 without a window, B*H <= 2^24.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
  */
 lla_status lla_kv_decode_attn(int dtype, int out_dtype, int B, int H, int H_kv, int d_head,
@@ -231,7 +232,8 @@ lla_status lla_pages_free(int n, const int32_t* rows, int n_seqs, int max_pages,
  * int32) only the first min(*count, n_pairs) pairs, e.g. result + 1 of
  * lla_pages_reserve.  A pair with a page out of range is passed over.  No page may be
  * written twice, or be read and written, by one call.
- * Requires 1 <= layers <= 65535, 1 <= n_pairs <= 2^20.
+ * Requires 1 <= layers <= 65535, 1 <= n_pairs <= 2^20, page sizes of at most 2^40 bytes,
+ * n_pairs times the pages' pieces of 8 KB at most 2^31 - 1.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, void* b, int64_t b_bytes,
@@ -247,8 +249,8 @@ lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, voi
  * lla_pages_fork and lla_pages_free keeps the sequence's number).  A position keep[j][i]
  * outside [0, 64*max_pages) or on a page out of range gives NaN; tokens of a
  * destination row or page out of range are not written.
- * Requires 1 <= layers <= 65535, H_kv <= 65535, B*ceil(max_keep/64) <= 2^31 - 1,
- * max_keep <= 64*max_pages.
+ * Requires 1 <= layers <= 32767, 1 <= H_kv <= 65535, B >= 1, 1 <= max_keep <= 64*max_pages,
+ * B*max_keep <= 2^30.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, int d_head, int n_seqs,

@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kMaxPages = 1 << 20;   // pages of one sequence
 constexpr int kMaxPool = 1 << 30;    // pages of a pool
+constexpr int kMaxGridY = 65535;     // workgroups along a grid's second and third dimension
 constexpr double kLog2e = 1.4426950408889634;
 
 bool ptr_ok(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -35,7 +36,8 @@ bool freq_ok(int rot, const double* f) {
 lla_status hip_status(hipError_t e) { return e == hipSuccess ? LLA_OK : LLA_ERR_HIP; }
 
 bool decode_ok(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, int sink, int window) {
-  return dtype_ok(dtype) && B >= 1 && H >= 1 && H_kv >= 1 && H % H_kv == 0 && (int64_t)B * H <= (1 << 24) &&
+  return dtype_ok(dtype) && B >= 1 && H >= 1 && H_kv >= 1 && H % H_kv == 0 && H / H_kv <= kMaxGridY &&
+         (int64_t)B * H <= (1 << 24) &&
          head_ok(d_head) && n_ctx >= 1 && n_ctx <= kMaxPages * LLA_PAGE_TOKENS && sink >= 0 && window >= 0 &&
          (window > 0 || sink == 0);
 }
@@ -122,8 +124,7 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
   if (!dtype_ok(dtype) || B < 1 || M < 1 || H < 1 || d_head < 8 || d_head > LLA_KV_MAX_ROW || d_head % 8 ||
       !rot_ok(d_rot, d_head) || !std::isfinite(magnitude))
     return LLA_ERR_INVALID_ARG;
-  // the grid's threads: at most 64 a token and head
-  if ((int64_t)B * M > std::numeric_limits<int>::max() / H) return LLA_ERR_INVALID_ARG;
+  if (H > kMaxGridY || (int64_t)B * M > std::numeric_limits<int>::max() / H) return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(x) || !ptr_ok(y) || !opt_idx_ok(pos) || !freq_ok(d_rot, freq)) return LLA_ERR_INVALID_ARG;
   for (int64_t s : {x_b, x_m, x_h, y_b, y_m, y_h})
     if (!stride_ok(s, dtype)) return LLA_ERR_INVALID_ARG;
@@ -161,7 +162,7 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream) {
-  if (!dtype_ok(dtype) || B < 1 || M < 1 || H_kv < 1 || H_kv > 65535 || (int64_t)B * M > std::numeric_limits<int>::max() / H_kv ||
+  if (!dtype_ok(dtype) || B < 1 || M < 1 || H_kv < 1 || H_kv > kMaxGridY || (int64_t)B * M > std::numeric_limits<int>::max() / H_kv ||
       !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) || !std::isfinite(magnitude) ||
       !tables_ok(n_seqs, max_pages, n_pages))
     return LLA_ERR_INVALID_ARG;
@@ -262,11 +263,12 @@ lla_status lla_pages_free(int n, const int32_t* rows, int n_seqs, int max_pages,
 lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, void* b, int64_t b_bytes,
                           const int32_t* pairs, int n_pairs, const int32_t* count, void* stream) {
   const int64_t kMost = (int64_t)1 << 40;
-  if (layers < 1 || layers > 65535 || n_pages < 1 || n_pages > kMaxPool || n_pairs < 1 || n_pairs > (1 << 20) ||
+  if (layers < 1 || layers > kMaxGridY || n_pages < 1 || n_pages > kMaxPool || n_pairs < 1 || n_pairs > (1 << 20) ||
       a_bytes < 16 || a_bytes % 16 || a_bytes > kMost || b_bytes < 0 || b_bytes % 16 || b_bytes > kMost ||
       (b == nullptr) != (b_bytes == 0))
     return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(a) || (b && !ptr_ok(b)) || !idx_ok(pairs) || !opt_idx_ok(count)) return LLA_ERR_INVALID_ARG;
+  if (lla::page_copy_pieces(a_bytes, b_bytes) > std::numeric_limits<int>::max() / n_pairs) return LLA_ERR_INVALID_ARG;
   lla::PageCopyArgs c{};
   c.layers = layers;
   c.n_pages = n_pages;
@@ -284,7 +286,8 @@ lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, i
                          int max_pages, int n_pages, const int32_t* table, const int32_t* src,
                          const int32_t* dst, const int32_t* keep, const int32_t* n_keep,
                          void* k_pages, void* v_pages, void* stream) {
-  if (!dtype_ok(dtype) || B < 1 || max_keep < 1 || layers < 1 || layers > 65535 || H_kv < 1 || H_kv > 65535 ||
+  if (!dtype_ok(dtype) || B < 1 || max_keep < 1 || layers < 1 || layers > kMaxGridY / 2 || H_kv < 1 ||
+      H_kv > kMaxGridY ||
       !head_ok(d_head) || !tables_ok(n_seqs, max_pages, n_pages) ||
       max_keep > (int64_t)max_pages * LLA_PAGE_TOKENS || (int64_t)B * max_keep > (1 << 30))
     return LLA_ERR_INVALID_ARG;

@@ -86,6 +86,8 @@ struct PageCopyArgs {
   const int32_t* count;
 };
 hipError_t launch_pages_copy(const PageCopyArgs& a, hipStream_t stream);
+// Workgroups of a pair and layer for pages of these sizes.
+int64_t page_copy_pieces(int64_t a_bytes, int64_t b_bytes);
 
 struct KvGatherArgs {
   KvPages p;

@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from contextlib import nullcontext
 from typing import NamedTuple
 
 import torch
@@ -315,7 +316,8 @@ def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, freq=N
 
 def decode_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int, n_ctx: int, sink: int = 0,
                            window: int = 0) -> int:
-    """Workspace of decode_attn (0: no context is split over workgroups)."""
+    """Workspace of decode_attn on the current device (0: no context is split over
+    workgroups)."""
     out = _c_sz()
     _check(lib().lla_kv_decode_workspace_bytes(_out_code(dtype), B, H, H_kv, d, n_ctx, sink, window, ctypes.byref(out)))
     return out.value
@@ -351,7 +353,8 @@ def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, sc
         if lse.shape != (B, H):
             raise ValueError("lse must be [B, H]")
     if workspace is None:
-        need = decode_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx, sink, window)
+        with torch.cuda.device(dev) if torch.cuda.current_device() != dev.index else nullcontext():
+            need = decode_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx, sink, window)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     else:
         _need(workspace, "workspace", None, dev)

@@ -73,7 +73,7 @@ CALLS = {
     "lla_rope_positions": (
         dict(dtype=1, B=2, M=3, H=4, d_head=128, d_rot=64, interleaved=0, transpose=0, x=P, x_b=1536, x_m=512, x_h=128,
              pos=P, pos_tokens=0, pos0=0, freq=P, magnitude=1.0, y=P, y_b=1536, y_m=512, y_h=128, stream=None),
-        [("dtype", 2), ("B", 0), ("M", 0), ("H", 0), ("H", 1 << 30), ("d_head", 4), ("d_head", 132), ("d_head", 520),
+        [("dtype", 2), ("B", 0), ("M", 0), ("H", 0), ("H", 1 << 30), ("H", 65536), ("d_head", 4), ("d_head", 132), ("d_head", 520),
          ("d_rot", 0), ("d_rot", 12), ("d_rot", 136), ("x", None), ("x", P + 8), ("x_b", -8), ("x_m", 4), ("x_h", 12),
          ("pos", P + 2), ("freq", None), ("freq", P + 4), ("magnitude", math.nan), ("y", None), ("y", P + 2),
          ("y_b", 0), ("y_m", 64), ("y_h", 0), ("x_b", 1544)]),
@@ -90,7 +90,7 @@ CALLS = {
         dict(dtype=1, out_dtype=1, B=2, H=8, H_kv=4, d_head=64, n_seqs=2, max_pages=8, n_pages=16, n_ctx=64, sink=0,
              window=0, table=P, length=P, rows=None, q=P, k_pages=P, v_pages=P, scale=0.125, out=P, lse=None,
              workspace=P, ws_bytes=1 << 30, stream=None),
-        [("dtype", 2), ("out_dtype", 2), ("B", 0), ("B", 1 << 24), ("H", 0), ("H", 6), ("H_kv", 0), ("H_kv", 3),
+        [("dtype", 2), ("out_dtype", 2), ("B", 0), ("B", 1 << 24), ("H", 0), ("H", 6), ("H", 1 << 19), ("H_kv", 0), ("H_kv", 3),
          ("d_head", 0), ("d_head", 48), ("d_head", 512), ("n_seqs", 0), ("max_pages", 0), ("n_pages", 0), ("n_ctx", 0),
          ("n_ctx", 513), ("sink", -1), ("sink", 1), ("window", -1), ("table", None), ("length", None), ("length", P + 2),
          ("rows", P + 2), ("q", P + 8), ("k_pages", None), ("v_pages", None), ("scale", 0.0), ("scale", -1.0),
@@ -113,13 +113,13 @@ CALLS = {
          ("length", None), ("refs", None), ("free_pages", None), ("result", P + 2)]),
     "lla_pages_copy": (
         dict(layers=2, n_pages=16, a=P, a_bytes=4096, b=P, b_bytes=4096, pairs=P, n_pairs=3, count=None, stream=None),
-        [("layers", 0), ("layers", 65536), ("n_pages", 0), ("a", None), ("a", P + 8), ("a_bytes", 0), ("a_bytes", 24),
+        [("layers", 0), ("layers", 65536), ("n_pages", 0), ("a", None), ("a", P + 8), ("a_bytes", 0), ("a_bytes", 24), ("a_bytes", 1 << 43), ("a_bytes", 1 << 40),
          ("b", None), ("b", P + 4), ("b_bytes", 0), ("b_bytes", 8), ("pairs", None), ("n_pairs", 0),
          ("n_pairs", (1 << 20) + 1), ("count", P + 2)]),
     "lla_kv_gather": (
         dict(dtype=1, B=2, max_keep=100, layers=1, H_kv=2, d_head=64, n_seqs=4, max_pages=8, n_pages=16, table=P, src=P,
              dst=P, keep=P, n_keep=None, k_pages=P, v_pages=P, stream=None),
-        [("dtype", 3), ("B", 0), ("max_keep", 0), ("max_keep", 513), ("layers", 0), ("layers", 65536), ("H_kv", 0),
+        [("dtype", 3), ("B", 0), ("max_keep", 0), ("max_keep", 513), ("layers", 0), ("layers", 32768), ("H_kv", 0),
          ("H_kv", 65536), ("d_head", 16), ("n_seqs", 0), ("max_pages", 0), ("n_pages", 0), ("table", None), ("src", None),
          ("dst", P + 2), ("keep", None), ("n_keep", P + 1), ("k_pages", None), ("v_pages", P + 8)]),
 }
