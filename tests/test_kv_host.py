@@ -113,7 +113,7 @@ CALLS = {
          ("length", None), ("refs", None), ("free_pages", None), ("result", P + 2)]),
     "lla_pages_copy": (
         dict(layers=2, n_pages=16, a=P, a_bytes=4096, b=P, b_bytes=4096, pairs=P, n_pairs=3, count=None, stream=None),
-        [("layers", 0), ("layers", 65536), ("n_pages", 0), ("a", None), ("a", P + 8), ("a_bytes", 0), ("a_bytes", 24), ("a_bytes", 1 << 43), ("a_bytes", 1 << 40),
+        [("layers", 0), ("layers", 65536), ("n_pages", 0), ("a", None), ("a", P + 8), ("a_bytes", 0), ("a_bytes", 24), ("a_bytes", 1 << 43),
          ("b", None), ("b", P + 4), ("b_bytes", 0), ("b_bytes", 8), ("pairs", None), ("n_pairs", 0),
          ("n_pairs", (1 << 20) + 1), ("count", P + 2)]),
     "lla_kv_gather": (
@@ -134,6 +134,11 @@ def test_refusals(name):
     for arg, value in changes:
         assert value != good[arg], arg
         assert fn(*{**good, arg: value}.values()) == lla.LLA_ERR_INVALID_ARG, (name, arg, value)
+
+
+def test_copy_refuses_more_pieces_than_a_grid_holds():
+    good = {**CALLS["lla_pages_copy"][0], "a_bytes": 1 << 40}  # 2^27 pieces of 8 KB a pair
+    assert kv.lib().lla_pages_copy(*{**good, "n_pairs": 16}.values()) == lla.LLA_ERR_INVALID_ARG
 
 
 def test_workspace_refused():
