@@ -321,15 +321,16 @@ __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m
 // NT tiles of 16 query heads.  Two wavefronts a SIMD; one above a width of 128,
 // where steps are twice as large, so as many bytes are on their way, and with two
 // tiles, whose accumulators need the registers.
-template <template <int, int> class StepOf, int D, int NT, int W>
-__global__ __launch_bounds__(W* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
+template <template <int, int> class StepOf, int D, int NT>
+__global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
   typedef StepOf<D, NT> Step;
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
   constexpr int kRow = D + 4, kCols = NT * kTile;
   // the wavefronts' steps, then what they join
-  __shared__ __align__(16) char s_raw[W * kStepBytes];
-  static_assert(W / 2 * kCols * (kRow + 2) * 4 <= W * kStepBytes);
+  extern __shared__ __align__(16) char s_raw[];
+  static_assert(kCols * (kRow + 2) * 4 <= 2 * kStepBytes);
+  const int W = blockDim.x / kWave;  // 1, 2 or 4
   float* const s_o = reinterpret_cast<float*>(s_raw);
   float(*const s_ml)[2][kCols] = reinterpret_cast<float(*)[2][kCols]>(s_o + W / 2 * kCols * kRow);
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
@@ -455,8 +456,7 @@ __global__ __launch_bounds__(W* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void d
   }
 
   // join the wavefronts, the upper half into the lower
-  __syncthreads();
-#pragma unroll
+  if (W > 1) __syncthreads();
   for (int half = W / 2; half >= 1; half /= 2) {
     if (w >= half && w < 2 * half) {
 #pragma unroll
@@ -578,16 +578,20 @@ int query_blocks(int group, int d) {
 
 template <template <int, int> class StepOf, int D>
 void launch_step(const KvDecodeArgs& a, hipStream_t stream) {
-  constexpr int W = kWaves;
+  typedef StepOf<D, 1> Step;
   const int group = a.H / a.p.Hkv;
   const dim3 grid(a.B * a.p.Hkv * a.slices, query_blocks(group, D));
+  // wavefronts: no more than a slice has steps
+  const int64_t steps = (int64_t)a.per * (kPage / Step::kTok);
+  const int W = steps >= kWaves ? kWaves : steps >= 2 ? 2 : 1;
+  const size_t lds = (size_t)W * Step::kTok * D * Step::kBytes;
   if constexpr (D <= kTwoTiles) {
     if (query_tiles(group, D) == 2) {
-      hipLaunchKernelGGL((decode_kernel<StepOf, D, 2, W>), grid, dim3(W * kWave), 0, stream, a);
+      hipLaunchKernelGGL((decode_kernel<StepOf, D, 2>), grid, dim3(W * kWave), lds, stream, a);
       return;
     }
   }
-  hipLaunchKernelGGL((decode_kernel<StepOf, D, 1, W>), grid, dim3(W * kWave), 0, stream, a);
+  hipLaunchKernelGGL((decode_kernel<StepOf, D, 1>), grid, dim3(W * kWave), lds, stream, a);
 }
 
 template <int D>
