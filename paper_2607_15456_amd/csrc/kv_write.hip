@@ -32,28 +32,27 @@ struct Entry {
   }
 };
 
-// Few tokens: one thread per (token, head) and run of N key pairs, of 8 copied
-// key features, or of 8 value features (stored one by one: a token is one
-// element of every feature row).
+// Few tokens: one thread per (token, head) and part of the key row or 8 value
+// features (stored one by one: a token is one element of every feature row).
 template <typename T, int N, bool Interleaved>
 __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
-  const int d = a.p.d, half = a.rot / 2, turned = half / N, kept = (d - a.rot) / 8, units = turned + kept + d / 8;
+  typedef Part<T, N, Interleaved> KeyPart;
+  const int d = a.p.d, parts = KeyPart::count(a.rot, d - a.rot), units = parts + d / 8;
   const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t at = idx / units;  // (b, m, h)
   const int u = (int)(idx - at * units);
   if (at >= (int64_t)a.B * a.M * a.p.Hkv) return;
   const int h = (int)(at % a.p.Hkv), bm = (int)(at / a.p.Hkv), b = bm / a.M, m = bm - b * a.M;
-  const T* k = static_cast<const T*>(a.k) + b * a.kb + m * a.km + (int64_t)h * d;
-  const T* v = static_cast<const T*>(a.v) + b * a.vb + m * a.vm + (int64_t)h * d;
   // the input is requested before the chain of entry, page and angle
-  Pairs<T, N, Interleaved> p;
+  KeyPart p(u, a.rot, d);
   Run<T, 8> r;
   double freq[N];
-  if (u < turned) {
-    p.load(k, u * N, half);
-    load_freq(freq, a.freq + u * N);
+  const bool key = u < parts;
+  if (key) {
+    p.load(static_cast<const T*>(a.k) + b * a.kb + m * a.km + (int64_t)h * d);
+    if (p.turned) p.load_freq(freq, a.freq);
   } else {
-    r = Run<T, 8>::load(u < turned + kept ? k + a.rot + 8 * (u - turned) : v + 8 * (u - turned - kept));
+    r = Run<T, 8>::load(static_cast<const T*>(a.v) + b * a.vb + m * a.vm + (int64_t)h * d + 8 * (u - parts));
   }
   const Entry e(a, b);
   if (m >= e.n) return;
@@ -61,18 +60,15 @@ __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
   const int page = e.page(a, pos / kPage), t = (int)(pos % kPage);
   if (page < 0) return;
   const int64_t unit = ((int64_t)page * a.p.Hkv + h) * kPage * d;
-  T* kp = static_cast<T*>(a.p.k) + unit + t * d;
-  T* vp = static_cast<T*>(a.p.v) + unit + t;
-  if (u < turned) {
+  if (key) {
     Turn<N> turn;
-    turn.at((double)pos, freq, a.magnitude, 1.f);
+    if (p.turned) turn.at((double)pos, freq, a.magnitude, 1.f);
     p.turn(turn);
-    p.store(kp, u * N, half);
-  } else if (u < turned + kept) {
-    r.store(kp + a.rot + 8 * (u - turned));
+    p.store(static_cast<T*>(a.p.k) + unit + t * d);
   } else {
+    T* vp = static_cast<T*>(a.p.v) + unit + t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) store_out(vp, (8 * (u - turned - kept) + i) * kPage, r.get(i));
+    for (int i = 0; i < 8; ++i) store_out(vp, (8 * (u - parts) + i) * kPage, r.get(i));
   }
 }
 
@@ -102,23 +98,19 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
   if (blockIdx.y == 0) {
     const T* k = static_cast<const T*>(a.k) + b * a.kb + m0 * a.km + (int64_t)h * d;
     T* kp = static_cast<T*>(a.p.k) + unit + t0 * d;
-    const int half = a.rot / 2, turned = half / N, units = turned + (d - a.rot) / 8;
-    for (int x = tid; x < count * units; x += kThreads) {
-      const int i = x / units, u = x - i * units;
-      if (u < turned) {
-        Pairs<T, N, Interleaved> p;
-        p.load(k + i * a.km, u * N, half);
+    const int parts = Part<T, N, Interleaved>::count(a.rot, d - a.rot);
+    for (int x = tid; x < count * parts; x += kThreads) {
+      const int i = x / parts;
+      Part<T, N, Interleaved> p(x - i * parts, a.rot, d);
+      p.load(k + i * a.km);
+      Turn<N> t;
+      if (p.turned) {
         double freq[N];
-        load_freq(freq, a.freq + u * N);
-        Turn<N> t;
+        p.load_freq(freq, a.freq);
         t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
-        p.turn(t);
-        if (page >= 0) p.store_past(kp + i * d, u * N, half);
-      } else {
-        const int f = a.rot + 8 * (u - turned);
-        const Run<T, 8> r = Run<T, 8>::load(k + i * a.km + f);
-        if (page >= 0) r.store_past(kp + i * d + f);
       }
+      p.turn(t);
+      if (page >= 0) p.store_past(kp + i * d);
     }
     return;
   }
@@ -162,7 +154,7 @@ template <typename T, int N, bool Interleaved>
 hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
   const int d = a.p.d;
   if (a.M < kPaged) {
-    const int units = a.rot / 2 / N + (d - a.rot) / 8 + d / 8;
+    const int units = Part<T, N, Interleaved>::count(a.rot, d - a.rot) + d / 8;
     const int64_t runs = (int64_t)a.B * a.M * a.p.Hkv * units;
     hipLaunchKernelGGL((write_few_kernel<T, N, Interleaved>), dim3((unsigned)((runs + kThreads - 1) / kThreads)),
                        dim3(kThreads), 0, stream, a);

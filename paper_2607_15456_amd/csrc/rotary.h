@@ -2,8 +2,6 @@
 // pairs, shared by the embedding of queries (rotary.hip) and the write of keys
 // into their pages (kv_write.hip).
 //
-// A thread holds the N pairs of one token and turns them for several heads, so
-// the angle (64-bit product and reduction, sine and cosine) is paid once.
 #pragma once
 
 #include "lla_device.h"
@@ -73,28 +71,42 @@ struct Turn {
     }
   }
 };
-template <int N>
-__device__ __forceinline__ void load_freq(double (&f)[N], const double* p) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) f[i] = p[i];
-}
-
-// The N pairs from pair p0 on of the row at x, turned, to the row at y (which
-// may be x): features (i, i + half), or (2i, 2i + 1) when interleaved.
+// A thread's part of a row: a run of N features and the one as far behind it as
+// half of the turned features, or half of the copied ones, are wide, so that
+// neighbouring threads touch neighbouring runs.  Half-split these are N pairs;
+// interleaved, N/2 pairs each; copied, the second may lie past the row's end.
+// Turned and copied parts are moved alike: a wavefront that holds both does not
+// branch.
 template <typename T, int N, bool Interleaved>
-struct Pairs {
-  Run<T, N> a, b;  // half-split: features p0 .., half + p0 ..; interleaved: 2 p0 .., 2 p0 + N ..
-  __device__ __forceinline__ static int first(int p0) { return Interleaved ? 2 * p0 : p0; }
-  __device__ __forceinline__ static int second(int p0, int half) { return Interleaved ? 2 * p0 + N : half + p0; }
-  __device__ __forceinline__ void load(const T* x, int p0, int half) {
-    a = Run<T, N>::load(x + first(p0));
-    b = Run<T, N>::load(x + second(p0, half));
+struct Part {
+  bool turned, second;
+  int a_at, b_at;
+  // parts of `copied` features, and of a row
+  __host__ __device__ __forceinline__ static int copies(int copied) { return (copied + 2 * N - 1) / (2 * N); }
+  __host__ __device__ __forceinline__ static int count(int rot, int copied) { return rot / 2 / N + copies(copied); }
+  __device__ __forceinline__ Part(int u, int rot, int d) {
+    const int pairs = rot / 2 / N;
+    turned = u < pairs;
+    a_at = turned ? u * N : rot + (u - pairs) * N;
+    b_at = a_at + (turned ? rot / 2 : copies(d - rot) * N);
+    second = b_at < d;
+  }
+  __device__ __forceinline__ void load_freq(double (&f)[N], const double* p) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = p[!Interleaved ? a_at + i : i < N / 2 ? a_at / 2 + i : b_at / 2 + i - N / 2];
+  }
+
+  Run<T, N> a, b;
+  __device__ __forceinline__ void load(const T* x) {
+    a = Run<T, N>::load(x + a_at);
+    b = Run<T, N>::load(x + (second ? b_at : a_at));
   }
   __device__ __forceinline__ void turn(const Turn<N>& t) {
+    Run<T, N> p = a, q = b;
     if constexpr (Interleaved) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        Run<T, N>& r = i < N / 2 ? a : b;
+        Run<T, N>& r = i < N / 2 ? p : q;
         const int j = 2 * (i % (N / 2));
         const float u = r.get(j), v = r.get(j + 1);
         r.set(j, u * t.c[i] - v * t.s[i]);
@@ -103,19 +115,23 @@ struct Pairs {
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float u = a.get(i), v = b.get(i);
-        a.set(i, u * t.c[i] - v * t.s[i]);
-        b.set(i, v * t.c[i] + u * t.s[i]);
+        const float u = p.get(i), v = q.get(i);
+        p.set(i, u * t.c[i] - v * t.s[i]);
+        q.set(i, v * t.c[i] + u * t.s[i]);
       }
     }
+    if (turned) {
+      a = p;
+      b = q;
+    }
   }
-  __device__ __forceinline__ void store(T* y, int p0, int half) const {
-    a.store(y + first(p0));
-    b.store(y + second(p0, half));
+  __device__ __forceinline__ void store(T* y) const {
+    a.store(y + a_at);
+    if (second) b.store(y + b_at);
   }
-  __device__ __forceinline__ void store_past(T* y, int p0, int half) const {
-    a.store_past(y + first(p0));
-    b.store_past(y + second(p0, half));
+  __device__ __forceinline__ void store_past(T* y) const {
+    a.store_past(y + a_at);
+    if (second) b.store_past(y + b_at);
   }
 };
 

@@ -21,35 +21,29 @@ __device__ __forceinline__ int64_t position(const RotaryArgs& a, int b, int m) {
   return (int64_t)a.pos[b] + a.pos0 + m;
 }
 
-// One thread per (token, run of N pairs or of 8 copied features) and chunk of
-// heads (blockIdx.y).
+// One thread per (token, part of its rows) and chunk of heads (blockIdx.y).
 template <typename T, int N, bool Interleaved>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int units, int heads_per) {
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int parts, int heads_per) {
   const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t tok = idx / units;
+  const int64_t tok = idx / parts;
   if (tok >= (int64_t)a.B * a.M) return;
-  const int u = (int)(idx - tok * units);
   const int b = (int)(tok / a.M), m = (int)(tok - (int64_t)b * a.M);
   const int h0 = blockIdx.y * heads_per, h1 = min(a.H, h0 + heads_per);
   const T* x = static_cast<const T*>(a.x) + b * a.xb + m * a.xm;
   T* y = static_cast<T*>(a.y) + b * a.yb + m * a.ym;
-  const int half = a.rot / 2, turned = half / N;
-  if (u < turned) {
-    Pairs<T, N, Interleaved> p;
-    p.load(x + h0 * a.xh, u * N, half);  // on its way while the angle is formed
+  Part<T, N, Interleaved> p((int)(idx - tok * parts), a.rot, a.d);
+  p.load(x + h0 * a.xh);  // on its way while the angle is formed
+  Turn<N> t;
+  if (p.turned) {
     double freq[N];
-    load_freq(freq, a.freq + u * N);
-    Turn<N> t;
+    p.load_freq(freq, a.freq);
     t.at((double)position(a, b, m), freq, a.magnitude, a.sign);
-    for (int h = h0;;) {
-      p.turn(t);
-      p.store(y + h * a.yh, u * N, half);
-      if (++h >= h1) break;
-      p.load(x + h * a.xh, u * N, half);
-    }
-  } else {
-    const int f = a.rot + 8 * (u - turned);
-    for (int h = h0; h < h1; ++h) Run<T, 8>::load(x + h * a.xh + f).store(y + h * a.yh + f);
+  }
+  for (int h = h0;;) {
+    p.turn(t);
+    p.store(y + h * a.yh);
+    if (++h >= h1) break;
+    p.load(x + h * a.xh);
   }
 }
 
@@ -64,12 +58,12 @@ constexpr int kHeads = 4;
 
 template <typename T, int N, bool Interleaved>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
-  const int units = a.rot / 2 / N + (a.x == a.y ? 0 : (a.d - a.rot) / 8);
-  const int64_t runs = (int64_t)a.B * a.M * units;
+  const int parts = Part<T, N, Interleaved>::count(a.rot, a.x == a.y ? 0 : a.d - a.rot);
+  const int64_t runs = (int64_t)a.B * a.M * parts;
   const int heads_per = runs * a.H < kMany ? 1 : kHeads;
   hipLaunchKernelGGL((rotary_kernel<T, N, Interleaved>),
                      dim3((unsigned)((runs + kThreads - 1) / kThreads), (a.H + heads_per - 1) / heads_per), dim3(kThreads), 0,
-                     stream, a, units, heads_per);
+                     stream, a, parts, heads_per);
   return hipGetLastError();
 }
 
