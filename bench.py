@@ -714,14 +714,19 @@ def cpu_baseline_prefill_2d(wl, r_k, r_v, ck, cv, loops, torch, budget_s=15.0):
 # ---------------------------------------------------------------------------
 
 PAPER_ABSORBED_SPEEDUP = {32768: 1.22, 131072: 2.17, 262144: 2.30}  # tab:absorbed_latency, its own GPU
+PAPER_TEACHER_SPEED = {32768: 0.56, 131072: 0.99, 262144: 1.05}  # of the teacher's decode, same table
 
 
 def run_absorbed_latency(args, torch, lla, W):
     """One layer's loop-l decode call of each kind, per context, timed with HIP
-    events around each call and interleaved (A, B, A, B, ...): the absorbed
-    call is the query rotation plus lla_decode_attn_rope, the other
-    lla_decode_attn_fullrope.  Ouro-1.4B geometry at the 4x tier (96, 160),
-    d_rope 64 (one rotary key per token shared by the heads)."""
+    events around each call and interleaved (A, B, C, A, ...): the absorbed
+    call is the query rotation plus lla_decode_attn_rope, the second
+    lla_decode_attn_fullrope, the third the teacher's own attention over a paged
+    K/V cache (query rotation plus lla_kv_decode_attn).  Ouro-1.4B geometry at
+    the 4x tier (96, 160), d_rope 64 (one rotary key per token shared by the
+    heads)."""
+    from paper_2607_15456_amd import kv
+
     B, H, d, r_k, r_v, dr = args.batch, 16, 128, 96, 160, 64
     wl = W.Workload("absorbed_latency", 1, H, d, 4, B, 0, ((r_k, r_v),), torch.bfloat16)
     dev = torch.device("cuda:0")
@@ -747,10 +752,25 @@ def run_absorbed_latency(args, torch, lla, W):
         def fullrope():
             lla.decode_attn_fullrope(q, ck, cv, uk, uv, n_ctx=N, out=out, workspace=ws)
 
-        ta, tf = KernelTimer(torch, stream), KernelTimer(torch, stream)
+        # the teacher's cache of one loop: whole keys and values of every token
+        P = N // 64
+        tk = W.normal((B * P, H, 64, d), (wl.name, "K", N), 1.0, wl.dtype, dev)
+        tv = W.normal((B * P, H, d, 64), (wl.name, "V", N), 1.0, wl.dtype, dev)
+        table = torch.arange(B * P, dtype=torch.int32, device=dev).view(B, P)
+        length = torch.full((B,), N, dtype=torch.int32, device=dev)
+        freq, _ = kv.rope_frequencies(d, device=dev)
+        tq, need = torch.empty_like(q), kv.decode_workspace_bytes(wl.dtype, B, H, H, d, N)
+        tws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+
+        def teacher():
+            kv.rope(q[:, None], freq, pos0=N - 1, out=tq[:, None])
+            kv.decode_attn(tq, tk, tv, table, length, n_ctx=N, out=out, workspace=tws)
+
+        ta, tf, tt = (KernelTimer(torch, stream) for _ in range(3))
         for _ in range(args.warmup):
             absorbed()
             fullrope()
+            teacher()
         for _ in range(args.steps):
             e = ta.start()
             absorbed()
@@ -758,18 +778,24 @@ def run_absorbed_latency(args, torch, lla, W):
             e = tf.start()
             fullrope()
             tf.stop(e)
+            e = tt.start()
+            teacher()
+            tt.stop(e)
         torch.cuda.synchronize()
-        a_ms, f_ms = ta.mean_ms(), tf.mean_ms()
+        a_ms, f_ms, t_ms = ta.mean_ms(), tf.mean_ms(), tt.mean_ms()
         ab = decode_bytes(B, H, d, N, r_k, r_v, d_rope=dr)
         fb = decode_bytes(B, H, d, N, r_k, r_v)
         rows.append({"context": N, "absorbed_rope_ms": round(a_ms, 5), "fullrope_ms": round(f_ms, 5),
                      "fullrope_over_absorbed": round(f_ms / a_ms, 3),
+                     "teacher_ms": round(t_ms, 5), "teacher_over_absorbed": round(t_ms / a_ms, 3),
+                     "teacher_gbs": round(2 * wl.dtype.itemsize * B * H * d * N / (t_ms * 1e-3) / 1e9, 1),
                      "absorbed_gbs": round(ab / (a_ms * 1e-3) / 1e9, 1),
                      "fullrope_gbs": round(fb / (f_ms * 1e-3) / 1e9, 1),
                      "splits": lla.decode_splits(torch.bfloat16, B, H, N, r_k, r_v, dr),
-                     "paper_speedup_other_gpu": PAPER_ABSORBED_SPEEDUP[N]})
+                     "paper_speedup_other_gpu": PAPER_ABSORBED_SPEEDUP[N],
+                     "paper_teacher_over_absorbed_other_gpu": PAPER_TEACHER_SPEED[N]})
         print(f"[bench] {json.dumps(rows[-1])}", file=sys.stderr, flush=True)
-        del ck, cv, rc, ws
+        del ck, cv, rc, ws, tk, tv
         torch.cuda.empty_cache()
     last = rows[-1]
     return {
