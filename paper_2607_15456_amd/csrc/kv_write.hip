@@ -80,8 +80,10 @@ __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
 // one angle for 2, 4 or 16 heads takes 1, 5, 40 us more, plain stores 2.
 template <typename T, int N, bool Interleaved>
 __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int blocks) {
-  constexpr int V = Elem<T>::kPer16B, kCols = 128, kRow = kCols + V;
-  __shared__ __align__(16) T s_v[kPage * kRow];
+  constexpr int V = Elem<T>::kPer16B, kCols = 128;
+  // 16-byte chunk c of token t at chunk c ^ (t / V): runs of a column meet different banks
+  __shared__ __align__(16) T s_v[kPage * kCols];
+  auto at = [](int t, int f) { return t * kCols + (f / V ^ t / V) * V + f % V; };
   // heads side by side, as a token's rows are (52 -> 47 us against pages side by side)
   const int h = blockIdx.x % a.p.Hkv, wg = blockIdx.x / a.p.Hkv;
   const int b = wg / blocks, d = a.p.d, tid = threadIdx.x;
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
     if (f0) __syncthreads();
     for (int x = tid; x < count * chunks; x += kThreads) {
       const int i = x / chunks, f = x - i * chunks;
-      *reinterpret_cast<uint4*>(s_v + (t0 + i) * kRow + f * V) = ld16(v + i * a.vm + f * V);
+      *reinterpret_cast<uint4*>(s_v + at(t0 + i, f * V)) = ld16(v + i * a.vm + f * V);
     }
     __syncthreads();
     if (page < 0) return;
@@ -135,12 +137,12 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
         Run<T, V> r;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[(t + i) * kRow + f]);
-          else if (i % 2 == 0) r.w[i / 2] = s_v[(t + i) * kRow + f] | (uint32_t(s_v[(t + i + 1) * kRow + f]) << 16);
+          if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(s_v[at(t + i, f)]);
+          else if (i % 2 == 0) r.w[i / 2] = s_v[at(t + i, f)] | (uint32_t(s_v[at(t + i + 1, f)]) << 16);
         }
         r.store_past(vp + f * kPage + t);
       } else {
-        for (int i = max(t, t0); i < min(t + V, t1); ++i) vp[f * kPage + i] = s_v[i * kRow + f];
+        for (int i = max(t, t0); i < min(t + V, t1); ++i) vp[f * kPage + i] = s_v[at(i, f)];
       }
     }
   }
