@@ -103,8 +103,9 @@ lla_status lla_rope_frequencies(int d_rot, double base, int scaling, double fact
  *   freq    device double [d_rot/2] (lla_rope_frequencies)
  *   x_b, x_m, x_h and y_b, y_m, y_h  strides in elements of b, m and h, each a
  *           multiple of 16 bytes (a row's features are dense).  x may be read
- *           with stride 0; y may be x with the same strides (in place), and must
- *           not overlap x or itself otherwise.
+ *           with stride 0; y's strides must nest (each at least as wide as what the
+ *           smaller ones span); y may be x with the same strides (in place), and
+ *           must not overlap it otherwise.
  * Angles are formed and reduced in 64 bits, sine and cosine and the products in
  * 32, rounded once to dtype.
  * Requires B, M >= 1; 1 <= H <= 65535; d_head a multiple of 8 in [8, LLA_KV_MAX_ROW]; d_rot a

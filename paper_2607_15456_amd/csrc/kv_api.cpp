@@ -33,6 +33,23 @@ bool tables_ok(int n_seqs, int max_pages, int n_pages) {
 bool freq_ok(int rot, const double* f) {
   return rot ? f && (reinterpret_cast<uintptr_t>(f) & 7u) == 0 : f == nullptr;
 }
+// Whether rows of d elements at these strides (n of each) each have a place of
+// their own: every dimension steps over all that the narrower ones span.
+bool rows_apart(int d, int n0, int64_t s0, int n1, int64_t s1, int n2, int64_t s2) {
+  struct Dim {
+    int n;
+    int64_t s;
+  } dim[3] = {{n0, s0}, {n1, s1}, {n2, s2}};
+  std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.s < b.s; });
+  int64_t span = d;
+  for (const Dim& x : dim) {
+    if (x.n == 1) continue;
+    if (x.s < span) return false;
+    if (x.s > (std::numeric_limits<int64_t>::max() - span) / x.n) return false;
+    span += x.s * (x.n - 1);
+  }
+  return true;
+}
 lla_status hip_status(hipError_t e) { return e == hipSuccess ? LLA_OK : LLA_ERR_HIP; }
 
 bool decode_ok(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, int sink, int window) {
@@ -128,8 +145,7 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
   if (!ptr_ok(x) || !ptr_ok(y) || !opt_idx_ok(pos) || !freq_ok(d_rot, freq)) return LLA_ERR_INVALID_ARG;
   for (int64_t s : {x_b, x_m, x_h, y_b, y_m, y_h})
     if (!stride_ok(s, dtype)) return LLA_ERR_INVALID_ARG;
-  // rows of y must not share their place
-  if ((B > 1 && y_b < d_head) || (M > 1 && y_m < d_head) || (H > 1 && y_h < d_head)) return LLA_ERR_INVALID_ARG;
+  if (!rows_apart(d_head, B, y_b, M, y_m, H, y_h)) return LLA_ERR_INVALID_ARG;
   if (x == y && ((B > 1 && x_b != y_b) || (M > 1 && x_m != y_m) || (H > 1 && x_h != y_h)))
     return LLA_ERR_INVALID_ARG;
   lla::RotaryArgs a{};

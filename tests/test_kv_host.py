@@ -76,7 +76,7 @@ CALLS = {
         [("dtype", 2), ("B", 0), ("M", 0), ("H", 0), ("H", 1 << 30), ("H", 65536), ("d_head", 4), ("d_head", 132), ("d_head", 520),
          ("d_rot", 0), ("d_rot", 12), ("d_rot", 136), ("x", None), ("x", P + 8), ("x_b", -8), ("x_m", 4), ("x_h", 12),
          ("pos", P + 2), ("freq", None), ("freq", P + 4), ("magnitude", math.nan), ("y", None), ("y", P + 2),
-         ("y_b", 0), ("y_m", 64), ("y_h", 0), ("x_b", 1544)]),
+         ("y_b", 0), ("y_m", 64), ("y_h", 0), ("y_b", 1024), ("y_b", 128), ("y_m", 384), ("y_h", 256), ("x_b", 1544)]),
     "lla_kv_write": (
         dict(dtype=0, B=2, M=3, H_kv=4, d_head=64, d_rot=64, interleaved=1, k=P, k_b=768, k_m=256, v=P, v_b=768, v_m=256,
              freq=P, magnitude=1.0, n_seqs=2, max_pages=8, n_pages=16, table=P, rows=None, start=P, n_new=None, k_pages=P,
