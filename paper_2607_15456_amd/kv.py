@@ -87,7 +87,7 @@ def _call(name, dev, *args):
 
 
 def _ints(t, name, shape, dev):
-    if t.dtype is not torch.int32 or t.shape != shape or t.device != dev or not (t.is_cuda and t.is_contiguous()):
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != dev or not t.is_contiguous() or not t.is_cuda:
         _need(t, name, torch.int32, dev)
         raise ValueError(f"{name} must have shape {list(shape)}")
 
@@ -95,13 +95,16 @@ def _ints(t, name, shape, dev):
 def _rows_of(t, name, dev, dtype):
     """Strides of t [B, M, heads, width] whose rows are dense (of a dimension of
     one entry, which torch leaves as it happens to be, 0)."""
-    if not t.is_cuda or t.device != dev:
+    if t.device != dev or not t.is_cuda:
         raise ValueError(f"{name} must be a tensor on {dev}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
-        raise ValueError(f"{name} must be [B, M, heads, width] with dense rows")
-    return [s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape)]
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, M, heads, width]")
+    (B, M, H, d), (b, m, h, one) = t.shape, t.stride()
+    if one != 1 and d != 1:
+        raise ValueError(f"{name} must have dense rows")
+    return b if B > 1 else 0, m if M > 1 else 0, h if H > 1 else 0
 
 
 # ---------------------------------------------------------------------------
@@ -122,10 +125,12 @@ def rope_frequencies(d_rot: int, *, base: float = 10000.0, scaling: str = "none"
 
 
 def _freq(freq, width, dev):
-    _need(freq, "freq", torch.float64, dev)
-    if freq.dim() != 1 or 2 * freq.numel() > width:
+    """Features that freq turns."""
+    rot = 2 * freq.numel()
+    if freq.dtype is not torch.float64 or freq.device != dev or freq.dim() != 1 or rot > width or not freq.is_contiguous():
+        _need(freq, "freq", torch.float64, dev)
         raise ValueError("freq must be [d_rot / 2] with d_rot at most the rows' width")
-    return 2 * freq.numel()
+    return rot
 
 
 def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitude: float = 1.0,
@@ -135,19 +140,21 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
     first 2 * len(freq) features turn in pairs, half-split or ``interleaved``, and
     are multiplied by ``magnitude``; the rest is copied.  ``transpose`` takes the
     gradient of the result to the gradient of x.  ``out`` may be x (in place)."""
-    dev = x.device
-    xs = _rows_of(x, "x", dev, x.dtype)
-    B, M, H, d = x.shape
-    rot = _freq(freq, d, dev)
+    dev, dtype = x.device, x.dtype
+    xs = _rows_of(x, "x", dev, dtype)
+    shape = x.shape
+    B, M, H, d = shape
+    rot, at, per_token = _freq(freq, d, dev), None, 0
     if pos is not None:
-        _ints(pos, "pos", (B, M) if pos.dim() == 2 else (B,), dev)
+        per_token = int(pos.dim() == 2)
+        _ints(pos, "pos", (B, M) if per_token else (B,), dev)
+        at = pos.data_ptr()
     if out is None:
-        out = torch.empty((B, M, H, d), dtype=x.dtype, device=dev)
-    elif out.shape != x.shape:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    elif out.shape != shape:
         raise ValueError("out must have x's shape")
-    ys = _rows_of(out, "out", dev, x.dtype)
-    _call("lla_rope_positions", dev, _dt(x), B, M, H, d, rot, int(interleaved), int(transpose), _ptr(x), *xs, _ptr(pos),
-          int(pos is not None and pos.dim() == 2), pos0, _ptr(freq), float(magnitude), _ptr(out), *ys)
+    _call("lla_rope_positions", dev, _dt(x), B, M, H, d, rot, int(interleaved), int(transpose), x.data_ptr(), *xs, at,
+          per_token, pos0, freq.data_ptr(), magnitude, out.data_ptr(), *_rows_of(out, "out", dev, dtype))
     return out
 
 
@@ -202,8 +209,10 @@ def _pools(k_pages, v_pages, layered=False):
     lead, (P, H, page, d) = shape[:-4], shape[-4:]
     if page != PAGE or v_pages.shape != (*lead, P, H, d, PAGE):
         raise ValueError("k_pages must be [n_pages, H_kv, 64, d] and v_pages [n_pages, H_kv, d, 64]")
-    _need(k_pages, "k_pages", None, None)
-    _need(v_pages, "v_pages", k_pages.dtype, k_pages.device)
+    if (not k_pages.is_cuda or v_pages.dtype is not k_pages.dtype or v_pages.device != k_pages.device
+            or not k_pages.is_contiguous() or not v_pages.is_contiguous()):
+        _need(k_pages, "k_pages")
+        _need(v_pages, "v_pages", k_pages.dtype, k_pages.device)
     return (lead[0] if lead else 1), P, H, d
 
 
@@ -352,6 +361,8 @@ def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, sc
         _need(lse, "lse", torch.float32, dev)
         if lse.shape != (B, H):
             raise ValueError("lse must be [B, H]")
+    if rows is None and B > n_seqs:
+        raise ValueError("more entries than sequences")
     if workspace is None:
         with torch.cuda.device(dev) if torch.cuda.current_device() != dev.index else nullcontext():
             need = decode_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx, sink, window)
