@@ -91,9 +91,13 @@ struct Part {
     b_at = a_at + (turned ? rot / 2 : copies(d - rot) * N);
     second = b_at < d;
   }
+  // the row's pair that is this part's i-th
+  __device__ __forceinline__ int pair(int i) const {
+    return !Interleaved ? a_at + i : i < N / 2 ? a_at / 2 + i : b_at / 2 + i - N / 2;
+  }
   __device__ __forceinline__ void load_freq(double (&f)[N], const double* p) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = p[!Interleaved ? a_at + i : i < N / 2 ? a_at / 2 + i : b_at / 2 + i - N / 2];
+    for (int i = 0; i < N; ++i) f[i] = p[pair(i)];
   }
 
   Run<T, N> a, b;

@@ -796,3 +796,19 @@ def test_free_of_more_entries_than_a_thread_holds():
     t.free_rows(everything)
     same_tables(pages, t)
     assert int(pages.free[0]) == 25000
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,M,H,d,rot", [(1, 5, 300, 16, 8), (1, 33, 1, 512, 8), (70, 1, 3, 32, 16), (2, 100, 7, 40, 32),
+                                         (1, 17, 2, 8, 8), (3, 40, 33, 256, 256)])
+def test_rope_many_heads_or_tokens(dtype, B, M, H, d, rot):
+    """Stretches that end inside a workgroup, in both orders of y's rows, more heads
+    or parts than a workgroup has threads for, and positions of one row a token."""
+    freq, _ = kv.rope_frequencies(rot)
+    x = normal((B, M, H, d), 14, dtype)
+    pos = np.broadcast_to((np.arange(M) + 9)[None, :, None], (B, M, H))
+    ref = O.kv_rope(f64(x), pos, f64(freq))
+    tol = rope_bound(f64(x), rot // 2, False, 1.0, ref, dtype)
+    near(kv.rope(x, freq, pos0=9), ref, tol, "heads inside")
+    out = torch.full((B, H, M, d), float("nan"), dtype=dtype, device=DEV).transpose(1, 2)
+    near(kv.rope(x.transpose(1, 2).contiguous().transpose(1, 2), freq, pos0=9, out=out), ref, tol, "tokens inside")
