@@ -87,6 +87,13 @@ __device__ __forceinline__ int entry_tokens(const KvDecodeArgs& a, int b, int& r
   return n < 0 || n > a.n_ctx ? -1 : n;
 }
 
+// Orders a wavefront's LDS accesses on either side: lanes read what others wrote.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // ---- one step of a wavefront ----
 //
 // A step's keys, then its values, go from memory to registers as whole
@@ -404,7 +411,9 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
     f32x4 sc[NT][kTiles];
     st.stage_k(lds, lane);
     if (more) st.load_k(keys(next), tok, lane);
+    wave_lds_order();
     st.scores(lds, c, g, sc);
+    wave_lds_order();
     const int t0 = sp.page(t / kSteps) * kPage + t % kSteps * Step::kTok;
     const bool whole = sp.whole(t0, Step::kTok);
     if (!whole) {
@@ -446,7 +455,9 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
     if (!whole) st.mask_values([&](int k) { return sp.seen(t0 + k); }, lane);
     st.stage_v(lds, lane);
     if (more) st.load_v(vals(next), tok, lane);
+    wave_lds_order();
     st.values(lds, c, g, sc, o);
+    wave_lds_order();
   }
 #pragma unroll
   for (int x = 0; x < NT; ++x) {
