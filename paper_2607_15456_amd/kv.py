@@ -66,22 +66,20 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-def _raw_stream(index):
-    return torch.cuda.current_stream(index).cuda_stream
-
-
-# the same without a stream object around it, where torch has it
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+# The current device's number and a device's current stream handle; torch's own
+# short ways to them where it has these (its public ones build objects).
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _call(name, dev, *args):
     """An entry point on dev's current stream, with dev the current device."""
     fn, index = getattr(_lib or lib(), name), dev.index
-    if torch.cuda.current_device() == index:
-        status = fn(*args, _raw_stream(index))
+    if _device() == index:
+        status = fn(*args, _stream(index))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, _raw_stream(index))
+            status = fn(*args, _stream(index))
     if status:
         _check(status)
 
@@ -150,11 +148,13 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
         _ints(pos, "pos", (B, M) if per_token else (B,), dev)
         at = pos.data_ptr()
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
-    elif out.shape != shape:
-        raise ValueError("out must have x's shape")
+        out, ys = torch.empty(shape, dtype=dtype, device=dev), (M * H * d, H * d, d)
+    else:
+        if out.shape != shape:
+            raise ValueError("out must have x's shape")
+        ys = _rows_of(out, "out", dev, dtype)
     _call("lla_rope_positions", dev, _dt(x), B, M, H, d, rot, int(interleaved), int(transpose), x.data_ptr(), *xs, at,
-          per_token, pos0, freq.data_ptr(), magnitude, out.data_ptr(), *_rows_of(out, "out", dev, dtype))
+          per_token, pos0, freq.data_ptr(), magnitude, out.data_ptr(), *ys)
     return out
 
 
@@ -203,17 +203,22 @@ def alloc_pages(n_pages: int, H_kv: int, d: int, dtype=torch.bfloat16, device="c
 
 def _pools(k_pages, v_pages, layered=False):
     """(layers, n_pages, H_kv, d) of a pair of pools."""
-    shape = k_pages.shape
-    if len(shape) not in ((4, 5) if layered else (4,)):
+    shape, layers = k_pages.shape, 1
+    if len(shape) == 4:
+        P, H, page, d = shape
+        other = (P, H, d, PAGE)
+    elif layered and len(shape) == 5:
+        layers, P, H, page, d = shape
+        other = (layers, P, H, d, PAGE)
+    else:
         raise ValueError("k_pages must be [n_pages, H_kv, 64, d]" + (", or with a layer dimension" if layered else ""))
-    lead, (P, H, page, d) = shape[:-4], shape[-4:]
-    if page != PAGE or v_pages.shape != (*lead, P, H, d, PAGE):
+    if page != PAGE or v_pages.shape != other:
         raise ValueError("k_pages must be [n_pages, H_kv, 64, d] and v_pages [n_pages, H_kv, d, 64]")
     if (not k_pages.is_cuda or v_pages.dtype is not k_pages.dtype or v_pages.device != k_pages.device
             or not k_pages.is_contiguous() or not v_pages.is_contiguous()):
         _need(k_pages, "k_pages")
         _need(v_pages, "v_pages", k_pages.dtype, k_pages.device)
-    return (lead[0] if lead else 1), P, H, d
+    return layers, P, H, d
 
 
 def _page_table(p, dev):
@@ -364,7 +369,7 @@ def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, sc
     if rows is None and B > n_seqs:
         raise ValueError("more entries than sequences")
     if workspace is None:
-        with torch.cuda.device(dev) if torch.cuda.current_device() != dev.index else nullcontext():
+        with torch.cuda.device(dev) if _device() != dev.index else nullcontext():
             need = decode_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx, sink, window)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     else:
