@@ -13,7 +13,7 @@
 // 5.0); two parts a thread 52, eight 74; non-temporal stores 48, but what reads
 // the result next would miss the caches.  The angles of the workgroup's tokens are
 // formed once, into LDS, while the rows are on their way.  One decode step's queries
-// (32 x 16 heads) 4 us, a launch and a chain of two reads.
+// (32 x 16 heads) 3 to 4 us, a launch and a chain of two reads.
 
 #include <algorithm>
 
