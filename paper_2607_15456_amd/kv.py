@@ -261,9 +261,10 @@ def free(pages: PageTable, rows, result):
 
 
 def copy_pages(a, b, pairs, result=None):
-    """Copy pages pairs[i, 0] -> pairs[i, 1] of the pools a and b (b may be None),
-    [n_pages, ...] or [layers, n_pages, H, 64, d]-like (five dimensions: layers
-    first); with the result of reserve, only the pairs that it gave."""
+    """Copy pages pairs[i, 0] -> pairs[i, 1] of the pools a and b (b may be None): the
+    first dimension numbers the pages, of five dimensions the second (layers
+    first); with the result of reserve, only the pairs that it gave.  A latent
+    cache is a pool too, seen as [B * H * n_max / 64, r, 64]."""
     dev, pools = a.device, []
     lead = a.shape[:2] if a.dim() == 5 else (1, a.shape[0])
     for t, name in ((a, "a"), (b, "b")):

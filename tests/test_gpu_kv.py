@@ -812,3 +812,18 @@ def test_rope_many_heads_or_tokens(dtype, B, M, H, d, rot):
     near(kv.rope(x, freq, pos0=9), ref, tol, "heads inside")
     out = torch.full((B, H, M, d), float("nan"), dtype=dtype, device=DEV).transpose(1, 2)
     near(kv.rope(x.transpose(1, 2).contiguous().transpose(1, 2), freq, pos0=9, out=out), ref, tol, "tokens inside")
+
+
+def test_latent_pages_are_copied_too():
+    """A sequence of the latent cache continues another: its pages copied, both
+    attend the same."""
+    H, P, d, r_k, r_v, n = 2, 5, 128, 18, 30, 180
+    c_k, c_v = (normal((2, H, P, r, 64), 80 + r, BF) for r in (r_k, r_v))
+    u_k, u_v = normal((H, d, r_k), 82, BF), normal((H, d, r_v), 83, BF)
+    q = normal((1, H, d), 84, BF).expand(2, H, d).contiguous()
+    before = c_k[1, :, 3:].clone()
+    pairs = [[h * P + p, (H + h) * P + p] for h in range(H) for p in range(3)]  # page (b, h, p) is b H P + h P + p
+    kv.copy_pages(c_k.view(2 * H * P, r_k, 64), c_v.view(2 * H * P, r_v, 64), ints(pairs))
+    out = lla.decode_attn(q, c_k, c_v, u_k, u_v, n_ctx=n)
+    assert torch.equal(out[0], out[1]) and torch.isfinite(out).all()
+    assert torch.equal(c_k[1, :, :3], c_k[0, :, :3]) and torch.equal(c_k[1, :, 3:], before)

@@ -170,6 +170,10 @@ def test_binding_refuses_before_the_library():
     with pytest.raises(ValueError):
         kv.write(q[None], q[None], k, v, ints.view(1, 1), ints)
     t = kv.new_page_table(2, 2, 3, device="cpu")
+    for change in (dict(table=t.table[0]), dict(table=t.table.long()), dict(table=t.table.t()), dict(length=t.length[:1]),
+                   dict(free=t.free[1:]), dict(refs=t.refs.view(1, 3)), dict(refs=t.refs[::2])):
+        with pytest.raises(ValueError):
+            kv.PageTable(**{**t._asdict(), **change})
     for call in (lambda: kv.free(t, ints, torch.zeros(4, dtype=torch.int32)),
                  lambda: kv.fork(t, ints, ints, torch.zeros(4, dtype=torch.int32)),
                  lambda: kv.copy_pages(k, v, torch.zeros(1, 2, dtype=torch.int32)),
