@@ -40,7 +40,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
 constexpr int kTile = 16;     // columns of a product: query heads
+// Wavefronts of a workgroup, at most: four, so that two workgroups fit a compute
+// unit; up to a width of 64, whose steps are small, eight where no second workgroup comes (24 x 17
+// pages, 8 key heads of 64: 16.0 -> 14.9 us; at 128 no gain, 29.2 -> 29.8 on 4 x 4096).
 constexpr int kWaves = 4;
+constexpr int most_waves(int d) { return d <= 64 ? 2 * kWaves : kWaves; }
 constexpr float kLazy = 8.f;  // log2 by which a step may exceed the running maximum
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -329,7 +333,7 @@ __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m
 // where steps are twice as large, so as many bytes are on their way, and with two
 // tiles, whose accumulators need the registers.
 template <template <int, int> class StepOf, int D, int NT>
-__global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
+__global__ __launch_bounds__(most_waves(D) * kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void decode_kernel(KvDecodeArgs a) {
   typedef StepOf<D, NT> Step;
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   // the wavefronts' steps, then what they join
   extern __shared__ __align__(16) char s_raw[];
   static_assert(kCols * (kRow + 2) * 4 <= 2 * kStepBytes);
-  const int W = blockDim.x / kWave;  // 1, 2 or 4
+  const int W = blockDim.x / kWave;  // 1, 2, 4 or 8
   float* const s_o = reinterpret_cast<float*>(s_raw);
   float(*const s_ml)[2][kCols] = reinterpret_cast<float(*)[2][kCols]>(s_o + W / 2 * kCols * kRow);
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
@@ -592,9 +596,10 @@ void launch_step(const KvDecodeArgs& a, hipStream_t stream) {
   typedef StepOf<D, 1> Step;
   const int group = a.H / a.p.Hkv;
   const dim3 grid(a.B * a.p.Hkv * a.slices, query_blocks(group, D));
-  // wavefronts: no more than a slice has steps
+  // wavefronts: no more than a slice has steps; of eight, each with a second one
   const int64_t steps = (int64_t)a.per * (kPage / Step::kTok);
-  const int W = steps >= kWaves ? kWaves : steps >= 2 ? 2 : 1;
+  const bool alone = (int64_t)grid.x * grid.y <= device_cu_count();
+  const int W = steps > most_waves(D) && alone ? most_waves(D) : steps >= kWaves ? kWaves : steps >= 2 ? 2 : 1;
   const size_t lds = (size_t)W * Step::kTok * D * Step::kBytes;
   if constexpr (D <= kTwoTiles) {
     if (query_tiles(group, D) == 2) {

@@ -827,3 +827,10 @@ def test_latent_pages_are_copied_too():
     out = lla.decode_attn(q, c_k, c_v, u_k, u_v, n_ctx=n)
     assert torch.equal(out[0], out[1]) and torch.isfinite(out).all()
     assert torch.equal(c_k[1, :, :3], c_k[0, :, :3]) and torch.equal(c_k[1, :, 3:], before)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,Hkv,H,d,n", [(3, 50, 50, 32, 900), (24, 8, 24, 64, 1088), (2, 60, 120, 64, 700), (130, 1, 20, 32, 650)])
+def test_decode_alone_on_a_compute_unit(dtype, B, Hkv, H, d, n):
+    """No more workgroups than compute units, narrow heads, over eight steps each."""
+    check_decode(Cache(dtype, [max(0, n - 37 * i % n) for i in range(B)], Hkv, d, seed=90), H)
