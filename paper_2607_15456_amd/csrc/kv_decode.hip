@@ -109,10 +109,11 @@ __device__ __forceinline__ void wave_lds_order() {
 // of a row are stored at chunk ^ swizzle(row), so that the 8 lanes that LDS
 // serves at a time meet different banks.
 
-// bf16: a page.
+// bf16: a page, half of one where two tiles' accumulators of a wide head leave no
+// registers for more (its values then come in 64-byte pieces).
 template <int D, int NT>
 struct StepBf16 {
-  static constexpr int kTok = 64, kTiles = kTok / 16, kBytes = 2;
+  static constexpr int kTok = NT * D > 384 ? 32 : 64, kTiles = kTok / 16, kBytes = 2;
   static constexpr int KS = D / 32, FT = D / 16, UU = kTok / 32;
   static constexpr int kLoads = kTok * D * 2 / 1024;  // of the keys, and of the values
   static constexpr int kKeyChunks = D / 8, kValChunks = kTok / 8;
@@ -128,7 +129,9 @@ struct StepBf16 {
     const int i = (row & 3) | ((row >> 1) & 4);
     return (row * kKeyChunks + (chunk ^ (kKeyChunks % 8 ? i >> 1 : i))) * 16;
   }
-  __device__ __forceinline__ static int val_at(int row, int chunk) { return (row * kValChunks + (chunk ^ (row & 7))) * 16; }
+  __device__ __forceinline__ static int val_at(int row, int chunk) {
+    return (row * kValChunks + (chunk ^ (kValChunks == 8 ? row & 7 : (row >> 1) & 3))) * 16;
+  }
   __device__ __forceinline__ void load_k(BufRsrc r, int tok, int lane) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) k[j] = buf_ld16(r, lane * 16, tok * D * 2 + j * 1024);
@@ -210,10 +213,10 @@ struct StepBf16 {
   }
 };
 
-// fp32: half a page.
+// fp32: half a page, or a quarter.
 template <int D, int NT>
 struct StepF32 {
-  static constexpr int kTok = 32, kTiles = kTok / 16, kBytes = 4;
+  static constexpr int kTok = NT * D > 384 ? 16 : 32, kTiles = kTok / 16, kBytes = 4;
   static constexpr int KS = D / 16, FT = D / 16;
   static constexpr int kLoads = kTok * D * 4 / 1024;
   static constexpr int kKeyChunks = D / 4, kValChunks = kTok / 4;
@@ -225,7 +228,9 @@ struct StepF32 {
       q[n][s] = in ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + 16 * s + 4 * g) : f32x4{0.f};
   }
   __device__ __forceinline__ static int key_at(int row, int chunk) { return (row * kKeyChunks + (chunk ^ (row & 7))) * 16; }
-  __device__ __forceinline__ static int val_at(int row, int chunk) { return (row * kValChunks + (chunk ^ (row & 7))) * 16; }
+  __device__ __forceinline__ static int val_at(int row, int chunk) {
+    return (row * kValChunks + (chunk ^ (kValChunks == 8 ? row & 7 : (row >> 1) & 3))) * 16;
+  }
   __device__ __forceinline__ void load_k(BufRsrc r, int tok, int lane) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) k[j] = __builtin_bit_cast(f32x4, buf_ld16(r, lane * 16, tok * D * 4 + j * 1024));
@@ -329,6 +334,9 @@ __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m
   }
 }
 
+// Bytes that a wavefront leaves for its neighbour to join.
+constexpr size_t join_bytes(int d, int tiles) { return (size_t)tiles * kTile * (d + 6) * sizeof(float); }
+
 // NT tiles of 16 query heads.  Two wavefronts a SIMD; one above a width of 128,
 // where steps are twice as large, so as many bytes are on their way, and with two
 // tiles, whose accumulators need the registers.
@@ -340,7 +348,6 @@ __global__ __launch_bounds__(most_waves(D) * kWave, D <= 128 && NT * D <= 128 ? 
   constexpr int kRow = D + 4, kCols = NT * kTile;
   // the wavefronts' steps, then what they join
   extern __shared__ __align__(16) char s_raw[];
-  static_assert(kCols * (kRow + 2) * 4 <= 2 * kStepBytes);
   const int W = blockDim.x / kWave;  // 1, 2, 4 or 8
   float* const s_o = reinterpret_cast<float*>(s_raw);
   float(*const s_ml)[2][kCols] = reinterpret_cast<float(*)[2][kCols]>(s_o + W / 2 * kCols * kRow);
@@ -581,33 +588,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
   }
 }
 
-// Tiles of a workgroup: two from 17 query heads a group on, where their registers
-// suffice (16 x 4096 tokens, 8 key heads, bf16, one tile / two: 20 heads a group 94
-// / 64 us, 64 131 / 115).
-constexpr int kTwoTiles = 192;  // widest head of two tiles
-int query_tiles(int group, int d) { return group > kTile && d <= kTwoTiles ? 2 : 1; }
-int query_blocks(int group, int d) {
-  const int cols = kTile * query_tiles(group, d);
-  return (group + cols - 1) / cols;
-}
+// Tiles of a workgroup: two from 17 query heads a group on (16 x 4096 tokens, 8 key
+// heads, bf16, one tile / two: 20 heads a group 94 / 64 us, 64 131 / 115; width 256,
+// 20 heads 184 / 131).
+int query_tiles(int group) { return group > kTile ? 2 : 1; }
+int query_blocks(int group) { return (group + kTile * query_tiles(group) - 1) / (kTile * query_tiles(group)); }
 
-template <template <int, int> class StepOf, int D>
-void launch_step(const KvDecodeArgs& a, hipStream_t stream) {
-  typedef StepOf<D, 1> Step;
-  const int group = a.H / a.p.Hkv;
-  const dim3 grid(a.B * a.p.Hkv * a.slices, query_blocks(group, D));
+template <template <int, int> class StepOf, int D, int NT>
+void launch_tiles(const KvDecodeArgs& a, hipStream_t stream) {
+  typedef StepOf<D, NT> Step;
+  const dim3 grid(a.B * a.p.Hkv * a.slices, query_blocks(a.H / a.p.Hkv));
   // wavefronts: no more than a slice has steps; of eight, each with a second one
   const int64_t steps = (int64_t)a.per * (kPage / Step::kTok);
   const bool alone = (int64_t)grid.x * grid.y <= device_cu_count();
   const int W = steps > most_waves(D) && alone ? most_waves(D) : steps >= kWaves ? kWaves : steps >= 2 ? 2 : 1;
-  const size_t lds = (size_t)W * Step::kTok * D * Step::kBytes;
-  if constexpr (D <= kTwoTiles) {
-    if (query_tiles(group, D) == 2) {
-      hipLaunchKernelGGL((decode_kernel<StepOf, D, 2>), grid, dim3(W * kWave), lds, stream, a);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((decode_kernel<StepOf, D, 1>), grid, dim3(W * kWave), lds, stream, a);
+  const size_t lds = std::max<size_t>((size_t)W * Step::kTok * D * Step::kBytes, W / 2 * join_bytes(D, NT));
+  hipLaunchKernelGGL((decode_kernel<StepOf, D, NT>), grid, dim3(W * kWave), lds, stream, a);
+}
+template <template <int, int> class StepOf, int D>
+void launch_step(const KvDecodeArgs& a, hipStream_t stream) {
+  if (query_tiles(a.H / a.p.Hkv) == 2) launch_tiles<StepOf, D, 2>(a, stream);
+  else launch_tiles<StepOf, D, 1>(a, stream);
 }
 
 template <int D>
@@ -638,7 +639,7 @@ size_t kv_decode_shape(KvDecodeArgs& a) {
   // most pages that an entry attends
   const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
   const int pages = a.window ? (int)std::min<int64_t>(all, budget) : all;
-  const int64_t units = (int64_t)a.B * a.p.Hkv * query_blocks(a.H / a.p.Hkv, a.p.d);
+  const int64_t units = (int64_t)a.B * a.p.Hkv * query_blocks(a.H / a.p.Hkv);
   const int64_t cus = device_cu_count();
   int64_t want = (2 * cus + units - 1) / units;
   if (pages < want * kLong) want = std::max<int64_t>(1, cus / units);

@@ -834,3 +834,13 @@ def test_latent_pages_are_copied_too():
 def test_decode_alone_on_a_compute_unit(dtype, B, Hkv, H, d, n):
     """No more workgroups than compute units, narrow heads, over eight steps each."""
     check_decode(Cache(dtype, [max(0, n - 37 * i % n) for i in range(B)], Hkv, d, seed=90), H)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [96, 160, 192, 224, 256])
+def test_decode_wide_heads_in_two_tiles(dtype, d):
+    """More than 16 query heads a key head at every size of a step, one to several
+    wavefronts, in one slice and in several, with a budget that cuts into pages."""
+    check_decode(Cache(dtype, [1, 77, 0, 230], 1, d, seed=91), 20)
+    check_decode(Cache(dtype, [3001, 64], 2, d, seed=92), 66)
+    check_decode(Cache(dtype, [1500], 1, d, seed=93), 17, sink=5, window=333)
