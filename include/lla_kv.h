@@ -109,7 +109,7 @@ lla_status lla_rope_frequencies(int d_rot, double base, int scaling, double fact
  * Angles are formed and reduced in 64 bits, sine and cosine and the products in
  * 32, rounded once to dtype.
  * Requires B, M >= 1; 1 <= H <= 65535; d_head a multiple of 8 in [8, LLA_KV_MAX_ROW]; d_rot a
- * multiple of 8 in [8, min(d_head, LLA_MAX_ROPE)]; B*M*H <= 2^31 - 1; magnitude finite.
+ * multiple of 8 in [8, min(d_head, LLA_MAX_ROPE)]; B*M < 2^24, B*M*H < 2^31; magnitude finite.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_rot, int interleaved,
@@ -136,7 +136,8 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
  * n_new[b] counts as at most M and no less than 0.  Slots of other positions
  * are not touched.  Pages written must have one holder, and a position must
  * occur once in a call.
- * Requires B, M >= 1; 1 <= H_kv <= 65535; B*M*H_kv <= 2^31 - 1; d_rot as above, or 0.
+ * Requires B, M >= 1; 1 <= H_kv <= 65535; B*M*H_kv < 2^31, B*(M/64 + 2)*H_kv < 2^24 (whole
+ * pages); d_rot as above, or 0.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot, int interleaved,
@@ -173,7 +174,7 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  * Products of bf16 are exact; the softmax weights enter their product with the
  * values as a sum of two bf16 (about 2^-17 relative).
  * Requires B >= 1, H a multiple of H_kv >= 1, H / H_kv <= 65535, sink >= 0, window >= 0,
- * sink = 0 without a window, B*H <= 2^24.
+ * sink = 0 without a window, B*H < 2^24.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
  */
 lla_status lla_kv_decode_attn(int dtype, int out_dtype, int B, int H, int H_kv, int d_head,
@@ -234,7 +235,7 @@ lla_status lla_pages_free(int n, const int32_t* rows, int n_seqs, int max_pages,
  * lla_pages_reserve.  A pair with a page out of range is passed over.  No page may be
  * written twice, or be read and written, by one call.
  * Requires 1 <= layers <= 65535, 1 <= n_pairs <= 2^20, page sizes of at most 2^40 bytes,
- * n_pairs times the pages' pieces of 8 KB at most 2^31 - 1.
+ * n_pairs times the pages' pieces of 8 KB below 2^24.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, void* b, int64_t b_bytes,
@@ -251,7 +252,7 @@ lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, voi
  * outside [0, 64*max_pages) or on a page out of range gives NaN; tokens of a
  * destination row or page out of range are not written.
  * Requires 1 <= layers <= 32767, 1 <= H_kv <= 65535, B >= 1, 1 <= max_keep <= 64*max_pages,
- * B*max_keep <= 2^30.
+ * B*max_keep <= 2^30, B times the pages of max_keep tokens below 2^24.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
  */
 lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, int d_head, int n_seqs,

@@ -16,6 +16,7 @@ namespace {
 constexpr int kMaxPages = 1 << 20;   // pages of one sequence
 constexpr int kMaxPool = 1 << 30;    // pages of a pool
 constexpr int kMaxGridY = 65535;     // workgroups along a grid's second and third dimension
+constexpr int kMaxGridX = (1 << 24) - 1;  // and its first: below 2^32 threads, 256 a workgroup
 constexpr double kLog2e = 1.4426950408889634;
 
 bool ptr_ok(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -54,8 +55,8 @@ lla_status hip_status(hipError_t e) { return e == hipSuccess ? LLA_OK : LLA_ERR_
 
 bool decode_ok(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, int sink, int window) {
   return dtype_ok(dtype) && B >= 1 && H >= 1 && H_kv >= 1 && H % H_kv == 0 && H / H_kv <= kMaxGridY &&
-         (int64_t)B * H <= (1 << 24) &&
-         head_ok(d_head) && n_ctx >= 1 && n_ctx <= kMaxPages * LLA_PAGE_TOKENS && sink >= 0 && window >= 0 &&
+         (int64_t)B * H <= kMaxGridX && head_ok(d_head) && n_ctx >= 1 &&
+         n_ctx <= kMaxPages * LLA_PAGE_TOKENS && sink >= 0 && window >= 0 &&
          (window > 0 || sink == 0);
 }
 
@@ -141,7 +142,8 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
   if (!dtype_ok(dtype) || B < 1 || M < 1 || H < 1 || d_head < 8 || d_head > LLA_KV_MAX_ROW || d_head % 8 ||
       !rot_ok(d_rot, d_head) || !std::isfinite(magnitude))
     return LLA_ERR_INVALID_ARG;
-  if (H > kMaxGridY || (int64_t)B * M > std::numeric_limits<int>::max() / H) return LLA_ERR_INVALID_ARG;
+  if (H > kMaxGridY || (int64_t)B * M > std::min(kMaxGridX, std::numeric_limits<int>::max() / H))
+    return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(x) || !ptr_ok(y) || !opt_idx_ok(pos) || !freq_ok(d_rot, freq)) return LLA_ERR_INVALID_ARG;
   for (int64_t s : {x_b, x_m, x_h, y_b, y_m, y_h})
     if (!stride_ok(s, dtype)) return LLA_ERR_INVALID_ARG;
@@ -179,7 +181,7 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream) {
   if (!dtype_ok(dtype) || B < 1 || M < 1 || H_kv < 1 || H_kv > kMaxGridY || (int64_t)B * M > std::numeric_limits<int>::max() / H_kv ||
-      !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) || !std::isfinite(magnitude) ||
+      (int64_t)B * (M / LLA_PAGE_TOKENS + 2) > kMaxGridX / H_kv || !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) || !std::isfinite(magnitude) ||
       !tables_ok(n_seqs, max_pages, n_pages))
     return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(k) || !ptr_ok(v) || !freq_ok(d_rot, freq) || !idx_ok(table) || !opt_idx_ok(rows) || !idx_ok(start) ||
@@ -284,7 +286,7 @@ lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, voi
       (b == nullptr) != (b_bytes == 0))
     return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(a) || (b && !ptr_ok(b)) || !idx_ok(pairs) || !opt_idx_ok(count)) return LLA_ERR_INVALID_ARG;
-  if (lla::page_copy_pieces(a_bytes, b_bytes) > std::numeric_limits<int>::max() / n_pairs) return LLA_ERR_INVALID_ARG;
+  if (lla::page_copy_pieces(a_bytes, b_bytes) > kMaxGridX / n_pairs) return LLA_ERR_INVALID_ARG;
   lla::PageCopyArgs c{};
   c.layers = layers;
   c.n_pages = n_pages;
@@ -305,7 +307,8 @@ lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, i
   if (!dtype_ok(dtype) || B < 1 || max_keep < 1 || layers < 1 || layers > kMaxGridY / 2 || H_kv < 1 ||
       H_kv > kMaxGridY ||
       !head_ok(d_head) || !tables_ok(n_seqs, max_pages, n_pages) ||
-      max_keep > (int64_t)max_pages * LLA_PAGE_TOKENS || (int64_t)B * max_keep > (1 << 30))
+      max_keep > (int64_t)max_pages * LLA_PAGE_TOKENS || (int64_t)B * max_keep > (1 << 30) ||
+      (max_keep + LLA_PAGE_TOKENS - 1) / LLA_PAGE_TOKENS > kMaxGridX / B)
     return LLA_ERR_INVALID_ARG;
   if (!idx_ok(table) || !idx_ok(src) || !idx_ok(dst) || !idx_ok(keep) || !opt_idx_ok(n_keep) || !ptr_ok(k_pages) ||
       !ptr_ok(v_pages))

@@ -180,3 +180,16 @@ def test_binding_refuses_before_the_library():
                  lambda: kv.gather(k, v, t.table, ints, ints, ints.view(1, 1))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("name,changes", [
+    ("lla_rope_positions", dict(B=1, M=1 << 24, H=1, d_head=8, d_rot=8, x_m=8, y_m=8)),
+    ("lla_kv_write", dict(B=1 << 21, M=4, H_kv=4)),
+    ("lla_kv_write", dict(B=1 << 22, M=1, H_kv=4)),
+    ("lla_kv_decode_attn", dict(B=1 << 21, H=8, H_kv=8)),
+    ("lla_pages_copy", dict(n_pairs=1 << 20, a_bytes=1 << 16, b_bytes=1 << 16)),
+    ("lla_kv_gather", dict(B=1 << 24, max_keep=1)),
+])
+def test_refuses_more_threads_than_a_launch_takes(name, changes):
+    """256 threads a workgroup: 2^24 workgroups along a dimension are 2^32 threads."""
+    assert getattr(kv.lib(), name)(*{**CALLS[name][0], **changes}.values()) == lla.LLA_ERR_INVALID_ARG
