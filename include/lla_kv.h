@@ -162,7 +162,7 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  *   rows    int32 [B], or NULL: entry b is sequence b
  *   n_ctx   upper bound of the lengths, in [1, 64*max_pages]: the split of the
  *           work over the device goes by it
- *   scale   finite, > 0 (usually 1/sqrt(d_head))
+ *   scale   > 0, scale * log2(e) finite in 32 bits (usually 1/sqrt(d_head))
  *   out     [B][H][d_head] of out_dtype
  *   lse     NULL, or float [B][H]: the natural logarithm of sum_n exp(s_n)
  *   workspace  device memory of ws_bytes >= lla_kv_decode_workspace_bytes(), no

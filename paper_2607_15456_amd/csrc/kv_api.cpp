@@ -225,7 +225,7 @@ lla_status lla_kv_decode_attn(int dtype, int out_dtype, int B, int H, int H_kv, 
                               void* workspace, size_t ws_bytes, void* stream) {
   if (!decode_ok(dtype, B, H, H_kv, d_head, n_ctx, sink, window) || !dtype_ok(out_dtype) ||
       !tables_ok(n_seqs, max_pages, n_pages) || n_ctx > (int64_t)max_pages * LLA_PAGE_TOKENS ||
-      !std::isfinite(scale) || !(scale > 0.f))
+      !std::isfinite((float)(scale * kLog2e)) || !(scale > 0.f))
     return LLA_ERR_INVALID_ARG;
   if (!idx_ok(table) || !idx_ok(length) || !opt_idx_ok(rows) || !ptr_ok(q) || !ptr_ok(k_pages) || !ptr_ok(v_pages) ||
       !ptr_ok(out) || !opt_idx_ok(lse))

@@ -274,7 +274,7 @@ def copy_pages(a, b, pairs, result=None):
         _need(t, name, None, dev)
         if (t.shape[:2] if t.dim() == 5 else (1, t.shape[0])) != lead:
             raise ValueError("a and b must have the same layers and pages")
-        pools += [_ptr(t), t.numel() // (lead[0] * lead[1]) * t.element_size()]
+        pools += [_ptr(t), t.numel() // max(lead[0] * lead[1], 1) * t.element_size()]
     _ints(pairs, "pairs", (pairs.shape[0], 2), dev)
     if result is not None:
         _ints(result, "result", (4,), dev)

@@ -844,3 +844,9 @@ def test_decode_wide_heads_in_two_tiles(dtype, d):
     check_decode(Cache(dtype, [1, 77, 0, 230], 1, d, seed=91), 20)
     check_decode(Cache(dtype, [3001, 64], 2, d, seed=92), 66)
     check_decode(Cache(dtype, [1500], 1, d, seed=93), 17, sink=5, window=333)
+
+
+def test_copy_of_a_pool_without_pages_is_refused():
+    with pytest.raises(lla.LLAError) as e:
+        kv.copy_pages(torch.empty((0, 2, 64, 32), device=DEV), None, ints([[0, 0]]))
+    assert e.value.status == lla.LLA_ERR_INVALID_ARG

@@ -193,3 +193,9 @@ def test_binding_refuses_before_the_library():
 def test_refuses_more_threads_than_a_launch_takes(name, changes):
     """256 threads a workgroup: 2^24 workgroups along a dimension are 2^32 threads."""
     assert getattr(kv.lib(), name)(*{**CALLS[name][0], **changes}.values()) == lla.LLA_ERR_INVALID_ARG
+
+
+def test_scale_that_overflows_in_base_two_is_refused():
+    """Scores are taken in powers of two: an infinite factor would make NaN of zeros."""
+    good = CALLS["lla_kv_decode_attn"][0]
+    assert kv.lib().lla_kv_decode_attn(*{**good, "scale": 3e38}.values()) == lla.LLA_ERR_INVALID_ARG
