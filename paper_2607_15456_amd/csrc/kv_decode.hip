@@ -631,10 +631,14 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
 //   1 x 32,768, 2 key heads            299 / 15.6 (4 pages; 2 pages 17.6, one 25)
 //   4 x 4096, 16 key heads             49.6 / 29.6 (16 pages; 8 pages 29.1)
 //   24 of 17 pages, 8 key heads of 64  16.2 / 18.6
+// and of 128 KB of keys and values or less, 8 wavefronts to a workgroup from 9 steps on:
+//   512 tokens, 8 key heads of 64, bf16 1 x 7.5 / 7.6, 16 x 8.4 / 11.2, 320 tokens 6.9 / 7.5
+//   1 x 512, 700, 1024, 8 of 32, bf16  5.8, 6.9, 7.1 / 7.3, 8.0, 7.4
+//   256 tokens, 8 of 64, fp32          4 x 8.2 / 9.0
 //   20 x 1024 .. 4096, 16 key heads    89 / 80;  12 x 2250 .. 9000, 8 key heads 100 / 59
 //   40 x 4096, 16 key heads (640 workgroups) 209 / 208 .. 214
 size_t kv_decode_shape(KvDecodeArgs& a) {
-  constexpr int kLong = 16;
+  constexpr int kLong = 16, kAlone = 128 << 10;
   const int all = (a.n_ctx + kPage - 1) / kPage;
   // most pages that an entry attends
   const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
@@ -643,7 +647,9 @@ size_t kv_decode_shape(KvDecodeArgs& a) {
   const int64_t cus = device_cu_count();
   int64_t want = (2 * cus + units - 1) / units;
   if (pages < want * kLong) want = std::max<int64_t>(1, cus / units);
-  if (pages <= (a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2)) want = 1;  // a step a wavefront
+  // a step a wavefront; of narrow heads, what eight wavefronts read in two steps or less
+  const int waves = a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2, bytes = a.p.d * (a.p.dtype == LLA_BF16 ? 256 : 512);
+  if (pages <= waves || (most_waves(a.p.d) > kWaves && units <= cus && pages <= kAlone / bytes)) want = 1;
   a.per = (int)((pages + want - 1) / want);
   a.per = std::max(a.per, (pages + kMaxSlices - 1) / kMaxSlices);
   a.slices = (pages + a.per - 1) / a.per;

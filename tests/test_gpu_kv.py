@@ -850,3 +850,13 @@ def test_copy_of_a_pool_without_pages_is_refused():
     with pytest.raises(lla.LLAError) as e:
         kv.copy_pages(torch.empty((0, 2, 64, 32), device=DEV), None, ints([[0, 0]]))
     assert e.value.status == lla.LLA_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 32), (BF, 64), (F32, 32), (F32, 64)])
+@pytest.mark.parametrize("B,Hkv", [(3, 2), (2, 200)])
+def test_decode_narrow_heads_around_128_kb(dtype, d, B, Hkv):
+    """Contexts of up to 128 KB of keys and values a head, which stay with one
+    workgroup where each has a compute unit, and of a page more."""
+    most = (128 << 10) // (2 * d * (2 if dtype == BF else 4))
+    for n in (most // 2 + 7, most, most + 1):
+        check_decode(Cache(dtype, [n] + [max(0, n - 65 * i) for i in range(1, B)], Hkv, d, seed=94), Hkv)
