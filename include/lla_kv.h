@@ -172,7 +172,7 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  * lse of -inf; another row outside [0, n_seqs), an N outside [0, n_ctx] or a page outside
  * [0, n_pages) among those read gets NaN.  Slots that are not attended may hold anything.
  * Products of bf16 are exact; the softmax weights enter their product with the
- * values as a sum of two bf16 (about 2^-17 relative).
+ * values with their 24 bits, as a sum of three bf16.
  * Requires B >= 1, H a multiple of H_kv >= 1, H / H_kv <= 65535, sink >= 0, window >= 0,
  * sink = 0 without a window, B*H < 2^24.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.

@@ -1,0 +1,41 @@
+"""Calls of the paged K/V cache that its header and binding allow and that come up
+in use beside the plain ones: against the definitions in 64 bits (EPS = 2^-24)."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_15456_amd import kv
+from tests.helpers import f64, log
+from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def two_token_weights(dtype, B, H):
+    """Entries of two tokens: the first's score is 0 and its values 0, the second's
+    score is a product that 32 bits hold, its values 1.  Results are w / (1 + w)."""
+    c = Cache(dtype, [2] * B, 1, 64, seed=1)
+    q, b = torch.zeros((B, H, 64), dtype=dtype, device=DEV), normal((B,), 2, F32).abs().clamp(0.1, 2.0).to(dtype)
+    q[:, :, 0] = normal((B, H), 3, F32).abs().clamp(0.1, 2.0).to(dtype)
+    page = c.table[:, 0].long()
+    c.k[page, 0, :2] = 0
+    c.k[page, 0, 1, 0] = -b
+    c.v[page, 0, :, 0] = 0
+    c.v[page, 0, :, 1] = 1
+    return c, q, np.exp(-f64(q[:, :, 0]) * f64(b)[:, None])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_decode_weights_keep_32_bits(dtype):
+    """Scores of at most 4: off by 8 EPS (two roundings), so the weight by 10 with its
+    exponential; sum and product take 4 roundings, the sum's share of the weight's
+    error is half of it at most, the division 1: 20 EPS in all, held to 32 (2^-19).
+    A weight cut to two bf16 is off by up to 256."""
+    c, q, w = two_token_weights(dtype, 60, 40)
+    lse = torch.empty((60, 40), device=DEV)
+    out = f64(kv.decode_attn(q, c.k, c.v, c.table, c.length, n_ctx=2, scale=1.0, lse=lse))
+    off = np.abs(out / (w / (1 + w))[..., None] - 1) / EPS
+    log(f"  {off.max():.1f} EPS")
+    assert off.max() <= 32
+    assert np.max(np.abs(f64(lse) - np.log1p(w))) <= 32 * EPS
