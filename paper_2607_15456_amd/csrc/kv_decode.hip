@@ -325,6 +325,14 @@ __device__ __forceinline__ float* partial(const KvDecodeArgs& a, int64_t row, in
   return a.part + (row * a.slices + slice) * (a.p.d + 4);
 }
 
+// score * scale - base, the product rounded as the maximum's was: a fused one would
+// leave the maximum's rounding, which past 2^31 is more than exp2 has a result for.
+__device__ __forceinline__ float below(float score, float scale, float base) {
+#pragma clang fp contract(off)
+  const float x = score * scale;
+  return x - base;
+}
+
 // One (m, l, o[]) into another: o2 and l2 were weighed by 2^-m2.
 template <int FT>
 __device__ __forceinline__ void join(float& m, float& l, f32x4 (&o)[FT], float m2, float l2, const float* o2) {
@@ -465,7 +473,7 @@ __global__ __launch_bounds__(most_waves(D) * kWave, D <= 128 && NT * D <= 128 ? 
       for (int y = 0; y < kTiles; ++y)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          sc[x][y][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][y][i], a.qscale, -base));
+          sc[x][y][i] = __builtin_amdgcn_exp2f(below(sc[x][y][i], a.qscale, base));
           l[x] += sc[x][y][i];
         }
     }

@@ -39,3 +39,28 @@ def test_decode_weights_keep_32_bits(dtype):
     log(f"  {off.max():.1f} EPS")
     assert off.max() <= 32
     assert np.max(np.abs(f64(lse) - np.log1p(w))) <= 32 * EPS
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lengths", [[40], [3000, 100]])
+def test_decode_of_far_scores(dtype, lengths):
+    """Finite scores of up to 200 * 2^40, of which the greatest stands alone: its
+    values are the result, and it is the lse."""
+    c = Cache(dtype, lengths, 1, 64, seed=2)
+    q = torch.zeros((len(lengths), 2, 64), dtype=dtype, device=DEV)
+    q[:, 0, 0], q[:, 1, 0] = 2.0 ** 20, 2.0 ** 15
+    want = []
+    for i, n in enumerate(lengths):
+        t = torch.arange(n, device=DEV)
+        page = c.table[i].long()[t // 64]
+        level = (t * 37 % 101 + 1).float()
+        level[n // 3] = 200
+        c.k[page, 0, t % 64] = 0
+        c.k[page, 0, t % 64, 0] = (level * 2.0 ** 20).to(dtype)
+        want.append(f64(c.v[page[n // 3], 0, :, n // 3 % 64]))
+    lse = torch.empty((len(lengths), 2), device=DEV)
+    out = f64(kv.decode_attn(q, c.k, c.v, c.table, c.length, n_ctx=max(lengths), scale=1.0, lse=lse))
+    for h, top in ((0, 200 * 2.0 ** 40), (1, 200 * 2.0 ** 35)):
+        assert np.array_equal(out[:, h], np.stack(want)), h
+        # the factor log2(e), the score, the lse: a rounding each, and ln 2's
+        assert np.all(np.abs(f64(lse)[:, h] - top) <= 5 * EPS * top)
