@@ -163,7 +163,7 @@ lla_status lla_rope_positions(int dtype, int B, int M, int H, int d_head, int d_
   a.xm = x_m;
   a.xh = x_h;
   a.pos = pos;
-  a.pos_tokens = pos_tokens != 0;
+  a.pos_tokens = pos && pos_tokens;  // (without pos, token m is at pos0 + m)
   a.pos0 = pos0;
   a.freq = freq;
   a.magnitude = magnitude;

@@ -5,11 +5,30 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2607_15456_amd import kv
+from paper_2607_15456_amd import kv, lla
 from tests.helpers import f64, log
 from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, normal
 
 pytestmark = pytest.mark.gpu
+
+
+def rope_abi(x, freq, pos, pos_tokens, pos0):
+    """lla_rope_positions itself on a dense x."""
+    B, M, H, d = x.shape
+    y, strides = torch.empty_like(x), (M * H * d, H * d, d)
+    kv._call("lla_rope_positions", x.device, lla._dt(x), B, M, H, d, 2 * freq.numel(), 0, 0, x.data_ptr(), *strides,
+             None if pos is None else pos.data_ptr(), pos_tokens, pos0, freq.data_ptr(), 1.0, y.data_ptr(), *strides)
+    return y
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rope_without_positions_counts_tokens(dtype):
+    """pos NULL: token m is at pos0 + m, whatever pos_tokens says."""
+    freq, _ = kv.rope_frequencies(64)
+    x = normal((2, 37, 3, 64), 1, dtype)
+    want = kv.rope(x, freq, pos0=11)
+    for pos_tokens in (0, 1, -1):
+        assert torch.equal(rope_abi(x, freq, None, pos_tokens, 11), want), pos_tokens
 
 
 def two_token_weights(dtype, B, H):
