@@ -11,6 +11,8 @@ A decode step of a batch, every call enqueued and none waiting for the host::
     kv.write(k, v, k_pages[l], v_pages[l], pages.table, start, rows=rows, freq=freq)
     o = kv.decode_attn(q[:, 0], k_pages[l], v_pages[l], pages.table, pages.length, rows=rows, n_ctx=n)
 
+rope is differentiable; no gradient passes through the cache.
+
 Pools: keys [n_pages, H_kv, 64, d], values [n_pages, H_kv, d, 64], with a leading
 layer dimension for the calls that take all layers at once.
 """
@@ -137,7 +139,12 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
     pos0 + m, plus pos[b] (int32 [B]), or pos0 + pos[b, m] (int32 [B, M]).  The
     first 2 * len(freq) features turn in pairs, half-split or ``interleaved``, and
     are multiplied by ``magnitude``; the rest is copied.  ``transpose`` takes the
-    gradient of the result to the gradient of x.  ``out`` may be x (in place)."""
+    gradient of the result to the gradient of x; autograd calls it where x
+    requires one.  ``out`` may be x (in place)."""
+    if torch.is_grad_enabled() and (x.requires_grad or freq.requires_grad or out is not None and out.requires_grad):
+        if out is not None or freq.requires_grad:
+            raise ValueError("no gradient passes through out or freq; leave out away, or call under torch.no_grad()")
+        return _Rope.apply(x, freq, pos, pos0, interleaved, magnitude, transpose)
     dev, dtype = x.device, x.dtype
     xs = _rows_of(x, "x", dev, dtype)
     shape = x.shape
@@ -156,6 +163,24 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
     _call("lla_rope_positions", dev, _dt(x), B, M, H, d, rot, int(interleaved), int(transpose), x.data_ptr(), *xs, at,
           per_token, pos0, freq.data_ptr(), magnitude, out.data_ptr(), *ys)
     return out
+
+
+class _Rope(torch.autograd.Function):
+    """rope with the transposed call as its gradient.  Positions are kept as they
+    are at the call: reserve writes them without torch's knowledge."""
+
+    @staticmethod
+    def forward(ctx, x, freq, pos, pos0, interleaved, magnitude, transpose):
+        ctx.save_for_backward(freq)
+        ctx.pos = None if pos is None else pos.clone()
+        ctx.args = dict(pos0=pos0, interleaved=interleaved, magnitude=magnitude)
+        ctx.transpose = transpose
+        return rope(x, freq, pos=pos, transpose=transpose, **ctx.args)
+
+    @staticmethod
+    def backward(ctx, grad):
+        freq, = ctx.saved_tensors
+        return rope(grad.contiguous(), freq, pos=ctx.pos, transpose=not ctx.transpose, **ctx.args), *[None] * 6
 
 
 # ---------------------------------------------------------------------------

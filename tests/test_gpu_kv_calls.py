@@ -5,9 +5,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv_oracle as O
 from paper_2607_15456_amd import kv, lla
 from tests.helpers import f64, log
-from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, normal
+from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, ints, near, normal, rope_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +84,70 @@ def test_decode_of_far_scores(dtype, lengths):
         assert np.array_equal(out[:, h], np.stack(want)), h
         # the factor log2(e), the score, the lse: a rounding each, and ln 2's
         assert np.all(np.abs(f64(lse)[:, h] - top) <= 5 * EPS * top)
+
+
+def test_rope_takes_gradients():
+    """Backward of rope is the transposed call, through views, shared rows and a
+    second derivative, and against differences."""
+    freq, mag = kv.rope_frequencies(32, scaling="yarn", factor=2.0, original=128)
+    fused, g = normal((2, 9, 6, 64), 5, F32).requires_grad_(), normal((2, 9, 2, 64), 6, F32)
+    args = dict(pos=ints([3, 900]), magnitude=mag, interleaved=True)
+    pos = np.broadcast_to((np.array([3, 900])[:, None] + np.arange(9))[..., None], (2, 9, 2))
+    y = kv.rope(fused[:, :, 2:4], freq, **args)
+    assert y.requires_grad
+    (y * g).sum().backward()
+    ref = O.kv_rope(f64(g), pos, f64(freq), True, mag, transpose=True)
+    tol = rope_bound(f64(g), 16, True, mag, ref, F32)
+    near(fused.grad[:, :, 2:4], ref, tol, "gradient of a slice")
+    assert not fused.grad[:, :, :2].any() and not fused.grad[:, :, 4:].any()
+    # one row that every head and token shares: gradients add up
+    row = normal((2, 1, 1, 64), 7, F32).requires_grad_()
+    got, = torch.autograd.grad(kv.rope(row.expand(2, 9, 2, 64), freq, **args), row, g)
+    near(got, ref.sum((1, 2), keepdims=True), tol.sum((1, 2), keepdims=True) + 18 * EPS * np.abs(ref).sum((1, 2), keepdims=True),
+         "a shared row")
+    # a gradient without strides of its own, the transposed call's gradient, and a derivative of the gradient
+    x = normal((2, 9, 2, 64), 8, F32).requires_grad_()
+    got, = torch.autograd.grad(kv.rope(x, freq, **args).sum(), x)
+    one = O.kv_rope(np.ones((2, 9, 2, 64)), pos, f64(freq), True, mag, transpose=True)
+    near(got, one, rope_bound(np.ones(one.shape), 16, True, mag, one, F32), "gradient of a sum")
+    got, = torch.autograd.grad(kv.rope(x, freq, transpose=True, **args), x, g)
+    back = O.kv_rope(f64(g), pos, f64(freq), True, mag)
+    near(got, back, rope_bound(f64(g), 16, True, mag, back, F32), "gradient of the transposed")
+    gg = g.clone().requires_grad_()
+    first, = torch.autograd.grad(kv.rope(x, freq, **args), x, gg, create_graph=True)
+    second, = torch.autograd.grad(first, gg, g)
+    near(second, back, rope_bound(f64(g), 16, True, mag, back, F32), "derivative of the gradient")
+    # differences: rope is linear
+    e = normal((2, 9, 2, 64), 9, F32)
+    with torch.no_grad():
+        slope = np.sum(f64(g) * (f64(kv.rope(x + e, freq, **args)) - f64(kv.rope(x - e, freq, **args)))) / 2
+    assert abs(slope - np.sum(ref * f64(e))) <= 1e-6 * np.sum(np.abs(f64(g))) * 6
+
+
+def test_rope_gradient_keeps_its_positions():
+    """Positions that a step overwrites before the backward pass (reserve writes its
+    start without torch's knowledge) are the forward's in the gradient."""
+    freq, _ = kv.rope_frequencies(64)
+    x, g, pos = normal((2, 3, 2, 64), 5, BF).requires_grad_(), normal((2, 3, 2, 64), 6, BF), ints([5, 70])
+    y = kv.rope(x, freq, pos=pos)
+    pages, result, pairs = kv.new_page_table(2, 4, 8), ints([0] * 4), ints([[0, 0]] * 2)
+    kv.reserve(pages, ints([0, 1]), ints([1, 1]), pos, pairs, result)
+    got, = torch.autograd.grad(y, x, g)
+    assert pos.tolist() == [0, 0] and torch.equal(got, kv.rope(g, freq, pos=ints([5, 70]), transpose=True))
+
+
+def test_rope_in_place_does_not_lose_gradients():
+    freq, _ = kv.rope_frequencies(64)
+    x = normal((1, 4, 2, 64), 5, F32)
+    leaf = x.clone().requires_grad_()
+    for a, out in ((leaf, torch.empty_like(x)), (leaf * 1, None), (x, leaf)):
+        with pytest.raises(ValueError):
+            kv.rope(a, freq, out=a if out is None else out)
+    with pytest.raises(ValueError):
+        kv.rope(x, freq.clone().requires_grad_())
+    with torch.no_grad():
+        want = kv.rope(leaf, freq)
+        assert torch.equal(kv.rope(leaf, freq, out=torch.empty_like(x)), want) and not want.requires_grad
+        kv.rope(leaf, freq, out=leaf)
+    assert torch.equal(leaf, want)
+    assert not kv.rope(x, freq).requires_grad
