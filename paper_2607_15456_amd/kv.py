@@ -92,6 +92,12 @@ def _ints(t, name, shape, dev):
         raise ValueError(f"{name} must have shape {list(shape)}")
 
 
+def _whole(x, names):
+    """x: numbers joined by or, that the library takes in 32 bits (ctypes would cut them)."""
+    if x >> 31 not in (0, -1):
+        raise ValueError(f"{names} must fit 32 bits")
+
+
 def _rows_of(t, name, dev, dtype):
     """Strides of t [B, M, heads, width] whose rows are dense (of a dimension of
     one entry, which torch leaves as it happens to be, 0)."""
@@ -149,6 +155,7 @@ def rope(x, freq, *, pos=None, pos0: int = 0, interleaved: bool = False, magnitu
     xs = _rows_of(x, "x", dev, dtype)
     shape = x.shape
     B, M, H, d = shape
+    _whole(pos0, "pos0")
     rot, at, per_token = _freq(freq, d, dev), None, 0
     if pos is not None:
         per_token = int(pos.dim() == 2)
@@ -359,6 +366,7 @@ def decode_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int
     """Workspace of decode_attn on the current device (0: no context is split over
     workgroups)."""
     out = _c_sz()
+    _whole(n_ctx | sink | window, "n_ctx, sink and window")
     _check(lib().lla_kv_decode_workspace_bytes(_out_code(dtype), B, H, H_kv, d, n_ctx, sink, window, ctypes.byref(out)))
     return out.value
 
@@ -378,6 +386,7 @@ def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, sc
     if width != d or k_pages.device != dev or v_pages.device != dev:
         raise ValueError("q must be [B, H, d] with the pools' width, on their device")
     n_seqs, max_pages = table.shape
+    _whole(n_ctx | sink | window, "n_ctx, sink and window")
     for t, name, shape in ((table, "table", (n_seqs, max_pages)), (length, "length", (n_seqs,))):
         _ints(t, name, shape, dev)
     if rows is not None:

@@ -151,3 +151,18 @@ def test_rope_in_place_does_not_lose_gradients():
         kv.rope(leaf, freq, out=leaf)
     assert torch.equal(leaf, want)
     assert not kv.rope(x, freq).requires_grad
+
+
+def test_positions_past_32_bits_are_refused():
+    """A whole number that the library's int would cut is refused, not cut."""
+    freq, _ = kv.rope_frequencies(64)
+    c = Cache(BF, [64], 1, 64)
+    x, q = normal((1, 2, 1, 64), 1, BF), normal((1, 1, 64), 2, BF)
+    for pos0 in (1 << 31, -(1 << 31) - 1, 1 << 32):
+        with pytest.raises(ValueError):
+            kv.rope(x, freq, pos0=pos0)
+    near(kv.rope(x, freq, pos0=(1 << 31) - 2), ref := O.kv_rope(f64(x), (1 << 31) - 2 + np.arange(2)[None, :, None], f64(freq)),
+         rope_bound(f64(x), 32, False, 1.0, ref, BF), "the last position")
+    for bad in (dict(n_ctx=(1 << 32) + 64), dict(n_ctx=64, window=(1 << 32) + 5), dict(n_ctx=64, window=1, sink=1 << 32)):
+        with pytest.raises(ValueError):
+            kv.decode_attn(q, c.k, c.v, c.table, c.length, **bad)
