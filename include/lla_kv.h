@@ -69,8 +69,9 @@ typedef enum lla_rope_scaling {
 typedef enum lla_pages_status {
   LLA_PAGES_OK = 0,
   LLA_PAGES_FULL = 1, /* fewer free pages than the call needs */
-  LLA_PAGES_BAD = 2   /* a row out of range or named twice, a sequence that would
-                         outgrow max_pages, a fork onto a sequence that is not empty */
+  LLA_PAGES_BAD = 2   /* a row out of range or named twice (-1 is padding, as often as
+                         wanted), a sequence that would outgrow max_pages, a fork onto
+                         a sequence that is not empty */
 } lla_pages_status;
 
 /* LLA_KV_ABI_VERSION of the built library. */
@@ -191,7 +192,10 @@ lla_status lla_kv_decode_attn(int dtype, int out_dtype, int B, int H, int H_kv, 
  * of copy pairs, the pages taken or given back, and the free pages left; with
  * any status but LLA_PAGES_OK it changes nothing else (lla_pages_reserve sets
  * start to -1 as well).  The outcome is that of taking the rows one after
- * another in the order of `rows`, and does not vary between runs.
+ * another in the order of `rows`, and does not vary between runs.  Rows of -1 (of
+ * lla_pages_fork: in dst) are padding, as in lla_kv_write and lla_kv_decode_attn: they
+ * are passed over, whatever stands beside them, and get a start of -1, so that a
+ * captured step of a fixed number of rows serves fewer sequences.
  */
 
 /*

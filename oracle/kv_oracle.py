@@ -80,7 +80,7 @@ def kv_decode_attn(q, k_pages, v_pages, table, length, rows=None, scale=None, si
 
 
 class KvTables:
-    """Tables as lists, changed one row after another."""
+    """Tables as lists, changed one row after another; rows of -1 are passed over."""
 
     def __init__(self, n_seqs, max_pages, n_pages):
         self.table = [[-1] * max_pages for _ in range(n_seqs)]
@@ -90,17 +90,21 @@ class KvTables:
         self.max_pages, self.n_pages = max_pages, n_pages
 
     def _bad(self, rows):
+        rows = [r for r in rows if r != -1]
         return len(set(rows)) < len(rows) or any(not 0 <= r < len(self.length) for r in rows)
 
     def reserve(self, rows, add):
         """(status, start, pairs)"""
         none = [-1] * len(rows)
-        if self._bad(rows) or any(a < 0 or self.length[r] + a > PAGE * self.max_pages for r, a in zip(rows, add)):
+        if self._bad(rows) or any(r != -1 and (a < 0 or self.length[r] + a > PAGE * self.max_pages) for r, a in zip(rows, add)):
             return BAD, none, []
         before = ([list(t) for t in self.table], list(self.length), list(self.refs), list(self.free))
         start, pairs = [], []
         try:
             for r, a in zip(rows, add):
+                if r == -1:
+                    start.append(-1)
+                    continue
                 n = self.length[r]
                 last = n // PAGE
                 if n % PAGE and a and self.refs[self.table[r][last]] > 1:
@@ -120,10 +124,11 @@ class KvTables:
         return OK, start, pairs
 
     def fork(self, src, dst):
-        if (self._bad(dst) or any(not 0 <= s < len(self.length) or s in dst for s in src)
-                or any(self.length[r] for r in dst)):
+        pairs = [(s, r) for s, r in zip(src, dst) if r != -1]
+        if (self._bad(dst) or any(not 0 <= s < len(self.length) or s in dst for s, _ in pairs)
+                or any(self.length[r] for _, r in pairs)):
             return BAD
-        for s, r in zip(src, dst):
+        for s, r in pairs:
             n = -(-self.length[s] // PAGE)
             self.table[r][:n] = self.table[s][:n]
             self.length[r] = self.length[s]
@@ -134,6 +139,7 @@ class KvTables:
     def free_rows(self, rows):
         if self._bad(rows):
             return BAD
+        rows = [r for r in rows if r != -1]
         back = []
         held = [(r, i) for r in rows for i in range(-(-self.length[r] // PAGE))]
         for r, i in held:

@@ -17,6 +17,7 @@ namespace lla {
 namespace {
 
 constexpr int kRows = LLA_KV_MAX_ROWS, kThreads = 1024;
+constexpr int kPadding = -1;  // a row that a call passes over
 
 __device__ __forceinline__ int pages_of(int64_t n) { return (int)((n + kPage - 1) / kPage); }
 
@@ -70,8 +71,8 @@ __device__ __forceinline__ void report(const TableArgs& a, int status, int pairs
 __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
   __shared__ int s_row[kRows], s_open[kRows], s_at[kRows], s_have[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
-  const bool mine = i < a.n;
-  s_row[i] = mine ? a.rows[i] : -1;
+  s_row[i] = i < a.n ? a.rows[i] : kPadding;
+  const bool mine = s_row[i] != kPadding;
   __syncthreads();
   bool ok = !mine || sound(s_row, i, a.n_seqs);
   const int row = mine && ok ? s_row[i] : -1;
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
   s_open[i] = open;
   ok = ok && n_free >= 0 && n_free <= a.n_pages;
   if (!__syncthreads_and(ok)) {
-    if (mine) a.start[i] = -1;
+    if (i < a.n) a.start[i] = -1;
     if (i == 0) report(a, LLA_PAGES_BAD, 0, 0, n_free);
     return;
   }
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
   const int at = prefix(need, s_wave, total);
   const int pair = prefix(copy ? 1 : 0, s_wave, pairs);
   if (total > n_free) {
-    if (mine) a.start[i] = -1;
+    if (i < a.n) a.start[i] = -1;
     if (i == 0) report(a, LLA_PAGES_FULL, 0, 0, n_free);
     return;
   }
@@ -120,6 +121,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
     }
     a.start[i] = len;
     a.length[row] = (int)end;
+  } else if (i < a.n) {
+    a.start[i] = -1;
   }
   __syncthreads();
   for (int e = i; e < total; e += kThreads) {
@@ -137,8 +140,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(TableArgs a) {
 __global__ __launch_bounds__(kThreads) void fork_kernel(TableArgs a) {
   __shared__ int s_row[kRows], s_src[kRows], s_at[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
-  const bool mine = i < a.n;
-  s_row[i] = mine ? a.rows[i] : -1;
+  s_row[i] = i < a.n ? a.rows[i] : kPadding;
+  const bool mine = s_row[i] != kPadding;
   s_src[i] = mine ? a.more[i] : -1;
   __syncthreads();
   bool ok = true;
@@ -179,8 +182,8 @@ __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
   constexpr int kNamed = (int)0x80000000;
   __shared__ int s_row[kRows], s_at[kRows], s_wave[kThreads / kWave];
   const int i = threadIdx.x;
-  const bool mine = i < a.n;
-  s_row[i] = mine ? a.rows[i] : -1;
+  s_row[i] = i < a.n ? a.rows[i] : kPadding;
+  const bool mine = s_row[i] != kPadding;
   __syncthreads();
   bool ok = true;
   int len = 0;

@@ -13,6 +13,9 @@ A decode step of a batch, every call enqueued and none waiting for the host::
 
 rope is differentiable; no gradient passes through the cache.
 
+Rows of -1 are padding in every call: a step captured for a fixed number of rows
+serves fewer sequences.
+
 Pools: keys [n_pages, H_kv, 64, d], values [n_pages, H_kv, d, 64], with a leading
 layer dimension for the calls that take all layers at once.
 """
@@ -262,7 +265,7 @@ def _page_table(p, dev):
 
 def reserve(pages: PageTable, rows, add, start, pairs, result):
     """Room for add[i] new tokens of sequence rows[i]; start[i] gets its length
-    before (-1 where the call is refused), pairs the pages to copy (copy on write)
+    before (-1 where the call is refused, and of padding), pairs the pages to copy (copy on write)
     and result (status, number of pairs, pages taken, pages left).  All int32:
     rows, add, start [n], pairs [n, 2], result [4]."""
     dev, n = rows.device, rows.numel()

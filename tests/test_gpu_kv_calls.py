@@ -8,7 +8,7 @@ import torch
 from oracle import kv_oracle as O
 from paper_2607_15456_amd import kv, lla
 from tests.helpers import f64, log
-from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, ints, near, normal, rope_bound
+from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, ints, near, normal, rope_bound, same_tables
 
 pytestmark = pytest.mark.gpu
 
@@ -151,6 +151,94 @@ def test_rope_in_place_does_not_lose_gradients():
         kv.rope(leaf, freq, out=leaf)
     assert torch.equal(leaf, want)
     assert not kv.rope(x, freq).requires_grad
+
+
+def test_rows_of_a_padded_batch():
+    """Rows of -1 pass through every call of a step: no room taken, start -1, nothing
+    written, zeros; several of them, and a batch of nothing else."""
+    pages, t = kv.new_page_table(5, 6, 20), O.KvTables(5, 6, 20)
+    result = ints([0] * 4)
+
+    def reserve(rows, add, n):
+        start, pairs = ints([-9] * n), ints([[-9, -9]] * n)
+        kv.reserve(pages, ints(rows), ints(add), start, pairs, result)
+        status, want, want_pairs = t.reserve(rows, add)
+        assert start.tolist() == want and pairs[:len(want_pairs)].tolist() == [list(p) for p in want_pairs]
+        assert result[0] == status and result[3] == len(t.free)
+        same_tables(pages, t)
+        return status
+
+    assert reserve([-1, 2, -1, 0], [1, 70, -5, 3], 4) == O.OK
+    assert reserve([-1, -1], [1, 1], 2) == O.OK
+    kv.fork(pages, ints([0, -1, 2, 77]), ints([1, -1, 4, -1]), result)
+    assert t.fork([0, -1, 2, 77], [1, -1, 4, -1]) == O.OK == int(result[0])
+    same_tables(pages, t)
+    assert reserve([-1, 4, 2, 0, -1, 1], [1] * 6, 6) == O.OK
+    assert reserve([-1, 2, -1, 2], [1] * 4, 4) == O.BAD
+    assert reserve([-2, 2], [1] * 2, 2) == O.BAD
+    kv.fork(pages, ints([-1]), ints([3]), result)  # a source is a sequence
+    assert t.fork([-1], [3]) == O.BAD == int(result[0])
+    kv.free(pages, ints([-1, 1, -1, 0]), result)
+    assert t.free_rows([-1, 1, -1, 0]) == O.OK == int(result[0])
+    same_tables(pages, t)
+    kv.free(pages, ints([-1] * 3), result)
+    assert t.free_rows([-1] * 3) == O.OK and result.tolist() == [0, 0, 0, len(t.free)]
+    same_tables(pages, t)
+
+
+def test_captured_step_with_padding():
+    """One captured step of four entries replayed with fewer and other live
+    sequences: as the eager step of these alone."""
+    dtype, H, Hkv, d, n_ctx = BF, 4, 2, 64, 64 * 6
+
+    def program(n):
+        pages = kv.new_page_table(6, 6, 40)
+        k, v = (x.zero_() for x in kv.alloc_pages(40, Hkv, d, dtype))
+        freq, _ = kv.rope_frequencies(d)
+        rows, add, start, pairs, result = ints([-1] * n), ints([1] * n), ints([0] * n), ints([[0, 0]] * n), ints([0] * 4)
+        x = torch.zeros((n, 1, H + 2 * Hkv, d), dtype=dtype, device=DEV)
+        out = torch.zeros((n, H, d), device=DEV)
+
+        def step():
+            kv.reserve(pages, rows, add, start, pairs, result)
+            kv.copy_pages(k, v, pairs, result)
+            kv.write(x[:, :, H:H + Hkv], x[:, :, H + Hkv:], k, v, pages.table, start, rows=rows, freq=freq)
+            q = kv.rope(x[:, :, :H], freq, pos=start)
+            kv.decode_attn(q[:, 0].contiguous(), k, v, pages.table, pages.length, rows=rows, n_ctx=n_ctx, out=out)
+        return step, rows, x, out, pages, (k, v), result
+
+    captured, eager = program(4), {n: program(n) for n in (1, 2, 3, 4)}
+    whole = eager[4]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    captured[0]()  # (with padding alone: nothing changes)
+    torch.cuda.synchronize()
+    assert not captured[4].length.any() and int(captured[4].free[0]) == 40
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        captured[0]()
+    for i, rows in enumerate(([0, 1, 2, 3], [1, -1, 3, -1], [-1, -1, -1, 5], [4, 3, -1, 0], [-1] * 4, [5, 4, 2, 1])):
+        x = normal((4, 1, H + 2 * Hkv, d), 40 + i, dtype)
+        captured[1].copy_(ints(rows))
+        captured[2].copy_(x)
+        g.replay()
+        live = [j for j in range(4) if rows[j] >= 0]
+        if i % 2:
+            torch.cuda.synchronize()
+        if live:  # the same step without padding, over the same tables and pools
+            p = eager[len(live)]
+            for mine, its in zip((*p[4], *p[5]), (*whole[4], *whole[5])):
+                mine.copy_(its)
+            p[1].copy_(ints([rows[j] for j in live]))
+            p[2].copy_(x[live])
+            p[0]()
+            if p is not whole:
+                for mine, its in zip((*whole[4], *whole[5]), (*p[4], *p[5])):
+                    mine.copy_(its)
+            assert torch.equal(captured[3][live], p[3]), i
+        assert captured[6][0] == 0 and not captured[3][[j for j in range(4) if j not in live]].any(), i
+        for mine, its in zip((*captured[4], *captured[5]), (*whole[4], *whole[5])):
+            assert torch.equal(mine, its), i
 
 
 def test_positions_past_32_bits_are_refused():
