@@ -147,8 +147,10 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream);
 
-/* Workspace bytes lla_kv_decode_attn needs for these sizes on the current
- * device: 0 when no context is split over workgroups.  Host only.
+/* Workspace bytes that serve lla_kv_decode_attn for every batch of 1 .. B entries
+ * and every bound of 1 .. n_ctx (other arguments the same) on the current device,
+ * so that the largest sizes of a program are asked for once: 0 where none of these
+ * calls splits a context over workgroups.  Host only.
  * Errors: LLA_ERR_INVALID_ARG. */
 lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int d_head, int n_ctx,
                                          int sink, int window, size_t* bytes);
@@ -168,7 +170,7 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  *   lse     NULL, or float [B][H]: the natural logarithm of sum_n exp(s_n)
  *   workspace  device memory of ws_bytes >= lla_kv_decode_workspace_bytes(), no
  *           initial contents needed and none kept between calls; NULL with ws_bytes == 0
- *           where that is 0
+ *           where that is 0 (a call whose own sizes need less takes less)
  * An entry with N = 0 or rows[b] = -1 (padding of a batch) gets zeros and an
  * lse of -inf; another row outside [0, n_seqs), an N outside [0, n_ctx] or a page outside
  * [0, n_pages) among those read gets NaN.  Slots that are not attended may hold anything.

@@ -212,8 +212,7 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
 lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int d_head, int n_ctx,
                                          int sink, int window, size_t* bytes) {
   if (!decode_ok(dtype, B, H, H_kv, d_head, n_ctx, sink, window) || !bytes) return LLA_ERR_INVALID_ARG;
-  lla::KvDecodeArgs a = decode_args(dtype, B, H, H_kv, d_head, n_ctx, sink, window);
-  *bytes = lla::kv_decode_shape(a);
+  *bytes = lla::kv_decode_workspace(decode_args(dtype, B, H, H_kv, d_head, n_ctx, sink, window));
   return LLA_OK;
 }
 

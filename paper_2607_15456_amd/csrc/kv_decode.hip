@@ -635,9 +635,7 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-}  // namespace
-
-// Slices of a context.  Long ones: as many as give each compute unit two
+// Slices of a context, at most.  Long ones: as many as give each compute unit two
 // workgroups, if a slice keeps kLong pages; otherwise one workgroup a unit, since
 // a join costs a launch (4 us) and has to save more.  Measured (width 128, bf16
 // but for the first; unsplit / split, us):
@@ -651,23 +649,41 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
 //   256 tokens, 8 of 64, fp32          4 x 8.2 / 9.0
 //   20 x 1024 .. 4096, 16 key heads    89 / 80;  12 x 2250 .. 9000, 8 key heads 100 / 59
 //   40 x 4096, 16 key heads (640 workgroups) 209 / 208 .. 214
-size_t kv_decode_shape(KvDecodeArgs& a) {
+int most_slices(const KvDecodeArgs& a, int units, int pages, int cus) {
   constexpr int kLong = 16, kAlone = 128 << 10;
-  const int all = (a.n_ctx + kPage - 1) / kPage;
-  // most pages that an entry attends
-  const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
-  const int pages = a.window ? (int)std::min<int64_t>(all, budget) : all;
-  const int64_t units = (int64_t)a.B * a.p.Hkv * query_blocks(a.H / a.p.Hkv);
-  const int64_t cus = device_cu_count();
-  int64_t want = (2 * cus + units - 1) / units;
-  if (pages < want * kLong) want = std::max<int64_t>(1, cus / units);
   // a step a wavefront; of narrow heads, what eight wavefronts read in two steps or less
   const int waves = a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2, bytes = a.p.d * (a.p.dtype == LLA_BF16 ? 256 : 512);
-  if (pages <= waves || (most_waves(a.p.d) > kWaves && units <= cus && pages <= kAlone / bytes)) want = 1;
-  a.per = (int)((pages + want - 1) / want);
-  a.per = std::max(a.per, (pages + kMaxSlices - 1) / kMaxSlices);
+  if (pages <= waves || (most_waves(a.p.d) > kWaves && units <= cus && pages <= kAlone / bytes)) return 1;
+  const int want = (2 * cus + units - 1) / units;
+  return std::min(pages < (int64_t)want * kLong ? std::max(1, cus / units) : want, kMaxSlices);
+}
+// Most pages that an entry attends.
+int most_pages(const KvDecodeArgs& a) {
+  const int all = (a.n_ctx + kPage - 1) / kPage;
+  const int64_t budget = ((int64_t)a.sink + kPage - 1) / kPage + ((int64_t)a.window + kPage - 1) / kPage + 1;
+  return a.window ? (int)std::min<int64_t>(all, budget) : all;
+}
+int units_of(const KvDecodeArgs& a) { return a.p.Hkv * query_blocks(a.H / a.p.Hkv); }  // of an entry
+size_t partial_bytes(const KvDecodeArgs& a, int B, int slices) {
+  return slices == 1 ? 0 : (size_t)B * a.H * slices * (a.p.d + 4) * sizeof(float);
+}
+}  // namespace
+
+size_t kv_decode_shape(KvDecodeArgs& a) {
+  const int pages = most_pages(a), want = most_slices(a, a.B * units_of(a), pages, device_cu_count());
+  a.per = (pages + want - 1) / want;
   a.slices = (pages + a.per - 1) / a.per;
-  return a.slices == 1 ? 0 : (size_t)a.B * a.H * a.slices * (a.p.d + 4) * sizeof(float);
+  return partial_bytes(a, a.B, a.slices);
+}
+
+// With more pages there are no fewer slices wanted, with more entries there may be: the
+// most of any number of them (none are split from 2 workgroups a compute unit on).
+size_t kv_decode_workspace(const KvDecodeArgs& a) {
+  const int pages = most_pages(a), cus = device_cu_count(), units = units_of(a);
+  size_t most = 0;
+  for (int B = 1; B <= a.B && (int64_t)B * units < 2 * cus; ++B)
+    most = std::max(most, partial_bytes(a, B, std::min(pages, most_slices(a, B * units, pages, cus))));
+  return most;
 }
 
 hipError_t launch_kv_decode(const KvDecodeArgs& a, hipStream_t stream) {

@@ -59,8 +59,10 @@ struct KvDecodeArgs {
   float* part;
 };
 hipError_t launch_kv_decode(const KvDecodeArgs& a, hipStream_t stream);
-// Chooses slices and per; returns the workspace bytes.
+// Chooses slices and per; returns the workspace bytes that this takes.
 size_t kv_decode_shape(KvDecodeArgs& a);
+// The most that it takes for any B and n_ctx up to a's.
+size_t kv_decode_workspace(const KvDecodeArgs& a);
 
 struct TableArgs {
   int n, n_seqs, max_pages, n_pages;

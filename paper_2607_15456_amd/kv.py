@@ -366,8 +366,8 @@ def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, freq=N
 
 def decode_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int, n_ctx: int, sink: int = 0,
                            window: int = 0) -> int:
-    """Workspace of decode_attn on the current device (0: no context is split over
-    workgroups)."""
+    """Workspace of decode_attn on the current device for up to B entries and bounds up
+    to n_ctx (0: none of these splits a context over workgroups)."""
     out = _c_sz()
     _whole(n_ctx | sink | window, "n_ctx, sink and window")
     _check(lib().lla_kv_decode_workspace_bytes(_out_code(dtype), B, H, H_kv, d, n_ctx, sink, window, ctypes.byref(out)))

@@ -86,6 +86,18 @@ def test_decode_of_far_scores(dtype, lengths):
         assert np.all(np.abs(f64(lse)[:, h] - top) <= 5 * EPS * top)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_decode_workspace_of_the_largest_call_serves_all(dtype):
+    """A program's one workspace, for its most entries and longest context, in every
+    call below: the same bits as with one of its own."""
+    c = Cache(dtype, [2112, 2048, 1088, 1024, 300, 77, 5000, 700], 4, 128, seed=6)
+    q = normal((8, 8, 128), 7, dtype)
+    ws = torch.empty(kv.decode_workspace_bytes(dtype, 8, 8, 4, 128, 5000), dtype=torch.uint8, device=DEV)
+    for B, n in ((1, 1024), (1, 1088), (1, 2048), (1, 2112), (2, 5000), (3, 2112), (7, 4097), (8, 5000), (8, 64), (5, 257)):
+        args = (q[:B], c.k, c.v, c.table, c.length.clamp(max=n))
+        assert torch.equal(kv.decode_attn(*args, n_ctx=n, workspace=ws), kv.decode_attn(*args, n_ctx=n)), (B, n)
+
+
 def test_rope_takes_gradients():
     """Backward of rope is the transposed call, through views, shared rows and a
     second derivative, and against differences."""

@@ -16,3 +16,20 @@ def test_numbers_past_32_bits_are_refused():
         with pytest.raises(lla.LLAError):
             kv.decode_workspace_bytes(torch.bfloat16, 1, 1, 1, 64, **bad)
     assert kv.decode_workspace_bytes(torch.bfloat16, 1, 1, 1, 64, 64, 5, (1 << 31) - 1) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,H_kv,d", [(16, 16, 128), (16, 2, 128), (24, 8, 64), (64, 1, 96), (8, 8, 32), (40, 2, 256)])
+@pytest.mark.parametrize("sink,window", [(0, 0), (4, 3000)])
+def test_a_workspace_serves_smaller_calls(dtype, H, H_kv, d, sink, window):
+    """What the largest batch and context of a program need is enough for all below."""
+    sizes = [1, 2, 3, 5, 8, 15, 16, 17, 31, 33, 64, 200, 513]
+    bounds = [1, 64, 129, 257, 500, 513, 1024, 1025, 1088, 2048, 2112, 3000, 4097, 8192, 16384, 20000, 32768, 40000, 131072]
+    need = {(B, n): kv.decode_workspace_bytes(dtype, B, H, H_kv, d, n, sink, window) for B in sizes for n in bounds}
+    assert any(need.values()) and not any(need[B, 64] for B in sizes)
+    for i, B in enumerate(sizes):
+        for j, n in enumerate(bounds):
+            if i:
+                assert need[sizes[i - 1], n] <= need[B, n], (B, n)
+            if j:
+                assert need[B, bounds[j - 1]] <= need[B, n], (B, n)
