@@ -163,8 +163,8 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  *
  *   q       [B][H][d_head]
  *   rows    int32 [B], or NULL: entry b is sequence b
- *   n_ctx   upper bound of the lengths, in [1, 64*max_pages]: the split of the
- *           work over the device goes by it
+ *   n_ctx   upper bound of the lengths, in [1, 64*max_pages]: how many workgroups
+ *           may share an entry goes by it; what each takes, by the entry's length
  *   scale   > 0, scale * log2(e) finite in 32 bits (usually 1/sqrt(d_head))
  *   out     [B][H][d_head] of out_dtype
  *   lse     NULL, or float [B][H]: the natural logarithm of sum_n exp(s_n)

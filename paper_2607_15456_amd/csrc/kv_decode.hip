@@ -86,6 +86,17 @@ struct Span {
   }
 };
 
+// Pages that each slice of an entry takes.  The split is of the entry's own pages: the
+// bound, which a captured step sets for a sequence's whole life, says how many slices
+// there may be (a sequence of 4096 tokens, 16 key heads, bound 131,072: 47 us with the
+// bound's slices, 14 with its own; 24 x 1000 tokens of 8 heads of 64, bound 8192: 17.4, 18.3).
+__device__ __forceinline__ int slice_pages(const KvDecodeArgs& a, int pages) {
+  if (a.slices == 1) return pages;
+  // the quotient: pages < 2^21 and slices <= 512, so the product with 2^32 / slices,
+  // rounded up, is off by less than 1 / slices
+  return max(a.least, (int)__umulhi((unsigned)(pages + a.slices - 1), a.inverse));
+}
+
 // Entry b's tokens: 0 for padding, -1 where its row or length is out of range.
 __device__ __forceinline__ int entry_tokens(const KvDecodeArgs& a, int b, int& row) {
   row = a.rows ? uniform(a.rows, b) : b;
@@ -378,7 +389,7 @@ __global__ __launch_bounds__(most_waves(D) * kWave, D <= 128 && NT * D <= 128 ? 
   int row;
   const int n = entry_tokens(a, b, row);
   const Span sp(max(n, 0), a.sink, a.window);
-  const int pb = slice * a.per, pe = min(sp.pages, pb + a.per);
+  const int per = slice_pages(a, sp.pages), pb = slice * per, pe = min(sp.pages, pb + per);
   if (n <= 0 || pb >= pe) {
     if (n <= 0 && slice == 0 && w == 0 && a.slices == 1) {
       const float none = n < 0 ? __builtin_nanf("") : 0.f;
@@ -550,7 +561,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
   int row;
   const int n = entry_tokens(a, b, row);
   const Span sp(max(n, 0), a.sink, a.window);
-  const int slices = (sp.pages + a.per - 1) / a.per;
+  const int per = slice_pages(a, sp.pages), slices = (sp.pages + per - 1) / per;
   float ms[kMaxSlices / kJoinThreads], ls[kMaxSlices / kJoinThreads], m = neg_inf(), l = 0.f;
 #pragma unroll
   for (int i = 0; i < kMaxSlices / kJoinThreads; ++i) {
@@ -635,6 +646,8 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+int wave_pages(const KvDecodeArgs& a) { return a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2; }  // of a step a wavefront
+
 // Slices of a context, at most.  Long ones: as many as give each compute unit two
 // workgroups, if a slice keeps kLong pages; otherwise one workgroup a unit, since
 // a join costs a launch (4 us) and has to save more.  Measured (width 128, bf16
@@ -652,8 +665,8 @@ hipError_t launch(const KvDecodeArgs& a, hipStream_t stream) {
 int most_slices(const KvDecodeArgs& a, int units, int pages, int cus) {
   constexpr int kLong = 16, kAlone = 128 << 10;
   // a step a wavefront; of narrow heads, what eight wavefronts read in two steps or less
-  const int waves = a.p.dtype == LLA_BF16 ? kWaves : kWaves / 2, bytes = a.p.d * (a.p.dtype == LLA_BF16 ? 256 : 512);
-  if (pages <= waves || (most_waves(a.p.d) > kWaves && units <= cus && pages <= kAlone / bytes)) return 1;
+  const int bytes = a.p.d * (a.p.dtype == LLA_BF16 ? 256 : 512);
+  if (pages <= wave_pages(a) || (most_waves(a.p.d) > kWaves && units <= cus && pages <= kAlone / bytes)) return 1;
   const int want = (2 * cus + units - 1) / units;
   return std::min(pages < (int64_t)want * kLong ? std::max(1, cus / units) : want, kMaxSlices);
 }
@@ -673,6 +686,8 @@ size_t kv_decode_shape(KvDecodeArgs& a) {
   const int pages = most_pages(a), want = most_slices(a, a.B * units_of(a), pages, device_cu_count());
   a.per = (pages + want - 1) / want;
   a.slices = (pages + a.per - 1) / a.per;
+  a.least = std::min(a.per, wave_pages(a));
+  a.inverse = a.slices == 1 ? 0 : (unsigned)(((1ull << 32) + a.slices - 1) / a.slices);
   return partial_bytes(a, a.B, a.slices);
 }
 

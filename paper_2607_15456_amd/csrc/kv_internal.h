@@ -49,7 +49,10 @@ struct KvDecodeArgs {
   KvPages p;
   int out_dtype, B, H;
   int n_ctx, sink, window;
-  int slices, per;  // workgroups per (entry, key head, query tile); pages a slice takes
+  // workgroups per (entry, key head, query tile); pages that a slice takes of the
+  // longest entry that n_ctx allows, and of any entry at least
+  int slices, per, least;
+  unsigned inverse;  // 2^32 / slices, rounded up
   const int32_t* length;
   const int32_t* rows;
   const void* q;
@@ -59,7 +62,7 @@ struct KvDecodeArgs {
   float* part;
 };
 hipError_t launch_kv_decode(const KvDecodeArgs& a, hipStream_t stream);
-// Chooses slices and per; returns the workspace bytes that this takes.
+// Chooses slices, per, least and inverse; returns the workspace bytes that this takes.
 size_t kv_decode_shape(KvDecodeArgs& a);
 // The most that it takes for any B and n_ctx up to a's.
 size_t kv_decode_workspace(const KvDecodeArgs& a);

@@ -8,7 +8,7 @@ import torch
 from oracle import kv_oracle as O
 from paper_2607_15456_amd import kv, lla
 from tests.helpers import f64, log
-from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, ints, near, normal, rope_bound, same_tables
+from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, check_decode, ints, near, normal, rope_bound, same_tables
 
 pytestmark = pytest.mark.gpu
 
@@ -96,6 +96,23 @@ def test_decode_workspace_of_the_largest_call_serves_all(dtype):
     for B, n in ((1, 1024), (1, 1088), (1, 2048), (1, 2112), (2, 5000), (3, 2112), (7, 4097), (8, 5000), (8, 64), (5, 257)):
         args = (q[:B], c.k, c.v, c.table, c.length.clamp(max=n))
         assert torch.equal(kv.decode_attn(*args, n_ctx=n, workspace=ws), kv.decode_attn(*args, n_ctx=n)), (B, n)
+
+
+@pytest.mark.parametrize("dtype,most", [(BF, 131072), (F32, 131072), (BF, 20000)])
+def test_decode_splits_an_entry_under_a_far_bound(dtype, most):
+    """A bound far above the lengths (a step captured once for a sequence's whole
+    life) does not leave an entry to one workgroup a head: the partials of eight
+    slices and more are laid into the workspace."""
+    n, H, d = 4096, 16, 128
+    c = Cache(dtype, [n, 70, 0], H, d, seed=5, max_pages=-(-most // 64))
+    q = normal((3, H, d), 99, dtype)
+    ws = torch.full((kv.decode_workspace_bytes(dtype, 3, H, H, d, most),), 0xa5, dtype=torch.uint8, device=DEV)
+    for b in (1, 3):
+        ws.fill_(0xa5)
+        out = kv.decode_attn(q[:b], c.k, c.v, c.table, c.length, n_ctx=most, workspace=ws)
+        assert int((ws.view(torch.int32) != -0x5a5a5a5b).sum()) >= (8 if b == 1 else 4) * H * (d + 1), b
+        assert torch.isfinite(out).all()
+    check_decode(c, H, n_ctx=most)
 
 
 def test_rope_takes_gradients():
