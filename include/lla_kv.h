@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define LLA_KV_ABI_VERSION 1
+#define LLA_KV_ABI_VERSION 2
 #define LLA_KV_MAX_ROWS 1024 /* sequences of one reserve, fork or free */
 #define LLA_KV_MAX_ROW 512   /* widest row of lla_rope_positions */
 
@@ -146,6 +146,20 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream);
+
+/*
+ * lla_kv_write for sequences whose places in the cache are not their positions, as
+ * after lla_kv_gather has kept a part of them: token m goes to place start[b] + m as
+ * there, and its key is turned to position pos[b] + m.
+ *   pos     int32 [B], or NULL: start
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
+ */
+lla_status lla_kv_write_at(int dtype, int B, int M, int H_kv, int d_head, int d_rot, int interleaved,
+                           const void* k, int64_t k_b, int64_t k_m, const void* v, int64_t v_b,
+                           int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
+                           int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
+                           const int32_t* pos, const int32_t* n_new, void* k_pages, void* v_pages,
+                           void* stream);
 
 /* Workspace bytes that serve lla_kv_decode_attn for every batch of 1 .. B entries
  * and every bound of 1 .. n_ctx (other arguments the same) on the current device,
@@ -252,7 +266,10 @@ lla_status lla_pages_copy(int layers, int n_pages, void* a, int64_t a_bytes, voi
  * Keep a part of a sequence's tokens: for i < n_keep[j], position i of sequence
  * dst[j] becomes position keep[j][i] of sequence src[j] (keys as they are
  * stored, so turned at the position they were written for), in pools of
- * [layers][n_pages] pages.
+ * [layers][n_pages] pages.  From then on a length counts kept tokens and is no
+ * position: the caller keeps the count of all tokens, turns queries to it
+ * (lla_rope_positions) and gives it to lla_kv_write_at for the keys.  A start of
+ * lla_pages_reserve would put new tokens before kept ones.
  *   src, dst  int32 [B];  keep  int32 [B][max_keep];  n_keep  int32 [B], or NULL: max_keep each
  * dst's pages must be its own and not src's (lla_pages_reserve after
  * lla_pages_fork and lla_pages_free keeps the sequence's number).  A position keep[j][i]

@@ -180,12 +180,21 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
                         int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
                         int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
                         const int32_t* n_new, void* k_pages, void* v_pages, void* stream) {
+  return lla_kv_write_at(dtype, B, M, H_kv, d_head, d_rot, interleaved, k, k_b, k_m, v, v_b, v_m, freq, magnitude,
+                         n_seqs, max_pages, n_pages, table, rows, start, nullptr, n_new, k_pages, v_pages, stream);
+}
+
+lla_status lla_kv_write_at(int dtype, int B, int M, int H_kv, int d_head, int d_rot, int interleaved,
+                           const void* k, int64_t k_b, int64_t k_m, const void* v, int64_t v_b,
+                           int64_t v_m, const double* freq, float magnitude, int n_seqs, int max_pages,
+                           int n_pages, const int32_t* table, const int32_t* rows, const int32_t* start,
+                           const int32_t* pos, const int32_t* n_new, void* k_pages, void* v_pages, void* stream) {
   if (!dtype_ok(dtype) || B < 1 || M < 1 || H_kv < 1 || H_kv > kMaxGridY || (int64_t)B * M > std::numeric_limits<int>::max() / H_kv ||
       (int64_t)B * (M / LLA_PAGE_TOKENS + 2) > kMaxGridX / H_kv || !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) || !std::isfinite(magnitude) ||
       !tables_ok(n_seqs, max_pages, n_pages))
     return LLA_ERR_INVALID_ARG;
   if (!ptr_ok(k) || !ptr_ok(v) || !freq_ok(d_rot, freq) || !idx_ok(table) || !opt_idx_ok(rows) || !idx_ok(start) ||
-      !opt_idx_ok(n_new) || !ptr_ok(k_pages) || !ptr_ok(v_pages))
+      !opt_idx_ok(pos) || !opt_idx_ok(n_new) || !ptr_ok(k_pages) || !ptr_ok(v_pages))
     return LLA_ERR_INVALID_ARG;
   for (int64_t s : {k_b, k_m, v_b, v_m})
     if (!stride_ok(s, dtype)) return LLA_ERR_INVALID_ARG;
@@ -205,6 +214,7 @@ lla_status lla_kv_write(int dtype, int B, int M, int H_kv, int d_head, int d_rot
   a.magnitude = magnitude;
   a.rows = rows;
   a.start = start;
+  a.pos = pos;
   a.n_new = n_new;
   return hip_status(lla::launch_kv_write(a, static_cast<hipStream_t>(stream)));
 }

@@ -41,6 +41,7 @@ struct KvWriteArgs {
   float magnitude;
   const int32_t* rows;
   const int32_t* start;
+  const int32_t* pos;  // NULL: start
   const int32_t* n_new;
 };
 hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t stream);

@@ -14,13 +14,15 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Where the tokens of entry b go: the first position and how many there are.
+// Where the tokens of entry b go: the first place, the position it is turned to, and
+// how many there are.
 struct Entry {
   int row, n;
-  int64_t first;
+  int64_t first, turned;
   __device__ __forceinline__ Entry(const KvWriteArgs& a, int b) {
     row = a.rows ? a.rows[b] : b;
     first = a.start[b];
+    turned = a.pos ? a.pos[b] : first;
     n = a.n_new ? max(0, min(a.n_new[b], a.M)) : a.M;
     if (first < 0 || row < 0 || row >= a.p.n_seqs) n = 0;
   }
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void write_few_kernel(KvWriteArgs a) {
   const int64_t unit = ((int64_t)page * a.p.Hkv + h) * kPage * d;
   if (key) {
     Turn<N> turn;
-    if (p.turned) turn.at((double)pos, freq, a.magnitude, 1.f);
+    if (p.turned) turn.at((double)(e.turned + m), freq, a.magnitude, 1.f);
     p.turn(turn);
     p.store(static_cast<T*>(a.p.k) + unit + t * d);
   } else {
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void write_page_kernel(KvWriteArgs a, int
       if (p.turned) {
         double freq[N];
         p.load_freq(freq, a.freq);
-        t.at((double)(e.first + m0 + i), freq, a.magnitude, 1.f);
+        t.at((double)(e.turned + m0 + i), freq, a.magnitude, 1.f);
       }
       p.turn(t);
       if (page >= 0) p.store_past(kp + i * d);

@@ -32,7 +32,7 @@ import torch
 from . import lla
 from .lla import PAGE, _c_f, _c_i64, _c_int, _c_sz, _c_vp, _check, _dt, _need, _out_code, _ptr
 
-ABI_VERSION = 1  # LLA_KV_ABI_VERSION of include/lla_kv.h this binding follows
+ABI_VERSION = 2  # LLA_KV_ABI_VERSION of include/lla_kv.h this binding follows
 MAX_ROWS = 1024
 PAGES_OK, PAGES_FULL, PAGES_BAD = range(3)  # result[0] of the table calls
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
@@ -44,6 +44,7 @@ _SIGS = {
     "lla_rope_frequencies": [_c_int, _c_d, _c_int, _c_d, _c_d, _c_d, _c_d, _c_vp, ctypes.POINTER(_c_d)],
     "lla_rope_positions": [_c_int] * 8 + _VP + _I64 * 3 + _VP + [_c_int] * 2 + _VP + [_c_f] + _VP + _I64 * 3 + _VP,
     "lla_kv_write": [_c_int] * 7 + (_VP + _I64 * 2) * 2 + _VP + [_c_f] + [_c_int] * 3 + _VP * 7,
+    "lla_kv_write_at": [_c_int] * 7 + (_VP + _I64 * 2) * 2 + _VP + [_c_f] + [_c_int] * 3 + _VP * 8,
     "lla_kv_decode_workspace_bytes": [_c_int] * 8 + [ctypes.POINTER(_c_sz)],
     "lla_kv_decode_attn": [_c_int] * 12 + _VP * 6 + [_c_f] + _VP * 3 + [_c_sz] + _VP,
     "lla_pages_reserve": [_c_int] + _VP * 2 + [_c_int] * 3 + _VP * 8,
@@ -318,7 +319,9 @@ def copy_pages(a, b, pairs, result=None):
 
 def gather(k_pages, v_pages, table, src, dst, keep, n_keep=None):
     """Position i of sequence dst[j] becomes position keep[j, i] of sequence src[j],
-    for i < n_keep[j] (all of keep's columns without n_keep); int32 tensors."""
+    for i < n_keep[j] (all of keep's columns without n_keep); int32 tensors.  Keys
+    stay turned to their old positions, so a length is no position any more: the
+    caller counts all tokens, and gives the count to rope and write as ``pos``."""
     dev = k_pages.device
     layers, P, H, d = _pools(k_pages, v_pages, layered=True)
     n_seqs, max_pages = table.shape
@@ -336,12 +339,13 @@ def gather(k_pages, v_pages, table, src, dst, keep, n_keep=None):
 # Write and attention
 # ---------------------------------------------------------------------------
 
-def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, freq=None, interleaved: bool = False,
-          magnitude: float = 1.0):
+def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, pos=None, freq=None,
+          interleaved: bool = False, magnitude: float = 1.0):
     """Write new tokens k, v [B, M, H_kv, d] (heads and rows dense, B and M of any
     strides) at positions start[b] + m of sequences rows[b] (None: b), m < n_new[b]
     (None: M), into one layer's pools; with freq, keys are turned to their
-    positions as by rope."""
+    positions as by rope, or to pos[b] + m (int32 [B]) where places in the cache
+    are not positions, as after gather."""
     dev = k_pages.device
     _, P, H, d = _pools(k_pages, v_pages)
     ks, vs = _rows_of(k, "k", dev, k_pages.dtype), _rows_of(v, "v", dev, k_pages.dtype)
@@ -354,14 +358,14 @@ def write(k, v, k_pages, v_pages, table, start, *, rows=None, n_new=None, freq=N
     n_seqs, max_pages = table.shape
     for t, name, shape in ((table, "table", (n_seqs, max_pages)), (start, "start", (B,))):
         _ints(t, name, shape, dev)
-    for t, name in ((rows, "rows"), (n_new, "n_new")):
+    for t, name in ((rows, "rows"), (n_new, "n_new"), (pos, "pos")):
         if t is not None:
             _ints(t, name, (B,), dev)
     if rows is None and B > n_seqs:
         raise ValueError("more entries than sequences")
-    _call("lla_kv_write", dev, _dt(k_pages), B, M, H, d, rot, int(interleaved), _ptr(k), *ks[:2], _ptr(v), *vs[:2],
-          _ptr(freq), float(magnitude), n_seqs, max_pages, P, _ptr(table), _ptr(rows), _ptr(start), _ptr(n_new),
-          _ptr(k_pages), _ptr(v_pages))
+    _call("lla_kv_write_at", dev, _dt(k_pages), B, M, H, d, rot, int(interleaved), _ptr(k), *ks[:2], _ptr(v), *vs[:2],
+          _ptr(freq), float(magnitude), n_seqs, max_pages, P, _ptr(table), _ptr(rows), _ptr(start), _ptr(pos),
+          _ptr(n_new), _ptr(k_pages), _ptr(v_pages))
 
 
 def decode_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int, n_ctx: int, sink: int = 0,

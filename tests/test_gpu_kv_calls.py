@@ -8,7 +8,7 @@ import torch
 from oracle import kv_oracle as O
 from paper_2607_15456_amd import kv, lla
 from tests.helpers import f64, log
-from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, check_decode, ints, near, normal, rope_bound, same_tables
+from tests.test_gpu_kv import BF, DEV, EPS, F32, Cache, check_decode, half_step, ints, near, normal, rope_bound, same_tables
 
 pytestmark = pytest.mark.gpu
 
@@ -268,6 +268,82 @@ def test_captured_step_with_padding():
         assert captured[6][0] == 0 and not captured[3][[j for j in range(4) if j not in live]].any(), i
         for mine, its in zip((*captured[4], *captured[5]), (*whole[4], *whole[5])):
             assert torch.equal(mine, its), i
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,inter", [(1, False), (3, True), (70, False)])
+def test_write_turns_to_given_positions(dtype, M, inter):
+    """pos: a token's place in the cache is start + m, its key's angle pos + m; the same as
+    rope to these positions and a write that does not turn."""
+    c, d, Hkv, B = Cache(dtype, [200] * 3, 2, 64, seed=7), 64, 2, 3
+    fused = normal((B, M, 3, Hkv, d), 20, dtype)
+    k, v = fused[:, :, 1], fused[:, :, 2]
+    freq, mag = kv.rope_frequencies(48, scaling="yarn", factor=2.0, original=100)
+    start, pos = [61, 0, -1], [5000, -3, 7]
+    k0, v0 = c.k.clone(), c.v.clone()
+    kv.write(k, v, c.k, c.v, c.table, ints(start), pos=ints(pos), freq=freq, interleaved=inter, magnitude=mag)
+    for b in (0, 1):
+        t = torch.arange(start[b], start[b] + M, device=DEV)
+        page = c.table[b].long()[t // 64]
+        at = np.broadcast_to((pos[b] + np.arange(M))[:, None], (M, Hkv))
+        ref = O.kv_rope(f64(k[b]), at, f64(freq), inter, mag)
+        near(c.k[page, :, t % 64], ref, rope_bound(f64(k[b]), 24, inter, mag, ref, dtype), f"entry {b}")
+        assert torch.equal(c.v[page, :, :, t % 64], v[b])
+        c.k[page, :, t % 64], c.v[page, :, :, t % 64] = k0[page, :, t % 64], v0[page, :, :, t % 64]
+    bits = torch.int16 if dtype == BF else torch.int32
+    assert torch.equal(c.k.view(bits), k0.view(bits)) and torch.equal(c.v.view(bits), v0.view(bits))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("fused", [True, False])
+def test_steps_after_an_eviction(dtype, fused):
+    """After gather keeps a part of a sequence, its next tokens are written behind the
+    kept ones and turned to their true positions (in the write, or by rope before it):
+    attention is the softmax over the kept and the new tokens at the positions they
+    were generated at."""
+    H, Hkv, d, n = 4, 2, 64, 400
+    pages = kv.new_page_table(2, 8, 20)
+    k, v = kv.alloc_pages(20, Hkv, d, dtype)
+    k.fill_(float("nan"))
+    v.fill_(float("nan"))
+    freq, mag = kv.rope_frequencies(d, scaling="yarn", factor=4.0, original=64)
+    start, pairs, result = ints([0]), ints([[0, 0]]), ints([0] * 4)
+    row, other, keys, values = ints([0]), ints([1]), [], []
+
+    def put(x, pos):
+        kv.reserve(pages, row, ints([x.shape[1]]), start, pairs, result)
+        key, val = x[:, :, H:H + Hkv], x[:, :, H + Hkv:]
+        if fused:
+            kv.write(key, val, k, v, pages.table, start, rows=row, pos=ints([pos]), freq=freq, magnitude=mag)
+        else:
+            kv.write(kv.rope(key, freq, pos=ints([pos]), magnitude=mag), val, k, v, pages.table, start, rows=row)
+        at = np.broadcast_to((pos + np.arange(x.shape[1]))[:, None], (x.shape[1], Hkv))
+        keys.extend(O.kv_rope(f64(key[0]), at, f64(freq), magnitude=mag))
+        values.extend(f64(val[0]))
+
+    put(normal((1, n, H + 2 * Hkv, d), 30, dtype), 0)
+    keep = [0, 1] + list(range(100, 300, 7)) + list(range(n - 20, n))
+    kv.fork(pages, row, other, result)
+    kv.free(pages, row, result)
+    kv.reserve(pages, row, ints([len(keep)]), start, pairs, result)
+    kv.gather(k, v, pages.table, other, row, ints([keep]))
+    kv.free(pages, other, result)
+    keys[:], values[:] = [keys[i] for i in keep], [values[i] for i in keep]
+    for step in range(3):
+        pos = n + step
+        x = normal((1, 1, H + 2 * Hkv, d), 31 + step, dtype)
+        put(x, pos)
+        assert int(pages.length[0]) == len(keep) + step + 1 and int(start) == len(keep) + step
+        q = kv.rope(x[:, :, :H], freq, pos=ints([pos]), magnitude=mag)
+        out = f64(kv.decode_attn(q[:, 0].contiguous(), k, v, pages.table, pages.length, rows=row, n_ctx=512))
+        q64 = O.kv_rope(f64(x[0, 0, :H]), np.full(H, pos), f64(freq), magnitude=mag)
+        for h in range(H):
+            kh, vh = np.stack(keys)[:, h // 2], np.stack(values)[:, h // 2]
+            s = kh @ q64[h] / 8
+            p = np.exp(s - s.max()) / np.exp(s - s.max()).sum()
+            # stored keys and queries are rounded once: scores off by 2 * 2^-8 (2^-24) of sum |q k|
+            ds = 2 * (2 * half_step(dtype) + 70 * EPS) * np.max(np.abs(kh) @ np.abs(q64[h])) / 8
+            assert np.all(np.abs(out[0, h] - p @ vh) <= (2 * ds + 1e-5) * (p @ np.abs(vh))), (step, h)
 
 
 def test_positions_past_32_bits_are_refused():

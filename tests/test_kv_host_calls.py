@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2607_15456_amd import kv, lla
+from tests.test_kv_host import CALLS, P
 
 
 def test_numbers_past_32_bits_are_refused():
@@ -33,3 +34,16 @@ def test_a_workspace_serves_smaller_calls(dtype, H, H_kv, d, sink, window):
                 assert need[sizes[i - 1], n] <= need[B, n], (B, n)
             if j:
                 assert need[B, bounds[j - 1]] <= need[B, n], (B, n)
+
+
+def test_write_at_refusals():
+    """lla_kv_write_at is lla_kv_write with positions of its own: the same refusals, and theirs."""
+    good, changes = CALLS["lla_kv_write"]
+    place = list(good).index("start") + 1
+    fn = kv.lib().lla_kv_write_at
+    for arg, value in changes:
+        args = list({**good, arg: value}.values())
+        assert fn(*args[:place], None, *args[place:]) == lla.LLA_ERR_INVALID_ARG, (arg, value)
+        assert fn(*args[:place], P, *args[place:]) == lla.LLA_ERR_INVALID_ARG, (arg, value)
+    args = list(good.values())
+    assert fn(*args[:place], P + 2, *args[place:]) == lla.LLA_ERR_INVALID_ARG
