@@ -172,7 +172,9 @@ hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
 
 template <typename T, bool Interleaved>
 hipError_t launch(const KvWriteArgs& a, hipStream_t stream) {
-  if (sizeof(T) == 2 && a.rot % 16 == 0) return launch<T, 8, Interleaved>(a, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (a.rot % 16 == 0) return launch<T, 8, Interleaved>(a, stream);
+  }
   return launch<T, 4, Interleaved>(a, stream);
 }
 

@@ -102,7 +102,9 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
 template <typename T, bool Interleaved>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
   // pairs of a thread: 16 bytes of each half of a bf16 row where rot/2 allows it
-  if (sizeof(T) == 2 && a.rot % 16 == 0) return launch<T, 8, Interleaved>(a, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (a.rot % 16 == 0) return launch<T, 8, Interleaved>(a, stream);
+  }
   return launch<T, 4, Interleaved>(a, stream);
 }
 

@@ -47,3 +47,10 @@ def test_write_at_refusals():
         assert fn(*args[:place], P, *args[place:]) == lla.LLA_ERR_INVALID_ARG, (arg, value)
     args = list(good.values())
     assert fn(*args[:place], P + 2, *args[place:]) == lla.LLA_ERR_INVALID_ARG
+
+
+def test_no_kernel_is_built_that_nothing_launches():
+    """Eight pairs a thread are for bf16 rows alone."""
+    built = open(lla.LIB_PATH, "rb").read()
+    for kernel in (b"rotary_kernel", b"write_few_kernel", b"write_page_kernel"):
+        assert kernel + b"IfLi4" in built and kernel + b"ItLi8" in built and kernel + b"IfLi8" not in built, kernel
