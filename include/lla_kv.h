@@ -189,6 +189,9 @@ lla_status lla_kv_decode_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  * lse of -inf; another row outside [0, n_seqs), an N outside [0, n_ctx] or a page outside
  * [0, n_pages) among those read gets NaN.  Slots that are not attended may hold anything.
  * Scores times log2(e) have to be finite in 32 bits (or -inf: such a key weighs nothing).
+ * An attended value that is not finite makes its feature's results not finite (NaN or
+ * infinite), and no other feature's.  Sums hold weights of up to 2^8, so finite values
+ * give finite results below 2^120 / N in magnitude.
  * Products of bf16 are exact; the softmax weights enter their product with the
  * values with their 24 bits, as a sum of three bf16.
  * Requires B >= 1, H a multiple of H_kv >= 1, H / H_kv <= 65535, sink >= 0, window >= 0,

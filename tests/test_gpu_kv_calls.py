@@ -87,6 +87,25 @@ def test_decode_of_far_scores(dtype, lengths):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [1, 300, 9000])
+def test_decode_of_infinite_and_large_values(dtype, n):
+    """An attended value that is not finite makes its feature's result not finite and
+    no other; values of 2^100 are averaged as any others."""
+    c = Cache(dtype, [n], 1, 64, seed=3)
+    q = normal((1, 3, 64), 4, dtype)
+    plain = kv.decode_attn(q, c.k, c.v, c.table, c.length, n_ctx=n)
+    v = c.v.clone()
+    page, t = int(c.table[0, (n - 1) // 64]), (n - 1) % 64
+    v[page, 0, 3, t], v[page, 0, 5, t], v[page, 0, 9, t] = float("inf"), -float("inf"), float("nan")
+    out = kv.decode_attn(q, c.k, v, c.table, c.length, n_ctx=n)
+    bad = torch.zeros(64, dtype=torch.bool, device=DEV)
+    bad[[3, 5, 9]] = True
+    assert not torch.isfinite(out[..., bad]).any() and torch.equal(out[..., ~bad], plain[..., ~bad])
+    c.v *= 2.0 ** 100  # (a power of two: the same roundings)
+    assert torch.equal(kv.decode_attn(q, c.k, c.v, c.table, c.length, n_ctx=n), plain * 2.0 ** 100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_decode_workspace_of_the_largest_call_serves_all(dtype):
     """A program's one workspace, for its most entries and longest context, in every
     call below: the same bits as with one of its own."""
