@@ -45,7 +45,7 @@ typedef __amdgpu_buffer_rsrc_t BufRsrc;
 constexpr int kTile = 16;     // columns of a product: query heads
 // Wavefronts of a workgroup, at most: four, so that two workgroups fit a compute
 // unit; up to a width of 64, whose steps are small, eight where no second workgroup comes (24 x 17
-// pages, 8 key heads of 64: 16.0 -> 14.9 us; at 128 no gain, 29.2 -> 29.8 on 4 x 4096).
+// pages, 8 key heads of 64: 16.0 -> 15.1 us; at 128 no gain, 28.8 -> 29.5 on 4 x 4096).
 constexpr int kWaves = 4;
 constexpr int most_waves(int d) { return d <= 64 ? 2 * kWaves : kWaves; }
 constexpr float kLazy = 8.f;  // log2 by which a step may exceed the running maximum
@@ -614,8 +614,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(KvDecodeArgs a) {
 }
 
 // Tiles of a workgroup: two from 17 query heads a group on (16 x 4096 tokens, 8 key
-// heads, bf16, one tile / two: 20 heads a group 94 / 64 us, 64 131 / 115; width 256,
-// 20 heads 184 / 131).
+// heads, bf16, one tile / two: 20 heads a group 92 / 64 us, 64 133 / 115; width 256,
+// 20 heads 187 / 135).
 int query_tiles(int group) { return group > kTile ? 2 : 1; }
 int query_blocks(int group) { return (group + kTile * query_tiles(group) - 1) / (kTile * query_tiles(group)); }
 
@@ -652,16 +652,16 @@ int wave_pages(const KvDecodeArgs& a) { return a.p.dtype == LLA_BF16 ? kWaves : 
 // workgroups, if a slice keeps kLong pages; otherwise one workgroup a unit, since
 // a join costs a launch (4 us) and has to save more.  Measured (width 128, bf16
 // but for the first; unsplit / split, us):
-//   1 x 512 tokens, fp32, 16 key heads 20.8 / 10.6 (a page a slice), bf16 11.7 / 8.6
-//   1 x 32,768, 2 key heads            299 / 15.6 (4 pages; 2 pages 17.6, one 25)
-//   4 x 4096, 16 key heads             49.6 / 29.6 (16 pages; 8 pages 29.1)
-//   24 of 17 pages, 8 key heads of 64  16.2 / 18.6
+//   1 x 512 tokens, fp32, 16 key heads 21.5 / 10.9 (a page a slice), bf16 11.7 / 8.5
+//   1 x 32,768, 2 key heads            312 / 15.9 (4 pages; 2 pages 17.9)
+//   4 x 4096, 16 key heads             48.3 / 28.8 (16 pages; 8 pages 29.4)
+//   24 of 17 pages, 8 key heads of 64  15.1 / 19.7
 // and of 128 KB of keys and values or less, 8 wavefronts to a workgroup from 9 steps on:
-//   512 tokens, 8 key heads of 64, bf16 1 x 7.5 / 7.6, 16 x 8.4 / 11.2, 320 tokens 6.9 / 7.5
-//   1 x 512, 700, 1024, 8 of 32, bf16  5.8, 6.9, 7.1 / 7.3, 8.0, 7.4
-//   256 tokens, 8 of 64, fp32          4 x 8.2 / 9.0
-//   20 x 1024 .. 4096, 16 key heads    89 / 80;  12 x 2250 .. 9000, 8 key heads 100 / 59
-//   40 x 4096, 16 key heads (640 workgroups) 209 / 208 .. 214
+//   512 tokens, 8 key heads of 64, bf16 1 x 7.7 / 7.6, 16 x 8.7 / 10.8, 320 tokens 7.3 / 7.7
+//   1 x 512, 700, 1024, 8 of 32, bf16  5.9, 7.0, 7.5 / 7.6, 8.4, 7.8
+//   256 tokens, 8 of 64, fp32          4 x 8.4 / 9.1
+//   20 x 1024 .. 4096, 16 key heads    88 / 80;  12 x 2250 .. 9000, 8 key heads 102 / 59
+//   40 x 4096, 16 key heads (640 workgroups) 219 / 218
 int most_slices(const KvDecodeArgs& a, int units, int pages, int cus) {
   constexpr int kLong = 16, kAlone = 128 << 10;
   // a step a wavefront; of narrow heads, what eight wavefronts read in two steps or less

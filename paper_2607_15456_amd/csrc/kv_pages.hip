@@ -5,9 +5,9 @@
 // rows' needs are a prefix sum, so the outcome is that of one row after another
 // in any run, with no lock and no order of atomics that shows.  They move a few
 // words a page; a launch and a chain of dependent reads bound them (16 rows of 36
-// pages dropped, forked and given room: 16.5 us for the three calls, 256 rows 71),
-// for thousands of pages the scattered words that one compute unit can ask for
-// (1000 rows of 32 pages 420).
+// pages dropped, forked and given room: 16.9 us for the three calls), for thousands of
+// pages the scattered words that one compute unit can ask for and the search for rows
+// named twice, n^2 / 2 reads of LDS (256 rows of 36 pages 121, 1000 of 30 437).
 
 #include "kv_internal.h"
 #include "lla_device.h"
@@ -294,9 +294,9 @@ __global__ __launch_bounds__(kThreads) void free_kernel(TableArgs a) {
 constexpr int kCopyThreads = 256;
 typedef unsigned int Words4 __attribute__((ext_vector_type(4)));
 
-// 768 pages of 524 KB (24 layers, 32 pairs, keys and values) in 108 us, 7.4 TB/s of
-// reads and writes, part of them held by the last-level cache; one workgroup a page
-// 180.  A workgroup copies kCopyBytes of one page of one layer (blockIdx.x: pair
+// 768 pages of 524 KB (24 layers, 32 pairs, keys and values) in 80 us, 108 where the
+// last-level cache holds others' lines (7.4 TB/s of reads and writes, 8 pages read by 4
+// pairs each); one workgroup a page 180.  A workgroup copies kCopyBytes of one page of one layer (blockIdx.x: pair
 // and piece of both pools' pages, blockIdx.y: layer).
 constexpr int kCopyRun = 2, kCopyBytes = kCopyRun * kCopyThreads * 16;
 __global__ __launch_bounds__(kCopyThreads) void copy_kernel(PageCopyArgs a, int pieces, int pieces_a) {
