@@ -50,8 +50,8 @@
 extern "C" {
 #endif
 
-#define LLA_KV_ABI_VERSION 2
-#define LLA_KV_MAX_ROWS 1024 /* sequences of one reserve, fork or free */
+#define LLA_KV_ABI_VERSION 3
+#define LLA_KV_MAX_ROWS 1024 /* sequences of one reserve, fork or free; entries of a packed or shared batch */
 #define LLA_KV_MAX_ROW 512   /* widest row of lla_rope_positions */
 
 /* How rotary frequencies are scaled for contexts past the trained length. */
@@ -286,6 +286,136 @@ lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, i
                          int max_pages, int n_pages, const int32_t* table, const int32_t* src,
                          const int32_t* dst, const int32_t* keep, const int32_t* n_keep,
                          void* k_pages, void* v_pages, void* stream);
+
+/*
+ * Packed batches.  The tokens of B <= LLA_KV_MAX_ROWS entries, n_new[b] each, lie one
+ * after another in `total` packed rows: entry b's are offset[b] .. offset[b+1] - 1, at
+ * places start[b], start[b] + 1, .. of sequence rows[b] (NULL: sequence b), as
+ * lla_pages_reserve gives them.  total is the rows that there is room for, so a
+ * captured step serves fewer tokens; rows from offset[B] on belong to nobody.
+ */
+
+/*
+ * Offsets, entries, positions and slots of packed tokens, from request lengths:
+ *   offset[b] = min(total, sum of max(0, n_new[i]) over i < b), b = 0 .. B
+ * and for token i of entry b, t = offset[b] + i:
+ *   entry[t] = b,  pos[t] = pos0[b] + i (pos0 NULL: start),
+ *   slot[t] = 64 * page + (start[b] + i) % 64, in the page of that place.
+ * Where start[b] < 0 (a refused or padding row), pos and slot are -1; slot is -1, too,
+ * where the row is outside [0, n_seqs), the place 64*max_pages or more, or the page
+ * outside [0, n_pages), and pos where it is not in [0, 2^31).  Tokens from offset[B] on
+ * get -1 in all three.
+ *   rows, pos0  int32 [B] or NULL;  start, n_new  int32 [B]
+ *   offset  int32 [B + 1];  entry, pos  int32 [total];  slot  int64 [total], 8-byte aligned
+ * Requires 1 <= B <= LLA_KV_MAX_ROWS, 1 <= total < 2^24.
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
+ */
+lla_status lla_kv_slots(int B, int total, int n_seqs, int max_pages, int n_pages, const int32_t* table,
+                        const int32_t* rows, const int32_t* start, const int32_t* pos0,
+                        const int32_t* n_new, int32_t* offset, int32_t* entry, int32_t* pos,
+                        int64_t* slot, void* stream);
+
+/*
+ * Write packed keys and values to their slots: token t's go to place slot[t] % 64 of
+ * page slot[t] / 64, its key turned to position pos[t] as by lla_rope_positions
+ * (d_rot = 0: not turned; freq is then NULL and pos may be).
+ *   k, v    [total][H_kv][d_head], heads and features dense, strides k_t, v_t in elements
+ *           (multiples of 16 bytes)
+ * Tokens with a slot outside [0, 64*n_pages) are not written, other slots are not
+ * touched.  Pages written must have one holder, and a slot must occur once in a call.
+ * Requires total >= 1, 1 <= H_kv <= 65535, (total/64 + 1)*H_kv < 2^24; d_rot as above, or 0.
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
+ */
+lla_status lla_kv_write_slots(int dtype, int total, int H_kv, int d_head, int d_rot, int interleaved,
+                              const void* k, int64_t k_t, const void* v, int64_t v_t,
+                              const double* freq, float magnitude, int n_pages, const int64_t* slot,
+                              const int32_t* pos, void* k_pages, void* v_pages, void* stream);
+
+/* Workspace bytes that serve lla_kv_prefill_attn for every batch of up to B entries,
+ * total tokens and a bound of n_ctx (other arguments the same) on the current device.
+ * Host only.
+ * Errors: LLA_ERR_INVALID_ARG. */
+lla_status lla_kv_prefill_workspace_bytes(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head,
+                                          int n_ctx, int sink, int window, size_t* bytes);
+
+/*
+ * Causal attention of packed tokens over the paged cache: token i of entry b, at place
+ * p = start[b] + i of sequence rows[b], attends the places n <= p, and with window > 0
+ * of these only n < sink and n > p - window; query head h reads key head h / (H / H_kv).
+ * Its own key and value must have been written.  Prompts, pieces of prompts, drafts and
+ * single tokens may stand in one batch.
+ *
+ *   q       [total][H][d_head], heads and features dense, stride q_t in elements (a
+ *           multiple of 16 bytes): a slice of a fused projection's rows can be passed
+ *   offset  int32 [B + 1], not decreasing (lla_kv_slots); start  int32 [B]
+ *   n_ctx   upper bound of the places, in [1, 64*max_pages]
+ *   scale   as for lla_kv_decode_attn
+ *   out     [total][H][d_head] of out_dtype
+ *   lse     NULL, or float [total][H]: the natural logarithm of sum_n exp(s_n)
+ *   workspace  device memory of ws_bytes >= lla_kv_prefill_workspace_bytes(), as for
+ *           lla_kv_decode_attn
+ * Tokens of an entry with rows[b] = -1 or start[b] < 0 get zeros and an lse of -inf;
+ * tokens of another row outside [0, n_seqs), at a place of n_ctx or more, or that attend
+ * a page outside [0, n_pages) get NaN.  Rows of out and lse that are no entry's are not
+ * touched.  What slots after a token hold does not matter to it, in the values of other
+ * tokens of its batch too: values that are not finite make results not finite (NaN
+ * or infinite) of the tokens that attend them, in their own feature.
+ * bf16: products are exact; with out_dtype LLA_F32 the softmax weights enter their
+ * product with the values with their 24 bits; with LLA_BF16 they are rounded to bf16, and
+ * summed as rounded (a weight is off by at most 2^-8 of itself, their sum not at all).
+ * Requires 1 <= B <= LLA_KV_MAX_ROWS, 1 <= total < 2^24, H a multiple of H_kv >= 1,
+ * total*H < 2^31, sink >= 0, window >= 0, sink = 0 without a window.
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
+ */
+lla_status lla_kv_prefill_attn(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head, int n_seqs,
+                               int max_pages, int n_pages, int n_ctx, int sink, int window,
+                               const int32_t* table, const int32_t* rows, const int32_t* offset,
+                               const int32_t* start, const void* q, int64_t q_t, const void* k_pages,
+                               const void* v_pages, float scale, void* out, float* lse,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Which neighbours among the entries rows[b] (NULL: sequence b) share leading pages:
+ * entry b joins the group of b - 1 when both read the same pages at their first
+ * c >= least places (c counts no place past either's length).  For all entries of a
+ * group, lead[b] is its first entry and shared[b] the least c of its joins; an entry
+ * alone has lead[b] = b and shared[b] = 0.  Sequences that lla_pages_fork made share the
+ * pages that they had, until lla_pages_reserve gives one a copy of its last.
+ *   rows  int32 [B] or NULL (-1 or out of range: joins nobody);  length  int32 [n_seqs]
+ *   lead, shared  int32 [B]
+ * Requires 1 <= B <= LLA_KV_MAX_ROWS, least >= 1.
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_HIP.
+ */
+lla_status lla_pages_shared(int B, int least, const int32_t* rows, int n_seqs, int max_pages, int n_pages,
+                            const int32_t* table, const int32_t* length, int32_t* lead, int32_t* shared,
+                            void* stream);
+
+/* Workspace bytes that serve lla_kv_decode_attn_shared for every batch of up to B
+ * entries and a bound of n_ctx (other arguments the same) on the current device.  Host
+ * only.
+ * Errors: LLA_ERR_INVALID_ARG. */
+lla_status lla_kv_shared_workspace_bytes(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, size_t* bytes);
+
+/*
+ * lla_kv_decode_attn for entries of which neighbours share a long prompt: the keys and
+ * values of entry b's places below shared[b] are those of entry lead[b], are read
+ * through that entry's pages, and once for all neighbours with the same lead and shared;
+ * the places from shared[b] to its length through its own pages.  (lla_pages_shared
+ * finds both; a program that knows its prompts may give other numbers, down to a place
+ * inside a page.)  Arguments and results are otherwise those of lla_kv_decode_attn without
+ * a window.
+ *   lead, shared  int32 [B]
+ * An entry with shared[b] < 0 or above its length, or with shared[b] > 0 and a lead[b]
+ * outside [0, B), whose row is out of range, or that has fewer places, gets NaN.
+ * Requires 1 <= B <= LLA_KV_MAX_ROWS, and as lla_kv_decode_attn.
+ * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
+ */
+lla_status lla_kv_decode_attn_shared(int dtype, int out_dtype, int B, int H, int H_kv, int d_head, int n_seqs,
+                                     int max_pages, int n_pages, int n_ctx, const int32_t* table,
+                                     const int32_t* length, const int32_t* rows, const int32_t* lead,
+                                     const int32_t* shared, const void* q, const void* k_pages,
+                                     const void* v_pages, float scale, void* out, float* lse,
+                                     void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

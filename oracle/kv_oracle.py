@@ -154,3 +154,87 @@ class KvTables:
             self.length[r] = 0
         self.free += back[::-1]
         return OK
+
+
+# ---------------------------------------------------------------------------
+# packed batches and shared prompts
+# ---------------------------------------------------------------------------
+
+def kv_slots(table, start, n_new, total, n_pages, rows=None, pos0=None):
+    """(offset, entry, pos, slot) of packed tokens, one token after another."""
+    offset, entry, pos, slot = [0], [-1] * total, [-1] * total, [-1] * total
+    t = 0
+    for b, n in enumerate(n_new):
+        row = b if rows is None else rows[b]
+        for i in range(max(0, n)):
+            if t == total:
+                break
+            entry[t] = b
+            if start[b] >= 0:
+                place, turned = start[b] + i, (start[b] if pos0 is None else pos0[b]) + i
+                if 0 <= turned < 2 ** 31:
+                    pos[t] = turned
+                if 0 <= row < len(table) and place < PAGE * len(table[0]) and 0 <= table[row][place // PAGE] < n_pages:
+                    slot[t] = PAGE * table[row][place // PAGE] + place % PAGE
+            t += 1
+        offset.append(t)
+    return offset, entry, pos, slot
+
+
+def kv_shared_prefix(table, length, n_pages, rows=None, least=1):
+    """(lead, shared): runs of neighbours with the same leading pages."""
+    rows = list(range(len(table))) if rows is None else rows
+    lead, shared, groups = [], [], []
+
+    def held(r):
+        return min(length[r], PAGE * len(table[r])) if 0 <= r < len(table) else 0
+
+    for b, r in enumerate(rows):
+        c = 0
+        if b and held(r) and held(rows[b - 1]):
+            x, y = table[r], table[rows[b - 1]]
+            c = min(held(r), held(rows[b - 1]))
+            if r != rows[b - 1]:
+                for i in range(-(-c // PAGE)):
+                    if x[i] != y[i] or not 0 <= x[i] < n_pages:
+                        c = min(c, PAGE * i)
+                        break
+        if c >= least:
+            groups[-1].append(c)
+        else:
+            groups.append([b])
+    for g in groups:
+        lead += [g[0]] * len(g)
+        shared += [min(g[1:], default=0)] * len(g)
+    return lead, shared
+
+
+def kv_prefill_seen(p, sink=0, window=0):
+    """Places that the token at place p attends."""
+    return [n for n in range(p + 1) if not window or n < sink or n > p - window]
+
+
+def kv_prefill_attn(q, k_pages, v_pages, table, offset, start, rows=None, scale=None, sink=0, window=0):
+    """(out [total, H, d], lse [total, H]) of packed tokens; NaN in rows that are no
+    entry's, zeros and -inf in those of padding."""
+    total, H, d = q.shape
+    group = H // k_pages.shape[1]
+    out, lse = np.full((total, H, d), np.nan), np.full((total, H), np.nan)
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    for b in range(len(start)):
+        row = b if rows is None else rows[b]
+        for t in range(offset[b], offset[b + 1]):
+            if row < 0 or start[b] < 0:
+                out[t], lse[t] = 0.0, -np.inf
+                continue
+            at = kv_prefill_seen(start[b] + t - offset[b], sink, window)
+            pages, slots = np.array([table[row][n // PAGE] for n in at]), np.array([n % PAGE for n in at])
+            for g in range(k_pages.shape[1]):
+                k, v = k_pages[pages, g, slots], v_pages[pages, g, :, slots]
+                hs = slice(g * group, (g + 1) * group)
+                s = q[t, hs] @ k.T * scale
+                m = s.max(axis=1, keepdims=True)
+                p = np.exp(s - m)
+                out[t, hs] = p @ v / p.sum(axis=1, keepdims=True)
+                lse[t, hs] = m[:, 0] + np.log(p.sum(axis=1))
+    return out, lse

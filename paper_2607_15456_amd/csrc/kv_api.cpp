@@ -73,6 +73,31 @@ lla::KvDecodeArgs decode_args(int dtype, int B, int H, int H_kv, int d_head, int
   return a;
 }
 
+bool slot_ok(const int64_t* p) { return p && (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+bool scale_ok(float scale) { return std::isfinite((float)(scale * kLog2e)) && scale > 0.f; }
+bool workspace_ok(const void* p, size_t bytes, size_t need) {
+  return (p == nullptr) == (bytes == 0) && bytes >= need && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+}
+bool packed_ok(int dtype, int B, int total, int H, int H_kv, int d_head, int n_ctx, int sink, int window) {
+  return decode_ok(dtype, 1, H, H_kv, d_head, n_ctx, sink, window) && B >= 1 && B <= LLA_KV_MAX_ROWS && total >= 1 &&
+         total <= kMaxGridX && total <= std::numeric_limits<int>::max() / H;
+}
+lla::KvTileArgs tile_args(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head, int n_ctx, int sink,
+                          int window) {
+  lla::KvTileArgs a{};
+  a.p.dtype = dtype;
+  a.p.Hkv = H_kv;
+  a.p.d = d_head;
+  a.out_dtype = out_dtype;
+  a.B = B;
+  a.total = total;
+  a.H = H;
+  a.n_ctx = n_ctx;
+  a.sink = sink;
+  a.window = window;
+  return a;
+}
+
 lla::TableArgs table_args(int n, const int32_t* rows, int n_seqs, int max_pages, int n_pages, int32_t* table,
                           int32_t* length, int32_t* refs, int32_t* free_pages, int32_t* result) {
   lla::TableArgs a{};
@@ -332,6 +357,126 @@ lla_status lla_kv_gather(int dtype, int B, int max_keep, int layers, int H_kv, i
   a.keep = keep;
   a.n_keep = n_keep;
   return hip_status(lla::launch_kv_gather(a, static_cast<hipStream_t>(stream)));
+}
+
+lla_status lla_kv_slots(int B, int total, int n_seqs, int max_pages, int n_pages, const int32_t* table,
+                        const int32_t* rows, const int32_t* start, const int32_t* pos0,
+                        const int32_t* n_new, int32_t* offset, int32_t* entry, int32_t* pos,
+                        int64_t* slot, void* stream) {
+  if (B < 1 || B > LLA_KV_MAX_ROWS || total < 1 || total > kMaxGridX || !tables_ok(n_seqs, max_pages, n_pages))
+    return LLA_ERR_INVALID_ARG;
+  if (!idx_ok(table) || !opt_idx_ok(rows) || !idx_ok(start) || !opt_idx_ok(pos0) || !idx_ok(n_new) || !idx_ok(offset) ||
+      !idx_ok(entry) || !idx_ok(pos) || !slot_ok(slot))
+    return LLA_ERR_INVALID_ARG;
+  const lla::KvSlotsArgs a{B, total, n_seqs, max_pages, n_pages, table, rows, start, pos0, n_new, offset, entry, pos, slot};
+  return hip_status(lla::launch_kv_slots(a, static_cast<hipStream_t>(stream)));
+}
+
+lla_status lla_kv_write_slots(int dtype, int total, int H_kv, int d_head, int d_rot, int interleaved,
+                              const void* k, int64_t k_t, const void* v, int64_t v_t,
+                              const double* freq, float magnitude, int n_pages, const int64_t* slot,
+                              const int32_t* pos, void* k_pages, void* v_pages, void* stream) {
+  if (!dtype_ok(dtype) || total < 1 || H_kv < 1 || H_kv > kMaxGridY ||
+      total / LLA_PAGE_TOKENS + 1 > kMaxGridX / H_kv || !head_ok(d_head) || (d_rot && !rot_ok(d_rot, d_head)) ||
+      !std::isfinite(magnitude) || n_pages < 1 || n_pages > kMaxPool)
+    return LLA_ERR_INVALID_ARG;
+  if (!ptr_ok(k) || !ptr_ok(v) || !freq_ok(d_rot, freq) || !slot_ok(slot) || !(d_rot ? idx_ok(pos) : opt_idx_ok(pos)) ||
+      !ptr_ok(k_pages) || !ptr_ok(v_pages) || !stride_ok(k_t, dtype) || !stride_ok(v_t, dtype))
+    return LLA_ERR_INVALID_ARG;
+  lla::KvWriteSlotsArgs a{};
+  a.p = {dtype, H_kv, d_head, 0, 0, n_pages, nullptr, k_pages, v_pages};
+  a.total = total;
+  a.rot = d_rot;
+  a.interleaved = interleaved != 0;
+  a.k = k;
+  a.v = v;
+  a.kt = k_t;
+  a.vt = v_t;
+  a.freq = freq;
+  a.magnitude = magnitude;
+  a.pos = pos;
+  a.slot = slot;
+  return hip_status(lla::launch_kv_write_slots(a, static_cast<hipStream_t>(stream)));
+}
+
+lla_status lla_kv_prefill_workspace_bytes(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head,
+                                          int n_ctx, int sink, int window, size_t* bytes) {
+  if (!packed_ok(dtype, B, total, H, H_kv, d_head, n_ctx, sink, window) || !dtype_ok(out_dtype) || !bytes)
+    return LLA_ERR_INVALID_ARG;
+  *bytes = lla::kv_prefill_workspace(tile_args(dtype, out_dtype, B, total, H, H_kv, d_head, n_ctx, sink, window));
+  return LLA_OK;
+}
+
+lla_status lla_kv_prefill_attn(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head, int n_seqs,
+                               int max_pages, int n_pages, int n_ctx, int sink, int window,
+                               const int32_t* table, const int32_t* rows, const int32_t* offset,
+                               const int32_t* start, const void* q, int64_t q_t, const void* k_pages,
+                               const void* v_pages, float scale, void* out, float* lse,
+                               void* workspace, size_t ws_bytes, void* stream) {
+  if (!packed_ok(dtype, B, total, H, H_kv, d_head, n_ctx, sink, window) || !dtype_ok(out_dtype) ||
+      !tables_ok(n_seqs, max_pages, n_pages) || n_ctx > (int64_t)max_pages * LLA_PAGE_TOKENS || !scale_ok(scale) ||
+      !stride_ok(q_t, dtype))
+    return LLA_ERR_INVALID_ARG;
+  if (!idx_ok(table) || !opt_idx_ok(rows) || !idx_ok(offset) || !idx_ok(start) || !ptr_ok(q) || !ptr_ok(k_pages) ||
+      !ptr_ok(v_pages) || !ptr_ok(out) || !opt_idx_ok(lse))
+    return LLA_ERR_INVALID_ARG;
+  lla::KvTileArgs a = tile_args(dtype, out_dtype, B, total, H, H_kv, d_head, n_ctx, sink, window);
+  if (!workspace_ok(workspace, ws_bytes, lla::kv_prefill_shape(a))) return LLA_ERR_WORKSPACE;
+  a.p = {dtype, H_kv, d_head, n_seqs, max_pages, n_pages, table, const_cast<void*>(k_pages), const_cast<void*>(v_pages)};
+  a.rows = rows;
+  a.offset = offset;
+  a.start = start;
+  a.q = q;
+  a.q_t = q_t;
+  a.qscale = (float)((double)scale * kLog2e);
+  a.out = out;
+  a.lse = lse;
+  a.small_part = static_cast<float*>(workspace);
+  return hip_status(lla::launch_kv_prefill(a, static_cast<hipStream_t>(stream)));
+}
+
+lla_status lla_pages_shared(int B, int least, const int32_t* rows, int n_seqs, int max_pages, int n_pages,
+                            const int32_t* table, const int32_t* length, int32_t* lead, int32_t* shared,
+                            void* stream) {
+  if (B < 1 || B > LLA_KV_MAX_ROWS || least < 1 || !tables_ok(n_seqs, max_pages, n_pages) || !opt_idx_ok(rows) ||
+      !idx_ok(table) || !idx_ok(length) || !idx_ok(lead) || !idx_ok(shared))
+    return LLA_ERR_INVALID_ARG;
+  const lla::PagesSharedArgs a{B, least, n_seqs, max_pages, n_pages, table, length, rows, lead, shared};
+  return hip_status(lla::launch_pages_shared(a, static_cast<hipStream_t>(stream)));
+}
+
+lla_status lla_kv_shared_workspace_bytes(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, size_t* bytes) {
+  if (!packed_ok(dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0) || !bytes) return LLA_ERR_INVALID_ARG;
+  *bytes = lla::kv_shared_workspace(tile_args(dtype, dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0));
+  return LLA_OK;
+}
+
+lla_status lla_kv_decode_attn_shared(int dtype, int out_dtype, int B, int H, int H_kv, int d_head, int n_seqs,
+                                     int max_pages, int n_pages, int n_ctx, const int32_t* table,
+                                     const int32_t* length, const int32_t* rows, const int32_t* lead,
+                                     const int32_t* shared, const void* q, const void* k_pages,
+                                     const void* v_pages, float scale, void* out, float* lse,
+                                     void* workspace, size_t ws_bytes, void* stream) {
+  if (!packed_ok(dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0) || !dtype_ok(out_dtype) ||
+      !tables_ok(n_seqs, max_pages, n_pages) || n_ctx > (int64_t)max_pages * LLA_PAGE_TOKENS || !scale_ok(scale))
+    return LLA_ERR_INVALID_ARG;
+  if (!idx_ok(table) || !idx_ok(length) || !opt_idx_ok(rows) || !idx_ok(lead) || !idx_ok(shared) || !ptr_ok(q) ||
+      !ptr_ok(k_pages) || !ptr_ok(v_pages) || !ptr_ok(out) || !opt_idx_ok(lse))
+    return LLA_ERR_INVALID_ARG;
+  lla::KvTileArgs a = tile_args(dtype, out_dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0);
+  if (!workspace_ok(workspace, ws_bytes, lla::kv_shared_shape(a))) return LLA_ERR_WORKSPACE;
+  a.p = {dtype, H_kv, d_head, n_seqs, max_pages, n_pages, table, const_cast<void*>(k_pages), const_cast<void*>(v_pages)};
+  a.rows = rows;
+  a.length = length;
+  a.lead = lead;
+  a.shared = shared;
+  a.q = q;
+  a.q_t = (int64_t)H * d_head;
+  a.qscale = (float)((double)scale * kLog2e);
+  a.out = out;
+  a.lse = lse;
+  a.small_part = static_cast<float*>(workspace);
+  return hip_status(lla::launch_kv_shared(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -68,6 +68,84 @@ size_t kv_decode_shape(KvDecodeArgs& a);
 // The most that it takes for any B and n_ctx up to a's.
 size_t kv_decode_workspace(const KvDecodeArgs& a);
 
+// Attention of packed tokens (offset, start), and of entries that share a prompt
+// (length, lead, shared), over the pages.
+struct KvTileArgs {
+  KvPages p;
+  int out_dtype, B, total, H;
+  int n_ctx, sink, window;
+  const int32_t* rows;
+  const int32_t* offset;
+  const int32_t* start;
+  const int32_t* length;
+  const int32_t* lead;
+  const int32_t* shared;
+  const void* q;
+  int64_t q_t;  // elements from one token's (entry's) queries to the next
+  float qscale;
+  void* out;
+  float* lse;
+  // slices of a tile at most, and pages of a slice at least
+  int most, least;
+  // workgroups that small tiles and large ones are shared out to
+  int small_wgs, large_wgs;
+  // rows of a packed entry up to which it is of small tiles
+  int small_rows;
+  // slices that an entry's own tokens are cut into, at most
+  int own_slices;
+  float* small_part;
+  float* large_part;
+  float* own_part;
+};
+// Choose how the work is cut; return the workspace bytes that this takes.
+size_t kv_prefill_shape(KvTileArgs& a);
+size_t kv_shared_shape(KvTileArgs& a);
+// The most that it takes for any smaller call.
+size_t kv_prefill_workspace(const KvTileArgs& a);
+size_t kv_shared_workspace(const KvTileArgs& a);
+hipError_t launch_kv_prefill(const KvTileArgs& a, hipStream_t stream);
+hipError_t launch_kv_shared(const KvTileArgs& a, hipStream_t stream);
+
+// Offsets, entries, positions and slots of packed tokens.
+struct KvSlotsArgs {
+  int B, total, n_seqs, max_pages, n_pages;
+  const int32_t* table;
+  const int32_t* rows;
+  const int32_t* start;
+  const int32_t* pos0;  // NULL: start
+  const int32_t* n_new;
+  int32_t* offset;
+  int32_t* entry;
+  int32_t* pos;
+  int64_t* slot;
+};
+hipError_t launch_kv_slots(const KvSlotsArgs& a, hipStream_t stream);
+
+// Groups of neighbouring entries with the same leading pages.
+struct PagesSharedArgs {
+  int B, least, n_seqs, max_pages, n_pages;
+  const int32_t* table;
+  const int32_t* length;
+  const int32_t* rows;
+  int32_t* lead;
+  int32_t* shared;
+};
+hipError_t launch_pages_shared(const PagesSharedArgs& a, hipStream_t stream);
+
+// Keys and values of packed tokens to their slots.
+struct KvWriteSlotsArgs {
+  KvPages p;  // (without a table)
+  int total, rot, interleaved;
+  const void* k;
+  const void* v;
+  int64_t kt, vt;
+  const double* freq;
+  float magnitude;
+  const int32_t* pos;
+  const int64_t* slot;
+};
+hipError_t launch_kv_write_slots(const KvWriteSlotsArgs& a, hipStream_t stream);
+
 struct TableArgs {
   int n, n_seqs, max_pages, n_pages;
   const int32_t* rows;

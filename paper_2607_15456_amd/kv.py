@@ -32,7 +32,7 @@ import torch
 from . import lla
 from .lla import PAGE, _c_f, _c_i64, _c_int, _c_sz, _c_vp, _check, _dt, _need, _out_code, _ptr
 
-ABI_VERSION = 2  # LLA_KV_ABI_VERSION of include/lla_kv.h this binding follows
+ABI_VERSION = 3  # LLA_KV_ABI_VERSION of include/lla_kv.h this binding follows
 MAX_ROWS = 1024
 PAGES_OK, PAGES_FULL, PAGES_BAD = range(3)  # result[0] of the table calls
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
@@ -52,6 +52,13 @@ _SIGS = {
     "lla_pages_free": [_c_int] + _VP + [_c_int] * 3 + _VP * 6,
     "lla_pages_copy": [_c_int] * 2 + (_VP + _I64) * 2 + _VP + [_c_int] + _VP * 2,
     "lla_kv_gather": [_c_int] * 9 + _VP * 8,
+    "lla_kv_slots": [_c_int] * 5 + _VP * 10,
+    "lla_kv_write_slots": [_c_int] * 6 + (_VP + _I64) * 2 + _VP + [_c_f, _c_int] + _VP * 5,
+    "lla_kv_prefill_workspace_bytes": [_c_int] * 10 + [ctypes.POINTER(_c_sz)],
+    "lla_kv_prefill_attn": [_c_int] * 13 + _VP * 5 + _I64 + _VP * 2 + [_c_f] + _VP * 3 + [_c_sz] + _VP,
+    "lla_pages_shared": [_c_int] * 2 + _VP + [_c_int] * 3 + _VP * 5,
+    "lla_kv_shared_workspace_bytes": [_c_int] * 6 + [ctypes.POINTER(_c_sz)],
+    "lla_kv_decode_attn_shared": [_c_int] * 10 + _VP * 8 + [_c_f] + _VP * 3 + [_c_sz] + _VP,
 }
 
 _lib = None
@@ -420,4 +427,229 @@ def decode_attn(q, k_pages, v_pages, table, length, *, n_ctx: int, rows=None, sc
     _call("lla_kv_decode_attn", dev, _dt(q), _out_code(out.dtype), B, H, Hkv, d, n_seqs, max_pages, P, n_ctx, sink,
           window, _ptr(table), _ptr(length), _ptr(rows), _ptr(q), _ptr(k_pages), _ptr(v_pages),
           float(1.0 / math.sqrt(d) if scale is None else scale), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Packed batches
+# ---------------------------------------------------------------------------
+
+class Slots(NamedTuple):
+    """Where the packed tokens of a batch belong: the first token of every entry and
+    their number, then of every token its entry, its position and its slot
+    (64 * page + place); -1 where there is none."""
+    offset: torch.Tensor   # int32 [B + 1]
+    entry: torch.Tensor    # int32 [total]
+    pos: torch.Tensor      # int32 [total]
+    slot: torch.Tensor     # int64 [total]
+
+
+def new_slots(B: int, total: int, device="cuda") -> Slots:
+    """Uninitialised maps of B entries and total tokens."""
+    ints = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=device)  # noqa: E731
+    return Slots(ints(B + 1), ints(total), ints(total), ints(total, torch.int64))
+
+
+def slots(pages: PageTable, start, n_new, total: int, *, rows=None, pos=None, out: Slots | None = None) -> Slots:
+    """The maps of a packed batch from request lengths: n_new[b] tokens of sequence
+    rows[b] (None: b) at places start[b] on, as reserve gives them, one entry after
+    another in ``total`` packed rows.  pos (int32 [B], None: start): the position of an
+    entry's first token where places are not positions, as after gather."""
+    dev, B = start.device, start.numel()
+    sizes = _page_table(pages, dev)
+    _whole(total, "total")
+    for t, name, shape in ((start, "start", (B,)), (n_new, "n_new", (B,))):
+        _ints(t, name, shape, dev)
+    for t, name in ((rows, "rows"), (pos, "pos")):
+        if t is not None:
+            _ints(t, name, (B,), dev)
+    if rows is None and B > sizes[0]:
+        raise ValueError("more entries than sequences")
+    if out is None:
+        out = new_slots(B, max(total, 0), dev)
+    else:
+        for t, name, shape in ((out.offset, "offset", (B + 1,)), (out.entry, "entry", (total,)), (out.pos, "pos", (total,))):
+            _ints(t, name, shape, dev)
+        _longs(out.slot, "slot", (total,), dev)
+    _call("lla_kv_slots", dev, B, total, *sizes, _ptr(pages.table), _ptr(rows), _ptr(start), _ptr(pos), _ptr(n_new),
+          *map(_ptr, out))
+    return out
+
+
+def _longs(t, name, shape, dev):
+    _need(t, name, torch.int64, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}")
+
+
+def _packed(t, name, heads, d, dtype, dev):
+    """Stride of tokens of t [total, heads, d], heads and rows dense."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [total, heads, width]")
+    _, stride, head = _rows_of(t[None], name, dev, dtype)
+    if t.shape[1:] != (heads, d) or heads > 1 and head != d:
+        raise ValueError(f"{name} must be [total, {heads}, {d}] with dense heads")
+    return stride
+
+
+def _no_gradient(*tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("no gradient passes through the cache; call under torch.no_grad()")
+
+
+def write_slots(k, v, k_pages, v_pages, slot, *, pos=None, freq=None, interleaved: bool = False,
+                magnitude: float = 1.0):
+    """Write packed k, v [total, H_kv, d] (heads and rows dense) to slot[t] (int64
+    [total]) of one layer's pools; with freq, keys are turned to pos[t] (int32 [total])
+    as by rope.  Tokens with a slot of -1 are not written."""
+    dev = k_pages.device
+    _, P, H, d = _pools(k_pages, v_pages)
+    _no_gradient(k, v, k_pages, v_pages, freq)
+    kt, vt = _packed(k, "k", H, d, k_pages.dtype, dev), _packed(v, "v", H, d, k_pages.dtype, dev)
+    total = k.shape[0]
+    if v.shape != k.shape:
+        raise ValueError("k and v must have the same shape")
+    _longs(slot, "slot", (total,), dev)
+    rot = 0 if freq is None else _freq(freq, d, dev)
+    if pos is not None:
+        _ints(pos, "pos", (total,), dev)
+    elif rot:
+        raise ValueError("freq needs pos")
+    _call("lla_kv_write_slots", dev, _dt(k_pages), total, H, d, rot, int(interleaved), _ptr(k), kt, _ptr(v), vt,
+          _ptr(freq), float(magnitude), P, _ptr(slot), _ptr(pos), _ptr(k_pages), _ptr(v_pages))
+
+
+def _results(q, out, out_dtype, lse, dev):
+    """The result tensor of attention of q [rows, H, d], and lse checked."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype, device=dev)
+    else:
+        _need(out, "out", None, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    if lse is not None:
+        _need(lse, "lse", torch.float32, dev)
+        if lse.shape != q.shape[:2]:
+            raise ValueError("lse must be [rows, H]")
+    return out
+
+
+def _workspace(workspace, dev, query):
+    """(tensor, pointer, bytes) of a workspace, made here to the size of query() if None."""
+    if workspace is None:
+        with torch.cuda.device(dev) if _device() != dev.index else nullcontext():
+            need = query()
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    else:
+        _need(workspace, "workspace", None, dev)
+    return workspace, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def prefill_workspace_bytes(dtype: torch.dtype, B: int, total: int, H: int, H_kv: int, d: int, n_ctx: int, sink: int = 0,
+                            window: int = 0, *, out_dtype=torch.float32) -> int:
+    """Workspace of prefill_attn on the current device for up to B entries, total tokens
+    and bounds up to n_ctx."""
+    out = _c_sz()
+    _whole(n_ctx | sink | window | total, "total, n_ctx, sink and window")
+    _check(lib().lla_kv_prefill_workspace_bytes(_out_code(dtype), _out_code(out_dtype), B, total, H, H_kv, d, n_ctx, sink,
+                                                window, ctypes.byref(out)))
+    return out.value
+
+
+def prefill_attn(q, k_pages, v_pages, table, offset, start, *, n_ctx: int, rows=None, scale: float | None = None,
+                 sink: int = 0, window: int = 0, out=None, out_dtype=torch.float32, lse=None, workspace=None):
+    """Causal attention of packed q [total, H, d] (heads and rows dense): tokens
+    offset[b] .. offset[b + 1] - 1 (int32 [B + 1], of slots) stand at places start[b] on
+    of sequences rows[b] (None: b) and attend every place up to their own, below n_ctx,
+    or with ``window`` of these the first ``sink`` and the last ``window``.  Their keys
+    and values must have been written.  Entries of row -1 or start -1 give zeros, rows
+    that are no entry's are left as they are.  With out_dtype bfloat16 the softmax weights
+    are rounded to it for their product.  lse: float32 [total, H] or None; workspace:
+    uint8 of prefill_workspace_bytes(...) (allocated here if None).  Returns out [total,
+    H, d]."""
+    dev = q.device
+    _, P, Hkv, d = _pools(k_pages, v_pages)
+    _no_gradient(q, k_pages, v_pages, out)
+    if q.dim() != 3:
+        raise ValueError("q must be [total, H, d]")
+    total, H, _ = q.shape
+    stride = _packed(q, "q", H, d, k_pages.dtype, dev)
+    if k_pages.device != dev:
+        raise ValueError("q must be on the pools' device")
+    n_seqs, max_pages = table.shape
+    _whole(n_ctx | sink | window, "n_ctx, sink and window")
+    B = start.numel()
+    for t, name, shape in ((table, "table", (n_seqs, max_pages)), (offset, "offset", (B + 1,)), (start, "start", (B,))):
+        _ints(t, name, shape, dev)
+    if rows is not None:
+        _ints(rows, "rows", (B,), dev)
+    elif B > n_seqs:
+        raise ValueError("more entries than sequences")
+    out = _results(q, out, out_dtype, lse, dev)
+    workspace, ws, ws_bytes = _workspace(workspace, dev, lambda: prefill_workspace_bytes(
+        q.dtype, B, total, H, Hkv, d, n_ctx, sink, window, out_dtype=out.dtype))
+    _call("lla_kv_prefill_attn", dev, _dt(q), _out_code(out.dtype), B, total, H, Hkv, d, n_seqs, max_pages, P, n_ctx, sink,
+          window, _ptr(table), _ptr(rows), _ptr(offset), _ptr(start), _ptr(q), stride, _ptr(k_pages), _ptr(v_pages),
+          float(1.0 / math.sqrt(d) if scale is None else scale), _ptr(out), _ptr(lse), ws, ws_bytes)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Shared prompts
+# ---------------------------------------------------------------------------
+
+def shared_prefix(pages: PageTable, rows=None, *, least: int = 1, out=None):
+    """(lead, shared), int32 [B]: neighbours among sequences rows[b] (None: all) that read
+    the same pages at their first ``least`` places or more are a group, whose first entry
+    is lead[b] and which shares shared[b] places (0 for an entry alone)."""
+    dev = pages.table.device
+    sizes = _page_table(pages, dev)
+    _whole(least, "least")
+    B = sizes[0] if rows is None else rows.numel()
+    if rows is not None:
+        _ints(rows, "rows", (B,), dev)
+    lead, shared = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2)) if out is None else out
+    for t, name in ((lead, "lead"), (shared, "shared")):
+        _ints(t, name, (B,), dev)
+    _call("lla_pages_shared", dev, B, least, _ptr(rows), *sizes, _ptr(pages.table), _ptr(pages.length), _ptr(lead),
+          _ptr(shared))
+    return lead, shared
+
+
+def shared_workspace_bytes(dtype: torch.dtype, B: int, H: int, H_kv: int, d: int, n_ctx: int) -> int:
+    """Workspace of decode_attn_shared on the current device for up to B entries and
+    bounds up to n_ctx."""
+    out = _c_sz()
+    _whole(n_ctx, "n_ctx")
+    _check(lib().lla_kv_shared_workspace_bytes(_out_code(dtype), B, H, H_kv, d, n_ctx, ctypes.byref(out)))
+    return out.value
+
+
+def decode_attn_shared(q, k_pages, v_pages, table, length, lead, shared, *, n_ctx: int, rows=None,
+                       scale: float | None = None, out=None, out_dtype=torch.float32, lse=None, workspace=None):
+    """decode_attn for entries of which neighbours share a prompt: the places below
+    shared[b] are read through the pages of entry lead[b], once for all neighbours with
+    the same lead and shared (of shared_prefix, or the program's own), the others through
+    b's.  workspace: uint8 of shared_workspace_bytes(...) (allocated here if None)."""
+    dev = q.device
+    _, P, Hkv, d = _pools(k_pages, v_pages)
+    _no_gradient(q, k_pages, v_pages, out)
+    _need(q, "q", k_pages.dtype, dev)
+    if q.dim() != 3 or q.shape[2] != d or k_pages.device != dev:
+        raise ValueError("q must be [B, H, d] with the pools' width, on their device")
+    B, H, _ = q.shape
+    n_seqs, max_pages = table.shape
+    _whole(n_ctx, "n_ctx")
+    for t, name, shape in ((table, "table", (n_seqs, max_pages)), (length, "length", (n_seqs,)), (lead, "lead", (B,)),
+                           (shared, "shared", (B,))):
+        _ints(t, name, shape, dev)
+    if rows is not None:
+        _ints(rows, "rows", (B,), dev)
+    elif B > n_seqs:
+        raise ValueError("more entries than sequences")
+    out = _results(q, out, out_dtype, lse, dev)
+    workspace, ws, ws_bytes = _workspace(workspace, dev, lambda: shared_workspace_bytes(q.dtype, B, H, Hkv, d, n_ctx))
+    _call("lla_kv_decode_attn_shared", dev, _dt(q), _out_code(out.dtype), B, H, Hkv, d, n_seqs, max_pages, P, n_ctx,
+          _ptr(table), _ptr(length), _ptr(rows), _ptr(lead), _ptr(shared), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+          float(1.0 / math.sqrt(d) if scale is None else scale), _ptr(out), _ptr(lse), ws, ws_bytes)
     return out
