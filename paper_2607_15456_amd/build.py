@@ -33,13 +33,16 @@ COMMON = [
     "-Wall",
     "-Wno-unused-result",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # MFMA accumulators in architectural VGPRs: the softmax reads them directly
-    # (no accvgpr moves)
-    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-I", os.path.join(ROOT, "include"),
     "-I", CSRC,
 ]
 
+
+# MFMA accumulators in architectural VGPRs: the softmax reads them directly (no
+# accvgpr moves).  Not where one wavefront a SIMD holds more than 256 registers:
+# there the accumulators are the ones that fit into the others.
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+AGPR_SOURCES = ("kv_large_packed_wide.hip", "kv_large_shared_wide.hip")
 
 # Per-source additions.  The prefills' scores are finite or -inf by
 # construction (finite queries, finite latents up to the prompt's end, zeros
@@ -53,7 +56,9 @@ def sources():
 
 def _compile(src, verbose):
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
-    cmd = [HIPCC, *COMMON, *EXTRA.get(os.path.basename(src), []), "-c", src, "-o", obj]
+    name = os.path.basename(src)
+    form = [] if name in AGPR_SOURCES else VGPR_FORM
+    cmd = [HIPCC, *COMMON, *form, *EXTRA.get(name, []), "-c", src, "-o", obj]
     if src.endswith(".cpp"):
         cmd[1:1] = ["-x", "hip"]
     if verbose:

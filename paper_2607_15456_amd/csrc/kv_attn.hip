@@ -14,203 +14,258 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr float kLn2 = 0.69314718055994531f;
 
-// Partial rows of one result: `count` of them from `at`, `stride` floats apart.
+// A result from its partial rows: d / 4 neighbouring threads hold four features each, and
+// all of them the maximum and the sum.
+struct Joined {
+  float m = neg_inf(), l = 0.f;
+  f32x4 o = f32x4{0.f};
+  // `count` partial rows from `at`, `stride` floats apart
+  __device__ __forceinline__ void add(const float* at, int64_t stride, int count, int d, int f) {
+#pragma unroll 4
+    for (int s = 0; s < count; ++s) {
+      const float* part = at + s * stride;
+      const float m2 = part[d], l2 = part[d + 1], to = fmaxf(m, m2), base = to == neg_inf() ? 0.f : to;
+      const f32x4 o2 = *reinterpret_cast<const f32x4*>(part + f);
+      const float x = __builtin_amdgcn_exp2f(m - base), y = __builtin_amdgcn_exp2f(m2 - base);
+      m = to;
+      l = l * x + l2 * y;
+      o = o * x + o2 * y;
+    }
+  }
+  __device__ __forceinline__ void store(const KvTileArgs& a, int64_t row, int f) const {
+    store_row4(a, row, f, o / l);
+    if (a.lse && f == 0) a.lse[row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+};
+
+// Partial rows of a tile's row x: from slice 0's, how far apart and how many.
 struct Slices {
   const float* at;
   int64_t stride;
   int count;
+  __device__ __forceinline__ Slices(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices, int least,
+                                    const float* part, int cols, int kvh, int x) {
+    const int per = slice_pages(least, t.keys.pages, slices), row = a.p.d + 4;
+    at = part + (item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
+    stride = (int64_t)tiles * a.p.Hkv * cols * row;
+    count = (t.keys.pages + per - 1) / per;
+  }
 };
 
-// Joins the partial rows of one result in a wavefront: the maximum first, then the
-// weights 2^(m_s - m), a slice a lane, then four features a lane over all slices.
-template <int N>
-__device__ __forceinline__ void join_row(const KvTileArgs& a, const Slices (&in)[N], int64_t row) {
-  const int lane = threadIdx.x % kWave, d = a.p.d;
-  float m = neg_inf();
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    for (int s = lane; s < in[n].count; s += kWave) m = fmaxf(m, in[n].at[s * in[n].stride + d]);
-#pragma unroll
-  for (int x = kWave / 2; x; x >>= 1) m = fmaxf(m, xor_shfl(m, x));
-  const float base = m == neg_inf() ? 0.f : m;
-  float l = 0.f;
-  f32x4 o = f32x4{0.f};
-  const int f = 4 * min(lane, d / 4 - 1);
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    for (int s0 = 0; s0 < in[n].count; s0 += kWave) {
-      const int many = min(kWave, in[n].count - s0);
-      const float* part = in[n].at + s0 * in[n].stride;
-      float w = 0.f;
-      if (lane < many) {
-        w = __builtin_amdgcn_exp2f(part[lane * in[n].stride + d] - base);
-        l += part[lane * in[n].stride + d + 1] * w;
-      }
-#pragma unroll 4
-      for (int s = 0; s < many; ++s) o += *reinterpret_cast<const f32x4*>(part + s * in[n].stride + f) * __shfl(w, s, kWave);
+constexpr int kJoinRows = 32;  // of a tile, that a workgroup joins at a time
+
+// Packed tokens: the tiles that were cut, a workgroup 32 rows of one.
+__global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int large_cols) {
+  __shared__ int s_small[kMostEntries + 1], s_large[kMostEntries + 1], s_wave[kWaves];
+  count_packed<kThreads>(a, a.small_cols, 0, a.small_rows, s_small, s_wave);
+  count_packed<kThreads>(a, large_cols, a.small_rows, kAllRows, s_large, s_wave);
+  const int small = s_small[a.B], small_slices = tile_slices(a, small, a.small_wgs);
+  const int large = s_large[a.B], large_slices = tile_slices(a, large, a.large_wgs);
+  const int chunks = large_cols / kJoinRows;
+  const int64_t of_small = small_slices > 1 ? (int64_t)small * a.p.Hkv : 0;
+  const int64_t of_large = large_slices > 1 ? (int64_t)large * a.p.Hkv * chunks : 0;
+  const int lanes = a.p.d / 4, r = threadIdx.x / lanes, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
+  if (r >= step) return;
+  for (int64_t i = blockIdx.x; i < of_small + of_large; i += gridDim.x) {
+    const bool is_small = i < of_small;
+    const int64_t j = is_small ? i : i - of_small, unit = is_small ? j : j / chunks;
+    const int chunk = (int)(j - (is_small ? j : unit * chunks)), kvh = (int)(unit % a.p.Hkv), tile = (int)(unit / a.p.Hkv);
+    const int* first = is_small ? s_small : s_large;
+    const int b = last_at_most(first, a.B, tile), cols = is_small ? a.small_cols : large_cols;
+    Tile t;
+    t.at<kPacked>(a, b, cols, tile - first[b]);
+    if (t.state != kFine) continue;
+    const int end = min(t.rows, (chunk + 1) * kJoinRows);
+    for (int x = chunk * kJoinRows + r; x < end; x += step) {
+      const Slices in = is_small ? Slices(a, t, small, tile, small_slices, a.small_least, a.small_part, cols, kvh, x)
+                                 : Slices(a, t, large, tile, large_slices, a.large_least, a.large_part, cols, kvh, x);
+      if (in.count <= 1) break;  // (written by the tile itself)
+      Joined row;
+      row.add(in.at, in.stride, in.count, a.p.d, f);
+      int64_t q_at, out_at;
+      t.row_keys<kPacked>(a, kvh, x, q_at, out_at);
+      row.store(a, out_at, f);
     }
   }
-#pragma unroll
-  for (int x = kWave / 2; x; x >>= 1) l += xor_shfl(l, x);
-  if (4 * lane < d) store_row4(a, row, f, o / l);
-  if (a.lse && lane == 0) a.lse[row] = (base + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-__device__ __forceinline__ void none_row(const KvTileArgs& a, int64_t row, bool nan) {
-  const int lane = threadIdx.x % kWave;
-  const float none = nan ? __builtin_nanf("") : 0.f;
-  if (4 * lane < a.p.d) store_row4(a, row, 4 * lane, f32x4{none, none, none, none});
-  if (a.lse && lane == 0) a.lse[row] = nan ? none : neg_inf();
-}
-
-// Slices of a tile, from row x of its first.
-__device__ __forceinline__ Slices slices_of(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices,
-                                            const float* part, int cols, int kvh, int x) {
-  const int per = slice_pages(a, t.keys.pages, slices), row = a.p.d + 4;
-  return {part + (item_of(a, tiles, 0, tile, kvh) * cols + x) * row, (int64_t)tiles * a.p.Hkv * cols * row,
-          (t.keys.pages + per - 1) / per};
-}
-
-__global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a) {
-  __shared__ int s_small[kMostEntries + 1], s_off[kMostEntries + 1], s_wave[kWaves];
-  count_tiles<kPacked, kThreads>(a, kSmallCols, 0, a.small_rows, s_small, s_wave);
+// Shared prompts: every (entry, query head), of its prompt's slices and its own.
+__global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
+  __shared__ int s_runs[kMostEntries + 1], s_small[kMostEntries + 1], s_large[kMostEntries + 1], s_wave[kWaves];
+  count_shared<kThreads>(a, s_runs, s_small, s_large, s_wave);
   const int small = s_small[a.B], small_slices = tile_slices(a, small, a.small_wgs);
-  if (small_slices == 1) return;
-  for (int b = threadIdx.x; b <= a.B; b += kThreads) s_off[b] = offset_of(a, b);
-  __syncthreads();
-  const int group = a.H / a.p.Hkv;
-  const int64_t rows = (int64_t)a.total * a.H;
-  for (int64_t i = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; i < rows; i += (int64_t)gridDim.x * kWaves) {
-    const int token = (int)(i / a.H), h = (int)(i - (int64_t)token * a.H), kvh = h / group;
-    if (token < s_off[0]) continue;
-    Tile t;
-    t.entry = last_at_most(s_off, a.B, token);
-    if (token >= s_off[t.entry + 1]) continue;
-    const int col = (token - s_off[t.entry]) * group + h - kvh * group, nth = col / kSmallCols;
-    t.at<kPacked>(a, s_small, kSmallCols, nth);
-    const Slices in[1] = {slices_of(a, t, small, s_small[t.entry] + nth, small_slices, a.small_part, kSmallCols, kvh,
-                                    col - nth * kSmallCols)};
-    if (t.state == kFine && in[0].count > 1) join_row(a, in, i);
-  }
-}
-
-__global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a, int own_cols) {
-  __shared__ int s_first[kMostEntries + 1], s_wave[kWaves];
-  count_tiles<kPrefix, kThreads>(a, kSmallCols, 0, 0, s_first, s_wave);
-  const int tiles = s_first[a.B], slices = tile_slices(a, tiles, a.small_wgs);
-  const int group = a.H / a.p.Hkv, own_blocks = (group + own_cols - 1) / own_cols;
+  const int large = s_large[a.B], large_slices = tile_slices(a, large, a.large_wgs);
+  const int group = a.H / a.p.Hkv, cols = a.small_cols, blocks = (group + cols - 1) / cols;
+  const int lanes = a.p.d / 4, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
   const int64_t rows = (int64_t)a.B * a.H;
-  for (int64_t i = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; i < rows; i += (int64_t)gridDim.x * kWaves) {
+  if ((int)threadIdx.x / lanes >= step) return;
+  for (int64_t i = (int64_t)blockIdx.x * step + threadIdx.x / lanes; i < rows; i += (int64_t)gridDim.x * step) {
     const int b = (int)(i / a.H), h = (int)(i - (int64_t)b * a.H), kvh = h / group, r = h - kvh * group;
+    const int shared = a.shared[b];
     Tile own;
-    own.entry = b;
-    own.at<kOwn>(a, s_first, own_cols, r / own_cols);
-    if (own.state != kFine) {
-      none_row(a, i, own.state == kNone);
+    own.at<kOwn>(a, b, cols, r / cols);
+    TileState state = own.state;
+    Joined row;
+    if (state == kFine && shared > 0) {
+      // the tile that b's queries are of begins at the last entry up to b that goes on with none
+      const int e = last_at_most(s_runs, a.B, s_runs[b + 1] - 1), many = run_entries(a, s_runs, e);
+      const bool is_small = s_small[e + 1] > s_small[e];
+      const int of = is_small ? cols : a.prefix_cols, col = (b - e) * group + r, nth = col / of, x = col - nth * of;
+      Tile t;
+      t.at<kPrefix>(a, e, of, nth, many);
+      const Slices in = is_small ? Slices(a, t, small, s_small[e] + nth, small_slices, a.small_least, a.small_part, of, kvh, x)
+                                 : Slices(a, t, large, s_large[e] + nth, large_slices, a.large_least, a.large_part, of, kvh, x);
+      if (t.state == kFine) row.add(in.at, in.stride, in.count, a.p.d, f);
+      else state = kNone;
+    }
+    if (state != kFine) {
+      const float none = state == kNone ? __builtin_nanf("") : 0.f;
+      store_row4(a, i, f, f32x4{none, none, none, none});
+      if (a.lse && f == 0) a.lse[i] = state == kNone ? none : neg_inf();
       continue;
     }
-    Slices in[2] = {{nullptr, 0, 0},
-                    slices_of(a, own, a.B * own_blocks, b * own_blocks + r / own_cols, a.own_slices, a.own_part, own_cols,
-                              kvh, r % own_cols)};
-    if (a.shared[b] > 0) {
-      // the tile that b's queries are of: the last that begins at or before b
-      const int each = tile_entries(group, kSmallCols), nth = each == 1 ? r / kSmallCols : 0;
-      Tile t;
-      const int tile = s_first[b + 1] - 1;  // the last of the entry's, or of the run's
-      t.entry = last_at_most(s_first, a.B, tile);
-      t.at<kPrefix>(a, s_first, kSmallCols, nth);
-      if (t.state != kFine) {
-        none_row(a, i, true);
-        continue;
-      }
-      in[0] = slices_of(a, t, tiles, s_first[t.entry] + nth, slices, a.small_part, kSmallCols, kvh,
-                        (b - t.entry) * group + r - nth * kSmallCols);
-    }
-    join_row(a, in, i);
+    const Slices in(a, own, a.B * blocks, b * blocks + r / cols, a.own_slices, a.small_least, a.own_part, cols, kvh, r % cols);
+    row.add(in.at, in.stride, in.count, a.p.d, f);
+    row.store(a, i, f);
   }
 }
 
-int cols_of(int group) { return group > 16 ? 32 : 16; }
 int64_t blocks_of(int64_t rows, int cols) { return (rows + cols - 1) / cols; }
-int bound_pages(const KvTileArgs& a) { return (a.n_ctx + kPage - 1) / kPage; }
-// Most pages that a tile reads.
-int most_pages(const KvTileArgs& a) {
-  if (!a.window) return bound_pages(a);
-  const int64_t budget = blocks_of(a.sink, kPage) + blocks_of((int64_t)a.window + 32, kPage) + 1;
-  return (int)std::min<int64_t>(bound_pages(a), budget);
+// Most pages that a tile of `cols` rows reads.
+int most_pages(const KvTileArgs& a, int cols) {
+  const int all = (int)blocks_of(a.n_ctx, kPage);
+  if (!a.window) return all;
+  return (int)std::min<int64_t>(all, blocks_of(a.sink, kPage) + blocks_of((int64_t)a.window + cols, kPage) + 1);
 }
 size_t row_bytes(const KvTileArgs& a) { return (size_t)(a.p.d + 4) * sizeof(float); }
-
-constexpr int kLeast = 4;
-
-}  // namespace
-
-namespace {
-// Tiles that a packed batch may have, at most: every entry may end inside one.
-int64_t most_tiles(const KvTileArgs& a, int cols) { return (int64_t)a.total * (a.H / a.p.Hkv) / cols + a.B; }
-int64_t split_items(const KvTileArgs& a, int64_t tiles, int wgs) {
-  const int64_t each = std::min<int64_t>(a.most, blocks_of(most_pages(a), a.least));
-  return each <= 1 ? 0 : std::min<int64_t>(wgs, tiles * a.p.Hkv * each);
+// Partial tiles, at most: `tiles` tiles cut over the workgroups (two rounds of them).
+int64_t partial_tiles(const KvTileArgs& a, int64_t tiles, int wgs, int least, int cols) {
+  const int64_t each = std::min<int64_t>(a.most, blocks_of(most_pages(a, cols), least));
+  return each <= 1 ? 0 : std::min<int64_t>(2 * wgs, tiles * a.p.Hkv * each);
 }
+
+constexpr int kSmallLeast = 4, kLargeLeast = 4, kMostSlices = 512;
+void limits(KvTileArgs& a) {
+  const int cus = device_cu_count();
+  a.small_least = kSmallLeast;
+  a.large_least = kLargeLeast;
+  a.most = blocks_of(a.n_ctx, kPage) <= kSmallLeast ? 1 : kMostSlices;
+  a.small_wgs = 2 * cus;
+  a.large_wgs = cus;
+}
+
+// Rows of a small tile: two products' columns where a group of heads is more than one's.
+int small_cols_of(const KvTileArgs& a) { return a.H / a.p.Hkv > 16 ? 32 : 16; }
+
+struct PackedShape {
+  int64_t small_tiles, large_tiles, small_partial, large_partial;
+  explicit PackedShape(const KvTileArgs& a) {
+    const int64_t rows = (int64_t)a.total * (a.H / a.p.Hkv);
+    const int cols = large_cols(a.p.d);
+    // every entry may end inside a tile; large ones have more than small_rows rows
+    small_tiles = a.small_rows == 0 ? 0
+                  : a.small_rows == kAllRows ? std::min(rows / a.small_cols + a.B, rows) : std::min(a.B, a.total);
+    large_tiles = rows > a.small_rows ? std::min(rows / cols + a.B, blocks_of(rows, a.small_rows + 1)) : 0;
+    small_partial = partial_tiles(a, small_tiles, a.small_wgs, a.small_least, a.small_cols);
+    large_partial = partial_tiles(a, large_tiles, a.large_wgs, a.large_least, cols);
+  }
+  size_t bytes(const KvTileArgs& a) const {
+    return (size_t)(small_partial * a.small_cols + large_partial * large_cols(a.p.d)) * row_bytes(a);
+  }
+};
+
 }  // namespace
 
+// Large tiles are of bf16.  In fp32 the matrix units are the bound from few rows on, and
+// small tiles keep them as busy (3 entries of 301 .. 101 tokens over 1020 of a window, 24
+// heads on 8 of 96: 108 us; with large fp32 tiles 134).
 size_t kv_prefill_shape(KvTileArgs& a) {
-  a.least = kLeast;
-  a.most = most_pages(a) <= a.least ? 1 : 512;
-  a.small_wgs = 2 * device_cu_count();
-  a.small_rows = 0x7fffffff;
-  return (size_t)split_items(a, most_tiles(a, kSmallCols), a.small_wgs) * kSmallCols * row_bytes(a);
+  limits(a);
+  a.small_cols = small_cols_of(a);
+  // a single entry is of one kind of tile, so one launch does
+  const bool one_large = a.B == 1 && (int64_t)a.total * (a.H / a.p.Hkv) > a.small_cols;
+  a.small_rows = a.p.dtype == LLA_F32 ? kAllRows : one_large ? 0 : a.small_cols;
+  return PackedShape(a).bytes(a);
 }
 size_t kv_prefill_workspace(const KvTileArgs& a) {
   KvTileArgs x = a;
   return kv_prefill_shape(x);
 }
 
-hipError_t launch_kv_prefill(const KvTileArgs& a, hipStream_t stream) {
-  const int64_t tiles = most_tiles(a, kSmallCols), items = split_items(a, tiles, a.small_wgs);
-  const unsigned grid = (unsigned)std::min<int64_t>(std::max(items, tiles * a.p.Hkv), 1 << 20);
-  const hipError_t e = launch_small_packed(a, grid, stream);
-  if (e != hipSuccess || items == 0) return e;
-  const unsigned joins = (unsigned)std::min<int64_t>(blocks_of((int64_t)a.total * a.H, kWaves), 2048);
-  hipLaunchKernelGGL(join_packed_kernel, dim3(joins), dim3(kThreads), 0, stream, a);
+hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
+  KvTileArgs a = args;
+  const PackedShape s(a);
+  a.large_part = a.small_part + s.small_partial * a.small_cols * (a.p.d + 4);
+  hipError_t e = hipSuccess;
+  // (a workgroup takes another tile where there are more)
+  auto grid = [&](int64_t tiles, int64_t partial) { return (unsigned)std::min<int64_t>(std::max(partial, tiles * a.p.Hkv), 1 << 16); };
+  if (s.large_tiles) e = launch_large_packed(a, grid(s.large_tiles, s.large_partial), stream);
+  if (e != hipSuccess) return e;
+  if (s.small_tiles) e = launch_small_packed(a, grid(s.small_tiles, s.small_partial), stream);
+  if (e != hipSuccess || s.small_partial + s.large_partial == 0) return e;
+  const int64_t joins = s.small_partial + s.large_partial * (large_cols(a.p.d) / kJoinRows);
+  hipLaunchKernelGGL(join_packed_kernel, dim3((unsigned)std::min<int64_t>(joins, 1024)), dim3(kThreads), 0, stream, a,
+                     large_cols(a.p.d));
   return hipGetLastError();
 }
 
-size_t kv_shared_shape(KvTileArgs& a) {
-  const int group = a.H / a.p.Hkv, cols = cols_of(group), cus = device_cu_count(), pages = bound_pages(a);
-  const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(group, cols);
-  a.least = kLeast;
-  a.most = pages <= a.least ? 1 : 512;
-  a.small_wgs = 2 * cus;
-  a.own_slices = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / units, blocks_of(pages, a.least)));
-  // prefix tiles without a split: of a run for every two entries, or a run for all
-  const int64_t tiles = (int64_t)a.B * blocks_of(group, kSmallCols);
-  const int64_t prefix = std::max(split_items(a, tiles, a.small_wgs), tiles * a.p.Hkv);
-  return ((size_t)prefix * kSmallCols + (size_t)units * a.own_slices * cols) * row_bytes(a);
-}
-size_t kv_shared_workspace(const KvTileArgs& a) {
-  size_t most = 0;
-  for (int B = 1; B <= a.B; ++B) {
-    KvTileArgs x = a;
-    x.B = B;
-    most = std::max(most, kv_shared_shape(x));
+namespace {
+struct SharedShape {
+  int64_t small, large, own;  // partial tiles: over prompts, small and large, and entries' own
+  explicit SharedShape(const KvTileArgs& a) {
+    const int group = a.H / a.p.Hkv;
+    const int64_t rows = (int64_t)a.B * group, blocks = blocks_of(group, a.prefix_cols);
+    auto items = [&](int64_t tiles, int wgs, int least, int cols) {
+      return tiles ? std::max(partial_tiles(a, tiles, wgs, least, cols), tiles * a.p.Hkv) : 0;
+    };
+    // any entry may begin a run; large tiles are of runs of more than small_rows rows
+    const int64_t runs = std::min<int64_t>(a.B, rows / (a.small_rows + (int64_t)1));
+    small = items(a.small_rows == kAllRows ? a.B * blocks : a.B, a.small_wgs, a.small_least, a.small_cols);
+    large = items(runs * blocks, a.large_wgs, a.large_least, a.prefix_cols);
+    own = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols) * a.own_slices;
   }
-  return most;
+  size_t bytes(const KvTileArgs& a) const {
+    return (size_t)((small + own) * a.small_cols + large * a.prefix_cols) * row_bytes(a);
+  }
+};
+}  // namespace
+
+size_t kv_shared_shape(KvTileArgs& a) {
+  limits(a);
+  const int group = a.H / a.p.Hkv;
+  a.small_cols = small_cols_of(a);
+  const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols);
+  const bool all_small = a.p.dtype == LLA_F32;
+  a.small_rows = all_small ? kAllRows : a.small_cols;
+  a.prefix_cols = all_small ? a.small_cols : large_cols(a.p.d);
+  a.own_slices =
+      (int)std::max<int64_t>(1, std::min<int64_t>(a.small_wgs / units, blocks_of(blocks_of(a.n_ctx, kPage), a.small_least)));
+  return SharedShape(a).bytes(a);
+}
+// Of any smaller batch: the partial tiles over prompts grow with the entries, and of own
+// ones there are no more than workgroups, or than entries have without a cut.
+size_t kv_shared_workspace(const KvTileArgs& a) {
+  KvTileArgs x = a;
+  kv_shared_shape(x);
+  SharedShape s(x);
+  const int64_t units = s.own / x.own_slices, pages = blocks_of(blocks_of(a.n_ctx, kPage), x.small_least);
+  s.own = std::min(std::max<int64_t>(x.small_wgs, units), units * pages);
+  return s.bytes(x);
 }
 
 hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
   KvTileArgs a = args;
-  const int group = a.H / a.p.Hkv, cols = cols_of(group);
-  const int64_t tiles = (int64_t)a.B * blocks_of(group, kSmallCols);
-  const int64_t prefix = std::max(split_items(a, tiles, a.small_wgs), tiles * a.p.Hkv);
-  a.own_part = a.small_part + prefix * kSmallCols * (a.p.d + 4);
-  const int64_t own = (int64_t)a.B * a.p.Hkv * blocks_of(group, cols) * a.own_slices;
-  hipError_t e = launch_small_prefix(a, (unsigned)std::min<int64_t>(prefix, 1 << 20), stream);
+  const SharedShape s(a);
+  a.own_part = a.small_part + s.small * a.small_cols * (a.p.d + 4);
+  a.large_part = a.own_part + s.own * a.small_cols * (a.p.d + 4);
+  auto grid = [](int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 16); };
+  hipError_t e = hipSuccess;
+  if (s.large) e = launch_large_prefix(a, grid(s.large), stream);
   if (e != hipSuccess) return e;
-  e = launch_small_own(a, cols / 16, (unsigned)std::min<int64_t>(own, 1 << 20), stream);
+  e = launch_small_shared(a, grid(s.small + s.own), stream);
   if (e != hipSuccess) return e;
-  const unsigned joins = (unsigned)std::min<int64_t>(blocks_of((int64_t)a.B * a.H, kWaves), 2048);
-  hipLaunchKernelGGL(join_shared_kernel, dim3(joins), dim3(kThreads), 0, stream, a, cols);
+  const int64_t joins = blocks_of((int64_t)a.B * a.H, kThreads / (a.p.d / 4));
+  hipLaunchKernelGGL(join_shared_kernel, dim3((unsigned)std::min<int64_t>(joins, 1024)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

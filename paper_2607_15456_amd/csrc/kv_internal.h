@@ -85,12 +85,14 @@ struct KvTileArgs {
   float qscale;
   void* out;
   float* lse;
-  // slices of a tile at most, and pages of a slice at least
-  int most, least;
+  // slices of a tile at most (1: none is cut); pages of a slice at least, of small tiles and large ones
+  int most, small_least, large_least;
   // workgroups that small tiles and large ones are shared out to
   int small_wgs, large_wgs;
-  // rows of a packed entry up to which it is of small tiles
+  // rows up to which a packed entry, or a run of entries that share a prompt, is of small tiles
   int small_rows;
+  // rows of a small tile, and at which a run is cut into tiles
+  int small_cols, prefix_cols;
   // slices that an entry's own tokens are cut into, at most
   int own_slices;
   float* small_part;

@@ -1,6 +1,6 @@
 // Work of the attention of packed tokens and of shared prompts over the paged K/V
 // cache: which rows make a tile, which pages it reads, and how tiles are shared out
-// (kv_tile_small.h, kv_join.hip).
+// (kv_tile_small.h, kv_tile_large.h, kv_attn.hip).
 //
 // A tile is up to kCols rows (token or entry, query head of the group) that read the
 // same pages for one key head.  How many tiles a call has is known on the device
@@ -15,6 +15,7 @@
 namespace lla {
 
 constexpr int kMostEntries = 1024;
+constexpr int kAllRows = 0x7fffffff;  // small_rows: all tiles are small ones
 
 enum TileMode { kPacked, kPrefix, kOwn };
 
@@ -85,54 +86,153 @@ __device__ __forceinline__ int last_at_most(const int* s_at, int n, int x) {
 // First packed token of entry b, within the tokens that there are.
 __device__ __forceinline__ int offset_of(const KvTileArgs& a, int b) { return max(0, min(a.offset[b], a.total)); }
 
-// Entries of a prefix tile: those of one run of equal (lead, shared), cut where the
+// Tiles of entries' counts n[] (entries tid * kEach ..) before each: s_first[b], all in s_first[B].
+template <int kThreads>
+struct EntryCounts {
+  static constexpr int kEach = (kMostEntries + kThreads - 1) / kThreads;
+  int n[kEach];
+  __device__ __forceinline__ static int entry(int i) { return threadIdx.x * kEach + i; }
+  __device__ __forceinline__ void sum(int B, int* s_first, int* s_wave) const {
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) total += n[i];
+    int at = prefix_sum<kThreads>(total, s_wave);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = entry(i);
+      if (b < B) s_first[b] = at;
+      at += n[i];
+      if (b == B - 1) s_first[B] = at;
+    }
+    __syncthreads();
+  }
+};
+
+// Packed entries with more than `over` and at most `upto` rows.
+template <int kThreads>
+__device__ __forceinline__ void count_packed(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int* s_wave) {
+  const int group = a.H / a.p.Hkv;
+  EntryCounts<kThreads> c;
+#pragma unroll
+  for (int i = 0; i < c.kEach; ++i) {
+    const int b = c.entry(i);
+    c.n[i] = 0;
+    if (b < a.B) {
+      const int64_t rows = (int64_t)max(0, offset_of(a, b + 1) - offset_of(a, b)) * group;
+      if (rows > over && rows <= upto) c.n[i] = (int)((rows + cols - 1) / cols);
+    }
+  }
+  c.sum(a.B, s_first, s_wave);
+}
+
+// Sum over the wavefront.
+__device__ __forceinline__ int wave_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // of rows of 16 lanes:
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row 0 into 1, 2 into 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the first two into the others
+  return __builtin_amdgcn_readlane(v, kWave - 1);
+}
+
+// The x-th tile of a packed batch, those that stand last in their sequences first: what
+// a causal tile costs goes by its place, and a heavy one that begins late would run
+// alone at the end.  Tiles are numbered by their places' tile in the sequence, v = s_from[b] + nth;
+// at_least(v) counts those at v or behind.  Every wavefront of the workgroup finds it.
+struct HeavyFirst {
+  const int *s_first, *s_from;
+  int B;
+  // tiles of entry b at v or behind
+  __device__ __forceinline__ int behind(int b, int v) const {
+    const int n = s_first[b + 1] - s_first[b];
+    return max(0, min(n, s_from[b] + n - v));
+  }
+  __device__ __forceinline__ int at_least(int v) const {
+    int n = 0;
+    for (int b = threadIdx.x % kWave; b < B; b += kWave) n += behind(b, v);
+    return wave_sum(n);
+  }
+  __device__ __forceinline__ void find(int x, int most, int& entry, int& nth) const {
+    int lo = 0, hi = most;  // the greatest v with at_least(v) > x
+    while (lo < hi) {
+      const int mid = lo + (hi - lo + 1) / 2;
+      if (at_least(mid) > x) lo = mid;
+      else hi = mid - 1;
+    }
+    int skip = x - at_least(lo + 1);  // of the entries with a tile at lo
+    entry = nth = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+      const int b = b0 + threadIdx.x % kWave;
+      const uint64_t in = __ballot(b < B && behind(min(b, B - 1), lo) > behind(min(b, B - 1), lo + 1));
+      const int here = __popcll(in);
+      if (skip < here) {
+        uint64_t left = in;
+        for (; skip; --skip) left &= left - 1;
+        entry = b0 + __builtin_ctzll(left);
+        nth = lo - s_from[entry];
+        return;
+      }
+      skip -= here;
+    }
+  }
+};
+
+// Entries of a tile over a shared prompt: a run of equal (lead, shared), cut where the
 // entry's number is a multiple of these many.
 __host__ __device__ __forceinline__ int tile_entries(int group, int cols) { return group >= cols ? 1 : cols / group; }
 
-// s_first[b] = tiles of the entries before b, s_first[B] = all.
-//   kPacked: tiles of entries with more than `over` and at most `upto` rows
-//   kPrefix: a run's tile, at its first entry
-template <TileMode Mode, int kThreads>
-__device__ __forceinline__ void count_tiles(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int* s_wave) {
-  constexpr int kEach = (kMostEntries + kThreads - 1) / kThreads;
-  const int tid = threadIdx.x, group = a.H / a.p.Hkv;
-  int n[kEach], sum = 0;
+// Tiles over shared prompts.  s_runs[b]: entries before b that do not go on with the tile
+// of the one before them; then the tiles of at most small_rows rows, which are small
+// ones, and the others, where an array for them is given.
+template <int kThreads>
+__device__ __forceinline__ void count_shared(const KvTileArgs& a, int* s_runs, int* s_small, int* s_large, int* s_wave) {
+  const int group = a.H / a.p.Hkv, each = tile_entries(group, a.prefix_cols);
+  EntryCounts<kThreads> c, small, large;
+  bool begins[c.kEach];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int b = tid * kEach + i;
-    n[i] = 0;
+  for (int i = 0; i < c.kEach; ++i) {
+    const int b = c.entry(i);
+    c.n[i] = 0;
+    begins[i] = false;
     if (b < a.B) {
-      if constexpr (Mode == kPacked) {
-        const int64_t rows = (int64_t)max(0, offset_of(a, b + 1) - offset_of(a, b)) * group;
-        if (rows > over && rows <= upto) n[i] = (int)((rows + cols - 1) / cols);
-      } else {
-        const int lead = a.lead[b], shared = a.shared[b];
-        if (shared > 0) {
-          const bool first = b % tile_entries(group, cols) == 0 || a.lead[b - 1] != lead || a.shared[b - 1] != shared;
-          n[i] = first ? (group + cols - 1) / cols : 0;
-        }
-      }
+      const int lead = a.lead[b], shared = a.shared[b];
+      const bool first = shared <= 0 || b % each == 0 || a.lead[b - 1] != lead || a.shared[b - 1] != shared;
+      c.n[i] = first;
+      begins[i] = first && shared > 0;
     }
-    sum += n[i];
   }
-  int at = prefix_sum<kThreads>(sum, s_wave);
+  c.sum(a.B, s_runs, s_wave);
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int b = tid * kEach + i;
-    if (b < a.B) s_first[b] = at;
-    at += n[i];
-    if (b == a.B - 1) s_first[a.B] = at;
+  for (int i = 0; i < c.kEach; ++i) {
+    const int b = c.entry(i);
+    small.n[i] = large.n[i] = 0;
+    if (!begins[i]) continue;
+    // few: all tiles are, or the run has at most `most` entries: one behind it begins
+    // another, or there are no more
+    const int most = a.small_rows / group, blocks = (group + a.prefix_cols - 1) / a.prefix_cols;
+    const bool few = a.small_rows == kAllRows ||
+                     (most >= 1 && (b + most >= a.B || s_runs[b + most + 1] > s_runs[b + 1]));
+    (few ? small : large).n[i] = blocks;
   }
-  __syncthreads();
+  if (s_small) small.sum(a.B, s_small, s_wave);
+  if (s_large) large.sum(a.B, s_large, s_wave);
+}
+// Entries of the tile that begins at b.
+__device__ __forceinline__ int run_entries(const KvTileArgs& a, const int* s_runs, int b) {
+  return last_at_most(s_runs, a.B + 1, s_runs[b + 1]) - b;
 }
 
-// Slices that every tile may be cut into: as many as the workgroups there are for.
+// Slices that every tile may be cut into, where there are fewer tiles than workgroups:
+// as many as give each a workgroup, or so many that two rounds of workgroups do better.
 __device__ __forceinline__ int tile_slices(const KvTileArgs& a, int tiles, int workgroups) {
   const int64_t units = (int64_t)tiles * a.p.Hkv;
-  return units == 0 || a.most == 1 ? 1 : (int)max((int64_t)1, min((int64_t)a.most, workgroups / units));
+  if (units == 0 || a.most == 1) return 1;
+  const int one = (int)max((int64_t)1, workgroups / units), two = (int)(2 * workgroups / units);
+  return min(a.most, 9 * two > 20 * one ? two : one);
 }
-__device__ __forceinline__ int slice_pages(const KvTileArgs& a, int pages, int slices) {
-  return slices == 1 ? max(pages, 1) : max(a.least, (pages + slices - 1) / slices);
+__device__ __forceinline__ int slice_pages(int least, int pages, int slices) {
+  return slices == 1 ? max(pages, 1) : max(least, (pages + slices - 1) / slices);
 }
 
 // One tile of one key head.
@@ -143,16 +243,12 @@ struct Tile {
   TileState state;
   TileKeys keys;
 
-  // Tile t of the call's; s_first as count_tiles left it.
+  // Entry b's tile number nth, of `cols` rows; many: the entries of a tile over a shared
+  // prompt.
   template <TileMode Mode>
-  __device__ __forceinline__ void find(const KvTileArgs& a, const int* s_first, int cols, int t) {
-    entry = last_at_most(s_first, a.B, t);
-    at<Mode>(a, s_first, cols, t - s_first[entry]);
-  }
-  // The entry's tile number `nth`.
-  template <TileMode Mode>
-  __device__ __forceinline__ void at(const KvTileArgs& a, const int* s_first, int cols, int nth) {
-    const int group = a.H / a.p.Hkv, b = entry;
+  __device__ __forceinline__ void at(const KvTileArgs& a, int b, int cols, int nth, int many = 1) {
+    entry = b;
+    const int group = a.H / a.p.Hkv;
     first = nth * cols;
     state = kFine;
     keys.sink = 0;
@@ -173,11 +269,6 @@ struct Tile {
       }
     } else if constexpr (Mode == kPrefix) {
       const int lead = a.lead[b];
-      int many = 1;
-      if (group < cols)
-        while (many < tile_entries(group, cols) && b + many < a.B && (b + many) % tile_entries(group, cols) &&
-               a.lead[b + many] == lead && a.shared[b + many] == a.shared[b])
-          ++many;
       rows = min(cols, many * group - first);
       state = lead < 0 || lead >= a.B ? kNone : kFine;
       row = state == kFine ? (a.rows ? a.rows[lead] : lead) : -1;

@@ -5,11 +5,14 @@
 
 namespace lla {
 
-constexpr int kSmallCols = 32;  // rows of a small tile
-
+// small_cols: 16 or 32
 hipError_t launch_small_packed(const KvTileArgs& a, unsigned grid, hipStream_t stream);
-hipError_t launch_small_prefix(const KvTileArgs& a, unsigned grid, hipStream_t stream);
-// tiles: of 16 query heads, 1 or 2 a workgroup
-hipError_t launch_small_own(const KvTileArgs& a, int tiles, unsigned grid, hipStream_t stream);
+hipError_t launch_small_shared(const KvTileArgs& a, unsigned grid, hipStream_t stream);
+
+constexpr int large_cols(int d) { return d <= 128 ? 256 : 128; }  // rows of a large tile (bf16)
+hipError_t launch_large_packed(const KvTileArgs& a, unsigned grid, hipStream_t stream);
+hipError_t launch_large_packed_wide(const KvTileArgs& a, unsigned grid, hipStream_t stream);
+hipError_t launch_large_prefix(const KvTileArgs& a, unsigned grid, hipStream_t stream);
+hipError_t launch_large_prefix_wide(const KvTileArgs& a, unsigned grid, hipStream_t stream);
 
 }  // namespace lla

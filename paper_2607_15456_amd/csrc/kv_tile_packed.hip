@@ -6,7 +6,7 @@
 namespace lla {
 
 hipError_t launch_small_packed(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
-  return launch_small_type<2, kPacked>(a, grid, stream);
+  return a.small_cols == 16 ? launch_small_type<1, true>(a, grid, stream) : launch_small_type<2, true>(a, grid, stream);
 }
 
 }  // namespace lla

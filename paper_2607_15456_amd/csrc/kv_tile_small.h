@@ -39,14 +39,16 @@ __device__ __forceinline__ void add_nonfinite(const T* v, int count, int g, cons
   }
 }
 
-template <template <int, int> class StepOf, int D, int NT, TileMode Mode>
+// Packed: entries of few rows.  Otherwise the few queries of a run over their shared
+// prompt, and every entry's own tokens, in one launch.
+template <template <int, int> class StepOf, int D, int NT, bool Packed>
 __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void small_tile_kernel(KvTileArgs a) {
   typedef StepOf<D, NT> Step;
   typedef std::conditional_t<Step::kBytes == 2, bf16_t, float> T;
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
   constexpr int kRow = D + 4, kCols = NT * kTile, kThreads = kWaves * kWave, W = kWaves;
-  __shared__ int s_first[Mode == kOwn ? 1 : kMostEntries + 1], s_wave[kThreads / kWave];
+  __shared__ int s_first[kMostEntries + 1], s_runs[Packed ? 1 : kMostEntries + 1], s_wave[kThreads / kWave];
   // the wavefronts' steps, then what they join
   extern __shared__ __align__(16) char s_raw[];
   float* const s_o = reinterpret_cast<float*>(s_raw);
@@ -56,31 +58,34 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   char* const lds = s_raw + w * kStepBytes;
   const int group = a.H / a.p.Hkv, blocks = (group + kCols - 1) / kCols;
 
-  int tiles, slices;
-  float* part;
-  if constexpr (Mode == kOwn) {
-    tiles = a.B * blocks;
-    slices = a.own_slices;
-    part = a.own_part;
-  } else {
-    count_tiles<Mode, kThreads>(a, kCols, 0, Mode == kPacked ? a.small_rows : 0, s_first, s_wave);
-    tiles = s_first[a.B];
-    slices = tile_slices(a, tiles, a.small_wgs);
-    part = a.small_part;
-  }
-  const int64_t items = (int64_t)tiles * a.p.Hkv * slices;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int kvh = (int)(item % a.p.Hkv), unit = (int)(item / a.p.Hkv);
-    const int slice = unit / tiles, tile = tiles - 1 - (unit - slice * tiles);
-    Tile t;
-    if constexpr (Mode == kOwn) {
-      t.entry = tile / blocks;
-      t.at<Mode>(a, s_first, kCols, tile - t.entry * blocks);
-    } else {
-      t.find<Mode>(a, s_first, kCols, tile);
+  // An entry's own tokens come first: how many tiles over prompts there are takes a count.
+  const int64_t own_items = Packed ? 0 : (int64_t)a.B * blocks * a.p.Hkv * a.own_slices;
+  int tiles = -1, slices = 1;
+  for (int64_t i = blockIdx.x;; i += gridDim.x) {
+    const bool own = !Packed && i < own_items;
+    if (!own && tiles < 0) {
+      if constexpr (Packed) count_packed<kThreads>(a, kCols, 0, a.small_rows, s_first, s_wave);
+      else count_shared<kThreads>(a, s_runs, s_first, nullptr, s_wave);
+      tiles = s_first[a.B];
+      slices = tile_slices(a, tiles, a.small_wgs);
     }
-    const int per = slice_pages(a, t.keys.pages, slices), pb = slice * per, pe = min(t.keys.pages, pb + per);
-    const bool direct = Mode == kPacked && per >= t.keys.pages;
+    const int64_t item = own ? i : i - own_items;
+    if (!own && item >= (int64_t)tiles * a.p.Hkv * slices) break;
+    const int kvh = (int)(item % a.p.Hkv), unit = (int)(item / a.p.Hkv), of = own ? a.B * blocks : tiles;
+    const int slice = unit / of, tile = of - 1 - (unit - slice * of);
+    float* const part = own ? a.own_part : a.small_part;
+    Tile t;
+    if (own) {
+      t.at<kOwn>(a, tile / blocks, kCols, tile % blocks);
+    } else {
+      const int b = last_at_most(s_first, a.B, tile);
+      if constexpr (Packed) t.at<kPacked>(a, b, kCols, tile - s_first[b]);
+      else t.at<kPrefix>(a, b, kCols, tile - s_first[b], run_entries(a, s_runs, b));
+    }
+    const int per = slice_pages(a.small_least, t.keys.pages, own ? a.own_slices : slices), pb = slice * per,
+              pe = min(t.keys.pages, pb + per);
+    const bool direct = Packed && per >= t.keys.pages;
+    constexpr TileMode Mode = Packed ? kPacked : kOwn;  // (rows of both kinds of shared tiles are entries)
     RowKeys rk[NT];
     int64_t q_at[NT], out_at[NT];
     bool in[NT];
@@ -91,7 +96,7 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
       rk[x] = t.row_keys<Mode>(a, kvh, min(col, t.rows - 1), q_at[x], out_at[x]);
     }
     if (t.state != kFine || pb >= pe) {
-      if (Mode == kPacked && slice == 0 && w == 0) {
+      if (Packed && slice == 0 && w == 0) {
         const float none = t.state == kNone ? __builtin_nanf("") : 0.f;
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
@@ -188,14 +193,14 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
       if (!whole) {
         const RowKeys most{t.keys.p_max, t.keys.low_min};
         st.mask_values([&](int k) { return good && most.seen(t0 + k, t.keys.sink); }, lane);
-        if (Mode == kPacked) odd = __any(st.drop_nonfinite());
+        if (Packed) odd = __any(st.drop_nonfinite());
       }
       st.stage_v(lds, lane);
       if (more) st.load_v(vals(next), tok, lane);
       wave_lds_order();
       st.values(lds, c, g, sc, o);
       wave_lds_order();
-      if (Mode == kPacked && odd)
+      if (Packed && odd)
         add_nonfinite<T, NT, FT>(reinterpret_cast<const T*>(static_cast<const char*>(a.p.v) + now) + t0 % kPage, Step::kTok,
                                  g, [&](int x, int k) { return rk[x].seen(t0 + k, t.keys.sink); }, o);
       now = next;
@@ -255,31 +260,31 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   }
 }
 
-template <template <int, int> class StepOf, int D, int NT, TileMode Mode>
+template <template <int, int> class StepOf, int D, int NT, bool Packed>
 hipError_t launch_small(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
   typedef StepOf<D, NT> Step;
   const size_t lds = std::max<size_t>((size_t)kWaves * Step::kTok * D * Step::kBytes, kWaves / 2 * join_bytes(D, NT));
-  hipLaunchKernelGGL((small_tile_kernel<StepOf, D, NT, Mode>), dim3(grid), dim3(kWaves * kWave), lds, stream, a);
+  hipLaunchKernelGGL((small_tile_kernel<StepOf, D, NT, Packed>), dim3(grid), dim3(kWaves * kWave), lds, stream, a);
   return hipGetLastError();
 }
 
-template <int NT, TileMode Mode, template <int, int> class StepOf>
+template <int NT, bool Packed, template <int, int> class StepOf>
 hipError_t launch_small_width(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
   switch (a.p.d) {
-    case 32: return launch_small<StepOf, 32, NT, Mode>(a, grid, stream);
-    case 64: return launch_small<StepOf, 64, NT, Mode>(a, grid, stream);
-    case 96: return launch_small<StepOf, 96, NT, Mode>(a, grid, stream);
-    case 128: return launch_small<StepOf, 128, NT, Mode>(a, grid, stream);
-    case 160: return launch_small<StepOf, 160, NT, Mode>(a, grid, stream);
-    case 192: return launch_small<StepOf, 192, NT, Mode>(a, grid, stream);
-    case 224: return launch_small<StepOf, 224, NT, Mode>(a, grid, stream);
-    default: return launch_small<StepOf, 256, NT, Mode>(a, grid, stream);
+    case 32: return launch_small<StepOf, 32, NT, Packed>(a, grid, stream);
+    case 64: return launch_small<StepOf, 64, NT, Packed>(a, grid, stream);
+    case 96: return launch_small<StepOf, 96, NT, Packed>(a, grid, stream);
+    case 128: return launch_small<StepOf, 128, NT, Packed>(a, grid, stream);
+    case 160: return launch_small<StepOf, 160, NT, Packed>(a, grid, stream);
+    case 192: return launch_small<StepOf, 192, NT, Packed>(a, grid, stream);
+    case 224: return launch_small<StepOf, 224, NT, Packed>(a, grid, stream);
+    default: return launch_small<StepOf, 256, NT, Packed>(a, grid, stream);
   }
 }
-template <int NT, TileMode Mode>
+template <int NT, bool Packed>
 hipError_t launch_small_type(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
-  return a.p.dtype == LLA_BF16 ? launch_small_width<NT, Mode, StepBf16>(a, grid, stream)
-                               : launch_small_width<NT, Mode, StepF32>(a, grid, stream);
+  return a.p.dtype == LLA_BF16 ? launch_small_width<NT, Packed, StepBf16>(a, grid, stream)
+                               : launch_small_width<NT, Packed, StepF32>(a, grid, stream);
 }
 
 }  // namespace lla

@@ -477,19 +477,23 @@ def slots(pages: PageTable, start, n_new, total: int, *, rows=None, pos=None, ou
 
 
 def _longs(t, name, shape, dev):
-    _need(t, name, torch.int64, dev)
-    if t.shape != shape:
+    if t.dtype is not torch.int64 or t.shape != shape or t.device != dev or not t.is_contiguous() or not t.is_cuda:
+        _need(t, name, torch.int64, dev)
         raise ValueError(f"{name} must have shape {list(shape)}")
 
 
 def _packed(t, name, heads, d, dtype, dev):
     """Stride of tokens of t [total, heads, d], heads and rows dense."""
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [total, heads, width]")
-    _, stride, head = _rows_of(t[None], name, dev, dtype)
-    if t.shape[1:] != (heads, d) or heads > 1 and head != d:
-        raise ValueError(f"{name} must be [total, {heads}, {d}] with dense heads")
-    return stride
+    if t.device != dev or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on {dev}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 3 or t.shape[1:] != (heads, d):
+        raise ValueError(f"{name} must be [total, {heads}, {d}]")
+    stride, head, one = t.stride()
+    if one != 1 or heads > 1 and head != d:
+        raise ValueError(f"{name} must have dense heads and rows")
+    return stride if t.shape[0] > 1 else 0
 
 
 def _no_gradient(*tensors):
