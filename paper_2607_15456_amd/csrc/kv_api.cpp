@@ -431,7 +431,7 @@ lla_status lla_kv_prefill_attn(int dtype, int out_dtype, int B, int total, int H
   a.qscale = (float)((double)scale * kLog2e);
   a.out = out;
   a.lse = lse;
-  a.small_part = static_cast<float*>(workspace);
+  a.small.part = static_cast<float*>(workspace);
   return hip_status(lla::launch_kv_prefill(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -475,7 +475,7 @@ lla_status lla_kv_decode_attn_shared(int dtype, int out_dtype, int B, int H, int
   a.qscale = (float)((double)scale * kLog2e);
   a.out = out;
   a.lse = lse;
-  a.small_part = static_cast<float*>(workspace);
+  a.small.part = static_cast<float*>(workspace);
   return hip_status(lla::launch_kv_shared(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -43,10 +43,10 @@ struct Slices {
   const float* at;
   int64_t stride;
   int count;
-  __device__ __forceinline__ Slices(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices, int least,
-                                    const float* part, int cols, int kvh, int x) {
-    const int per = slice_pages(least, t.keys.pages, slices), row = a.p.d + 4;
-    at = part + (item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
+  __device__ __forceinline__ Slices(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices, const KvTileCut& cut,
+                                    int cols, int kvh, int x) {
+    const int per = slice_pages(cut.least, t.keys.pages, slices), row = a.p.d + 4;
+    at = cut.part + (item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
     stride = (int64_t)tiles * a.p.Hkv * cols * row;
     count = (t.keys.pages + per - 1) / per;
   }
@@ -56,11 +56,12 @@ constexpr int kJoinRows = 32;  // of a tile, that a workgroup joins at a time
 
 // Packed tokens: the tiles that were cut, a workgroup 32 rows of one.
 __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int large_cols) {
-  __shared__ int s_small[kMostEntries + 1], s_large[kMostEntries + 1], s_wave[kWaves];
+  __shared__ int s_small[kMostEntries + 1], s_large[kMostEntries + 1];
+  __shared__ int64_t s_wave[kThreads / kWave];
   count_packed<kThreads>(a, a.small_cols, 0, a.small_rows, s_small, s_wave);
   count_packed<kThreads>(a, large_cols, a.small_rows, kAllRows, s_large, s_wave);
-  const int small = s_small[a.B], small_slices = tile_slices(a, small, a.small_wgs);
-  const int large = s_large[a.B], large_slices = tile_slices(a, large, a.large_wgs);
+  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, (int64_t)small * a.p.Hkv);
+  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, (int64_t)large * a.p.Hkv);
   const int chunks = large_cols / kJoinRows;
   const int64_t of_small = small_slices > 1 ? (int64_t)small * a.p.Hkv : 0;
   const int64_t of_large = large_slices > 1 ? (int64_t)large * a.p.Hkv * chunks : 0;
@@ -77,8 +78,8 @@ __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int
     if (t.state != kFine) continue;
     const int end = min(t.rows, (chunk + 1) * kJoinRows);
     for (int x = chunk * kJoinRows + r; x < end; x += step) {
-      const Slices in = is_small ? Slices(a, t, small, tile, small_slices, a.small_least, a.small_part, cols, kvh, x)
-                                 : Slices(a, t, large, tile, large_slices, a.large_least, a.large_part, cols, kvh, x);
+      const Slices in = is_small ? Slices(a, t, small, tile, small_slices, a.small, cols, kvh, x)
+                                 : Slices(a, t, large, tile, large_slices, a.large, cols, kvh, x);
       if (in.count <= 1) break;  // (written by the tile itself)
       Joined row;
       row.add(in.at, in.stride, in.count, a.p.d, f);
@@ -91,10 +92,11 @@ __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int
 
 // Shared prompts: every (entry, query head), of its prompt's slices and its own.
 __global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
-  __shared__ int s_runs[kMostEntries + 1], s_small[kMostEntries + 1], s_large[kMostEntries + 1], s_wave[kWaves];
+  __shared__ int s_runs[kMostEntries + 1], s_small[kMostEntries + 1], s_large[kMostEntries + 1];
+  __shared__ int64_t s_wave[kThreads / kWave];
   count_shared<kThreads>(a, s_runs, s_small, s_large, s_wave);
-  const int small = s_small[a.B], small_slices = tile_slices(a, small, a.small_wgs);
-  const int large = s_large[a.B], large_slices = tile_slices(a, large, a.large_wgs);
+  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, (int64_t)small * a.p.Hkv);
+  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, (int64_t)large * a.p.Hkv);
   const int group = a.H / a.p.Hkv, cols = a.small_cols, blocks = (group + cols - 1) / cols;
   const int lanes = a.p.d / 4, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
   const int64_t rows = (int64_t)a.B * a.H;
@@ -113,8 +115,8 @@ __global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
       const int of = is_small ? cols : a.prefix_cols, col = (b - e) * group + r, nth = col / of, x = col - nth * of;
       Tile t;
       t.at<kPrefix>(a, e, of, nth, many);
-      const Slices in = is_small ? Slices(a, t, small, s_small[e] + nth, small_slices, a.small_least, a.small_part, of, kvh, x)
-                                 : Slices(a, t, large, s_large[e] + nth, large_slices, a.large_least, a.large_part, of, kvh, x);
+      const Slices in = is_small ? Slices(a, t, small, s_small[e] + nth, small_slices, a.small, of, kvh, x)
+                                 : Slices(a, t, large, s_large[e] + nth, large_slices, a.large, of, kvh, x);
       if (t.state == kFine) row.add(in.at, in.stride, in.count, a.p.d, f);
       else state = kNone;
     }
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
       if (a.lse && f == 0) a.lse[i] = state == kNone ? none : neg_inf();
       continue;
     }
-    const Slices in(a, own, a.B * blocks, b * blocks + r / cols, a.own_slices, a.small_least, a.own_part, cols, kvh, r % cols);
+    const KvTileCut cut{0, a.small.least, 0, 0, a.own_part};
+    const Slices in(a, own, a.B * blocks, b * blocks + r / cols, a.own_slices, cut, cols, kvh, r % cols);
     row.add(in.at, in.stride, in.count, a.p.d, f);
     row.store(a, i, f);
   }
@@ -139,19 +142,20 @@ int most_pages(const KvTileArgs& a, int cols) {
 }
 size_t row_bytes(const KvTileArgs& a) { return (size_t)(a.p.d + 4) * sizeof(float); }
 // Partial tiles, at most: `tiles` tiles cut over the workgroups (two rounds of them).
-int64_t partial_tiles(const KvTileArgs& a, int64_t tiles, int wgs, int least, int cols) {
-  const int64_t each = std::min<int64_t>(a.most, blocks_of(most_pages(a, cols), least));
-  return each <= 1 ? 0 : std::min<int64_t>(2 * wgs, tiles * a.p.Hkv * each);
+int64_t partial_tiles(const KvTileArgs& a, const KvTileCut& cut, int64_t tiles) {
+  return cut.most == 1 ? 0 : std::min<int64_t>(2 * cut.wgs, tiles * a.p.Hkv * cut.most);
 }
 
-constexpr int kSmallLeast = 4, kLargeLeast = 4, kMostSlices = 512;
-void limits(KvTileArgs& a) {
-  const int cus = device_cu_count();
-  a.small_least = kSmallLeast;
-  a.large_least = kLargeLeast;
-  a.most = blocks_of(a.n_ctx, kPage) <= kSmallLeast ? 1 : kMostSlices;
-  a.small_wgs = 2 * cus;
-  a.large_wgs = cus;
+// A slice keeps a step for each of a small tile's wavefronts (bf16: a page, fp32: half of
+// one), and four pages of a large tile; a tile gets no more slices than its longest has such.
+constexpr int kMostSlices = 512;
+void limits(KvTileArgs& a, int cols) {
+  const int cus = device_cu_count(), pages = most_pages(a, cols);
+  auto cut = [&](int least, int wgs) {
+    return KvTileCut{(int)std::min<int64_t>(kMostSlices, blocks_of(pages, least)), least, wgs, 0, nullptr};
+  };
+  a.small = cut(a.p.dtype == LLA_F32 ? 2 : 4, 2 * cus);
+  a.large = cut(4, cus);
 }
 
 // Rows of a small tile: two products' columns where a group of heads is more than one's.
@@ -166,8 +170,8 @@ struct PackedShape {
     small_tiles = a.small_rows == 0 ? 0
                   : a.small_rows == kAllRows ? std::min(rows / a.small_cols + a.B, rows) : std::min(a.B, a.total);
     large_tiles = rows > a.small_rows ? std::min(rows / cols + a.B, blocks_of(rows, a.small_rows + 1)) : 0;
-    small_partial = partial_tiles(a, small_tiles, a.small_wgs, a.small_least, a.small_cols);
-    large_partial = partial_tiles(a, large_tiles, a.large_wgs, a.large_least, cols);
+    small_partial = partial_tiles(a, a.small, small_tiles);
+    large_partial = partial_tiles(a, a.large, large_tiles);
   }
   size_t bytes(const KvTileArgs& a) const {
     return (size_t)(small_partial * a.small_cols + large_partial * large_cols(a.p.d)) * row_bytes(a);
@@ -180,7 +184,7 @@ struct PackedShape {
 // small tiles keep them as busy (3 entries of 301 .. 101 tokens over 1020 of a window, 24
 // heads on 8 of 96: 108 us; with large fp32 tiles 134).
 size_t kv_prefill_shape(KvTileArgs& a) {
-  limits(a);
+  limits(a, large_cols(a.p.d));
   a.small_cols = small_cols_of(a);
   // a single entry is of one kind of tile, so one launch does
   const bool one_large = a.B == 1 && (int64_t)a.total * (a.H / a.p.Hkv) > a.small_cols;
@@ -195,13 +199,15 @@ size_t kv_prefill_workspace(const KvTileArgs& a) {
 hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
   KvTileArgs a = args;
   const PackedShape s(a);
-  a.large_part = a.small_part + s.small_partial * a.small_cols * (a.p.d + 4);
+  a.small.tiles = s.small_tiles;
+  a.large.tiles = s.large_tiles;
+  a.large.part = a.small.part + s.small_partial * a.small_cols * (a.p.d + 4);
   hipError_t e = hipSuccess;
   // (a workgroup takes another tile where there are more)
   auto grid = [&](int64_t tiles, int64_t partial) { return (unsigned)std::min<int64_t>(std::max(partial, tiles * a.p.Hkv), 1 << 16); };
   if (s.large_tiles) e = launch_large_packed(a, grid(s.large_tiles, s.large_partial), stream);
   if (e != hipSuccess) return e;
-  if (s.small_tiles) e = launch_small_packed(a, grid(s.small_tiles, s.small_partial), stream);
+  if (s.small_tiles) e = launch_small_packed(a, grid(s.small_tiles, std::min<int64_t>(s.small_partial, a.small.wgs)), stream);
   if (e != hipSuccess || s.small_partial + s.large_partial == 0) return e;
   const int64_t joins = s.small_partial + s.large_partial * (large_cols(a.p.d) / kJoinRows);
   hipLaunchKernelGGL(join_packed_kernel, dim3((unsigned)std::min<int64_t>(joins, 1024)), dim3(kThreads), 0, stream, a,
@@ -211,17 +217,18 @@ hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
 
 namespace {
 struct SharedShape {
+  int64_t small_tiles, large_tiles;
   int64_t small, large, own;  // partial tiles: over prompts, small and large, and entries' own
   explicit SharedShape(const KvTileArgs& a) {
     const int group = a.H / a.p.Hkv;
     const int64_t rows = (int64_t)a.B * group, blocks = blocks_of(group, a.prefix_cols);
-    auto items = [&](int64_t tiles, int wgs, int least, int cols) {
-      return tiles ? std::max(partial_tiles(a, tiles, wgs, least, cols), tiles * a.p.Hkv) : 0;
-    };
+    auto items = [&](const KvTileCut& cut, int64_t tiles) { return std::max(partial_tiles(a, cut, tiles), tiles * a.p.Hkv); };
     // any entry may begin a run; large tiles are of runs of more than small_rows rows
     const int64_t runs = std::min<int64_t>(a.B, rows / (a.small_rows + (int64_t)1));
-    small = items(a.small_rows == kAllRows ? a.B * blocks : a.B, a.small_wgs, a.small_least, a.small_cols);
-    large = items(runs * blocks, a.large_wgs, a.large_least, a.prefix_cols);
+    small_tiles = a.small_rows == kAllRows ? a.B * blocks : a.B;
+    large_tiles = runs * blocks;
+    small = items(a.small, small_tiles);
+    large = items(a.large, large_tiles);
     own = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols) * a.own_slices;
   }
   size_t bytes(const KvTileArgs& a) const {
@@ -231,7 +238,7 @@ struct SharedShape {
 }  // namespace
 
 size_t kv_shared_shape(KvTileArgs& a) {
-  limits(a);
+  limits(a, 0);
   const int group = a.H / a.p.Hkv;
   a.small_cols = small_cols_of(a);
   const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols);
@@ -239,7 +246,7 @@ size_t kv_shared_shape(KvTileArgs& a) {
   a.small_rows = all_small ? kAllRows : a.small_cols;
   a.prefix_cols = all_small ? a.small_cols : large_cols(a.p.d);
   a.own_slices =
-      (int)std::max<int64_t>(1, std::min<int64_t>(a.small_wgs / units, blocks_of(blocks_of(a.n_ctx, kPage), a.small_least)));
+      (int)std::max<int64_t>(1, std::min<int64_t>(a.small.wgs / units, a.small.most));
   return SharedShape(a).bytes(a);
 }
 // Of any smaller batch: the partial tiles over prompts grow with the entries, and of own
@@ -248,16 +255,18 @@ size_t kv_shared_workspace(const KvTileArgs& a) {
   KvTileArgs x = a;
   kv_shared_shape(x);
   SharedShape s(x);
-  const int64_t units = s.own / x.own_slices, pages = blocks_of(blocks_of(a.n_ctx, kPage), x.small_least);
-  s.own = std::min(std::max<int64_t>(x.small_wgs, units), units * pages);
+  const int64_t units = s.own / x.own_slices;
+  s.own = std::min(std::max<int64_t>(x.small.wgs, units), units * x.small.most);
   return s.bytes(x);
 }
 
 hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
   KvTileArgs a = args;
   const SharedShape s(a);
-  a.own_part = a.small_part + s.small * a.small_cols * (a.p.d + 4);
-  a.large_part = a.own_part + s.own * a.small_cols * (a.p.d + 4);
+  a.small.tiles = s.small_tiles;
+  a.large.tiles = s.large_tiles;
+  a.own_part = a.small.part + s.small * a.small_cols * (a.p.d + 4);
+  a.large.part = a.own_part + s.own * a.small_cols * (a.p.d + 4);
   auto grid = [](int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 16); };
   hipError_t e = hipSuccess;
   if (s.large) e = launch_large_prefix(a, grid(s.large), stream);

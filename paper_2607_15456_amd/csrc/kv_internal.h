@@ -68,6 +68,15 @@ size_t kv_decode_shape(KvDecodeArgs& a);
 // The most that it takes for any B and n_ctx up to a's.
 size_t kv_decode_workspace(const KvDecodeArgs& a);
 
+// How tiles are cut into slices of their pages: slices of a tile at most, pages of a slice
+// at least, the workgroups that they are shared out to, the tiles that there is room for
+// (more are of offsets that decrease, and left out), and their partial rows.
+struct KvTileCut {
+  int most, least, wgs;
+  int64_t tiles;
+  float* part;
+};
+
 // Attention of packed tokens (offset, start), and of entries that share a prompt
 // (length, lead, shared), over the pages.
 struct KvTileArgs {
@@ -85,18 +94,13 @@ struct KvTileArgs {
   float qscale;
   void* out;
   float* lse;
-  // slices of a tile at most (1: none is cut); pages of a slice at least, of small tiles and large ones
-  int most, small_least, large_least;
-  // workgroups that small tiles and large ones are shared out to
-  int small_wgs, large_wgs;
+  KvTileCut small, large;
   // rows up to which a packed entry, or a run of entries that share a prompt, is of small tiles
   int small_rows;
   // rows of a small tile, and at which a run is cut into tiles
   int small_cols, prefix_cols;
   // slices that an entry's own tokens are cut into, at most
   int own_slices;
-  float* small_part;
-  float* large_part;
   float* own_part;
 };
 // Choose how the work is cut; return the workspace bytes that this takes.

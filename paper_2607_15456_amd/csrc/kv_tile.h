@@ -5,8 +5,8 @@
 // A tile is up to kCols rows (token or entry, query head of the group) that read the
 // same pages for one key head.  How many tiles a call has is known on the device
 // alone, by the offsets of a packed batch or the groups of a shared one, so each
-// workgroup counts them itself (a prefix sum over at most 1024 entries, 1 us), and with
-// fewer tiles than workgroups the pages of each are split.
+// workgroup counts them itself (a prefix sum over at most 1024 entries), and with fewer
+// tiles than workgroups the pages of each are split.
 #pragma once
 
 #include "kv_internal.h"
@@ -92,17 +92,18 @@ struct EntryCounts {
   static constexpr int kEach = (kMostEntries + kThreads - 1) / kThreads;
   int n[kEach];
   __device__ __forceinline__ static int entry(int i) { return threadIdx.x * kEach + i; }
-  __device__ __forceinline__ void sum(int B, int* s_first, int* s_wave) const {
-    int total = 0;
+  // (sums past 32 bits, of offsets that decrease, stop there)
+  __device__ __forceinline__ void sum(int B, int* s_first, int64_t* s_wave) const {
+    int64_t total = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) total += n[i];
-    int at = prefix_sum<kThreads>(total, s_wave);
+    int64_t at = prefix_sum<kThreads>(total, s_wave);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int b = entry(i);
-      if (b < B) s_first[b] = at;
+      if (b < B) s_first[b] = (int)min(at, (int64_t)kAllRows);
       at += n[i];
-      if (b == B - 1) s_first[B] = at;
+      if (b == B - 1) s_first[B] = (int)min(at, (int64_t)kAllRows);
     }
     __syncthreads();
   }
@@ -110,7 +111,7 @@ struct EntryCounts {
 
 // Packed entries with more than `over` and at most `upto` rows.
 template <int kThreads>
-__device__ __forceinline__ void count_packed(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int* s_wave) {
+__device__ __forceinline__ void count_packed(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int64_t* s_wave) {
   const int group = a.H / a.p.Hkv;
   EntryCounts<kThreads> c;
 #pragma unroll
@@ -186,7 +187,8 @@ __host__ __device__ __forceinline__ int tile_entries(int group, int cols) { retu
 // of the one before them; then the tiles of at most small_rows rows, which are small
 // ones, and the others, where an array for them is given.
 template <int kThreads>
-__device__ __forceinline__ void count_shared(const KvTileArgs& a, int* s_runs, int* s_small, int* s_large, int* s_wave) {
+__device__ __forceinline__ void count_shared(const KvTileArgs& a, int* s_runs, int* s_small, int* s_large,
+                                             int64_t* s_wave) {
   const int group = a.H / a.p.Hkv, each = tile_entries(group, a.prefix_cols);
   EntryCounts<kThreads> c, small, large;
   bool begins[c.kEach];
@@ -223,13 +225,14 @@ __device__ __forceinline__ int run_entries(const KvTileArgs& a, const int* s_run
   return last_at_most(s_runs, a.B + 1, s_runs[b + 1]) - b;
 }
 
+// The tiles that are worked on, of those that were counted.
+__device__ __forceinline__ int tiles_of(const KvTileCut& cut, int counted) { return (int)min((int64_t)counted, cut.tiles); }
 // Slices that every tile may be cut into, where there are fewer tiles than workgroups:
 // as many as give each a workgroup, or so many that two rounds of workgroups do better.
-__device__ __forceinline__ int tile_slices(const KvTileArgs& a, int tiles, int workgroups) {
-  const int64_t units = (int64_t)tiles * a.p.Hkv;
-  if (units == 0 || a.most == 1) return 1;
-  const int one = (int)max((int64_t)1, workgroups / units), two = (int)(2 * workgroups / units);
-  return min(a.most, 9 * two > 20 * one ? two : one);
+__device__ __forceinline__ int tile_slices(const KvTileCut& cut, int64_t units) {
+  if (units == 0 || cut.most == 1) return 1;
+  const int one = (int)max((int64_t)1, cut.wgs / units), two = (int)(2 * cut.wgs / units);
+  return min(cut.most, 9 * two > 20 * one ? two : one);
 }
 __device__ __forceinline__ int slice_pages(int least, int pages, int slices) {
   return slices == 1 ? max(pages, 1) : max(least, (pages + slices - 1) / slices);

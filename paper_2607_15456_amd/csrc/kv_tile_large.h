@@ -198,7 +198,8 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   typedef LargeTile<D, Terms> L;
   constexpr int kCols = L::kCols, kThreads = L::kThreads, KT = L::KT, FT = L::FT, kTok = L::kTok;
   constexpr int kHeadBytes = kPage * D * 2;
-  __shared__ int s_first[kMostEntries + 1], s_runs[kMostEntries + 1], s_wave[kThreads / kWave];
+  __shared__ int s_first[kMostEntries + 1], s_runs[kMostEntries + 1];
+  __shared__ int64_t s_wave[kThreads / kWave];
   __shared__ int s_odd[2];  // step + 1 whose values were not all finite, of either buffer
   extern __shared__ __align__(16) char s_raw[];
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 32, hf = lane / 32;
@@ -220,7 +221,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
     int kvh, pb, pe;
     {
       const KvTileArgs& a = args_again();
-      const int tiles = s_first[a.B], slices = tile_slices(a, tiles, a.large_wgs);
+      const int tiles = tiles_of(a.large, s_first[a.B]), slices = tile_slices(a.large, (int64_t)tiles * a.p.Hkv);
       if (item >= (int64_t)tiles * a.p.Hkv * slices) break;
       const int unit = (int)(item / a.p.Hkv), slice = unit / tiles, tile = tiles - 1 - (unit - slice * tiles);
       kvh = (int)(item % a.p.Hkv);
@@ -229,7 +230,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
         if (slices == 1 && a.B > 1) HeavyFirst{s_first, s_runs, a.B}.find(unit, last_from, b, nth);
       }
       t.at<Mode>(a, b, kCols, nth, Mode == kPacked ? 1 : run_entries(a, s_runs, b));
-      const int per = slice_pages(a.large_least, t.keys.pages, slices);
+      const int per = slice_pages(a.large.least, t.keys.pages, slices);
       pb = slice * per;
       pe = min(t.keys.pages, pb + per);
       if (t.state != kFine || pb >= pe) {
@@ -449,7 +450,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
         }
       if (a.lse && hf == 0) a.lse[out_at] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
-      float* to = partial_row(a.large_part, item, kCols, col, D);
+      float* to = partial_row(a.large.part, item, kCols, col, D);
 #pragma unroll
       for (int f = 0; f < FT; ++f)
 #pragma unroll

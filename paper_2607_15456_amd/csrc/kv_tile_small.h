@@ -48,7 +48,8 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
   constexpr int kRow = D + 4, kCols = NT * kTile, kThreads = kWaves * kWave, W = kWaves;
-  __shared__ int s_first[kMostEntries + 1], s_runs[Packed ? 1 : kMostEntries + 1], s_wave[kThreads / kWave];
+  __shared__ int s_first[kMostEntries + 1], s_runs[Packed ? 1 : kMostEntries + 1];
+  __shared__ int64_t s_wave[kThreads / kWave];
   // the wavefronts' steps, then what they join
   extern __shared__ __align__(16) char s_raw[];
   float* const s_o = reinterpret_cast<float*>(s_raw);
@@ -66,14 +67,14 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
     if (!own && tiles < 0) {
       if constexpr (Packed) count_packed<kThreads>(a, kCols, 0, a.small_rows, s_first, s_wave);
       else count_shared<kThreads>(a, s_runs, s_first, nullptr, s_wave);
-      tiles = s_first[a.B];
-      slices = tile_slices(a, tiles, a.small_wgs);
+      tiles = tiles_of(a.small, s_first[a.B]);
+      slices = tile_slices(a.small, (int64_t)tiles * a.p.Hkv);
     }
     const int64_t item = own ? i : i - own_items;
     if (!own && item >= (int64_t)tiles * a.p.Hkv * slices) break;
     const int kvh = (int)(item % a.p.Hkv), unit = (int)(item / a.p.Hkv), of = own ? a.B * blocks : tiles;
     const int slice = unit / of, tile = of - 1 - (unit - slice * of);
-    float* const part = own ? a.own_part : a.small_part;
+    float* const part = own ? a.own_part : a.small.part;
     Tile t;
     if (own) {
       t.at<kOwn>(a, tile / blocks, kCols, tile % blocks);
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
       if constexpr (Packed) t.at<kPacked>(a, b, kCols, tile - s_first[b]);
       else t.at<kPrefix>(a, b, kCols, tile - s_first[b], run_entries(a, s_runs, b));
     }
-    const int per = slice_pages(a.small_least, t.keys.pages, own ? a.own_slices : slices), pb = slice * per,
+    const int per = slice_pages(a.small.least, t.keys.pages, own ? a.own_slices : slices), pb = slice * per,
               pe = min(t.keys.pages, pb + per);
     const bool direct = Packed && per >= t.keys.pages;
     constexpr TileMode Mode = Packed ? kPacked : kOwn;  // (rows of both kinds of shared tiles are entries)

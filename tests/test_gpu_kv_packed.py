@@ -8,7 +8,8 @@ times a constant of one rounding, its difference to the maximum one more: off by
 e = (d + 4) eps scale max_n sum|q k|; the exponential adds 2^-21.  A weight and the
 sum of weights are each off by that, sums over N tokens by their longest chains
 (N / 16 + 64) eps, all relative to sum p |v|.  Weights rounded to bf16 add 2^-8 in the
-numerator and, as they are summed as rounded, as much in the denominator.
+numerator and, as they are summed as rounded, as much in the denominator; weights
+of 16 bits (over a shared prompt, with results in bf16) 2^-16 in the numerator.
 """
 
 import numpy as np
@@ -61,7 +62,7 @@ def bounds(q, k, v, seen, scale, dtype, out_dtype, rounded):
     out, spread = p @ v / total, p @ np.abs(v) / total
     e = (q.shape[1] + 4) * EPS * np.max(np.where(seen, mag, 0.0), axis=1, keepdims=True)
     n = seen.sum(axis=1, keepdims=True)
-    off = 2 * e + 2 * 2.0 ** -21 + 2 * (n / 16 + 64) * EPS + (2 * 2.0 ** -8 if rounded else 0.0)
+    off = 2 * e + 2 * 2.0 ** -21 + 2 * (n / 16 + 64) * EPS + rounded
     tol = off * spread * (1 + half_step(out_dtype)) + half_step(out_dtype) * np.abs(out) + 1e-30
     lse = (top + np.log(total))[:, 0]
     return out, lse, tol, (off + 4 * EPS * np.abs(lse)[:, None] + 1e-6)[:, 0]
@@ -109,7 +110,7 @@ def prefill_reference(q, k_pages, v_pages, table, offset, start, rows, scale, si
         for h in range(q.shape[1]):
             k, v = places(table, row, n, k_pages, v_pages, h // group)
             out[t0:t1, h], lse[t0:t1, h], tol[t0:t1, h], lse_tol[t0:t1, h] = bounds(
-                q[t0:t1, h], k, v, seen, scale, dtype, out_dtype, dtype == BF and out_dtype == BF)
+                q[t0:t1, h], k, v, seen, scale, dtype, out_dtype, 2 * 2.0 ** -8 if dtype == BF and out_dtype == BF else 0.0)
     return out, lse, tol, lse_tol
 
 
@@ -374,6 +375,26 @@ def test_prefill_padding_and_bad_indices(dtype, long):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("offsets", [[0, 300, 0, 300, 0, 300], [300, 0, 300, 0], [-5, 400, -(1 << 31), (1 << 31) - 1, 3], [7] * 6])
+def test_prefill_offsets_that_decrease_do_no_harm(dtype, offsets):
+    """Which tokens are done is not defined; nothing but the results and the workspace is written, and a call after it is whole."""
+    B, total = len(offsets) - 1, 300
+    table, n_pages = pages_for([1200] * B, np.random.default_rng(0))
+    kp, vp = pool(1, n_pages, 2, 64, dtype)
+    q = normal((total, 4, 64), 2, dtype)
+    need = kv.prefill_workspace_bytes(dtype, B, total, 4, 2, 64, 1216)
+    ws = torch.full((need + 65536,), 90, dtype=torch.uint8, device=DEV)
+    out = torch.full((total + 64, 4, 64), 7.0, device=DEV)
+    before = kp.clone(), vp.clone()
+    kv.prefill_attn(q, kp, vp, ints(table), ints(offsets), ints([800] * B), n_ctx=1216, out=out[:total], workspace=ws[:need])
+    assert (ws[need:] == 90).all() and (out[total:] == 7).all()
+    assert torch.equal(kp, before[0]) and torch.equal(vp, before[1])
+    kv.prefill_attn(q, kp, vp, ints(table[:1]), ints([0, total]), ints([900]), n_ctx=1216, out=out[:total], workspace=ws[:need])
+    ref = prefill_reference(q, kp, vp, table[:1], [0, total], [900], None, 1 / 8, 0, 0, dtype, F32)
+    near(out[:total], ref[0], ref[2], "after it")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("n,start", [(2, 70), (40, 50), (300, 100)])
 def test_prefill_masked_places_may_hold_anything(dtype, bad, n, start):
@@ -485,7 +506,8 @@ def check_shared(dtype, out_dtype, H, H_kv, d, groups, seed=0, rows=None, scale=
             k[:shared[b]], v[:shared[b]] = first
             hs = slice(g * H // H_kv, (g + 1) * H // H_kv)
             ref[b, hs], ref_lse[b, hs], tol[b, hs], lse_tol[b, hs] = bounds(
-                qn[b, hs], k, v, np.ones((H // H_kv, ends[b]), dtype=bool), s, dtype, out_dtype, False)
+                qn[b, hs], k, v, np.ones((H // H_kv, ends[b]), dtype=bool), s, dtype, out_dtype,
+                2.0 ** -16 if dtype == BF and out_dtype == BF else 0.0)
     what = f"shared {dtype} {out_dtype} H={H}/{H_kv} d={d} {[(p, m[:3], len(m)) for p, m in groups][:4]}"
     some = np.array(ends) > 0
     near(out[torch.as_tensor(some)], ref[some], tol[some], what)
@@ -541,7 +563,7 @@ def test_shared_padding_and_bad_indices(dtype):
         for h in range(4):
             k, v = places(table, rows[b], 200, kn, vn, h // 2)
             k[:shared[b]], v[:shared[b]] = places(table, rows[lead[b]], shared[b], kn, vn, h // 2)
-            ref, _, tol, _ = bounds(qn[b, h:h + 1], k, v, np.ones((1, 200), dtype=bool), 1 / 8, dtype, F32, False)
+            ref, _, tol, _ = bounds(qn[b, h:h + 1], k, v, np.ones((1, 200), dtype=bool), 1 / 8, dtype, F32, 0.0)
             near(out[b, h:h + 1], ref, tol, f"entry {b}")
             if b in (0, 11):
                 near(plain[b, h:h + 1], ref, tol, f"decode of {b}")
@@ -627,7 +649,7 @@ def history_attention(server, history, x, lens):
             g = h * G // H
             # a turned value may round to its other neighbour: one step more of q and k in each score
             o[:, h], _, t[:, h], _ = bounds(q[:, h], k[:, g], v[:, g], seen, d ** -0.5, server.dtype, server.dtype,
-                                            server.dtype == BF)
+                                            2 * 2.0 ** -8 if server.dtype == BF else 0.0)
             mag = np.max(np.abs(q[:, h]) @ np.abs(k[:, g]).T, axis=1, keepdims=True) * d ** -0.5
             flips = 2.0 ** -7 if server.dtype == BF else 2.0 ** -20
             t[:, h] += 2 * 2 * flips * mag * np.max(np.abs(v[:, g]))
