@@ -8,7 +8,9 @@
  * table: rotary positions for queries and keys, the write of new tokens, the
  * attention of one new token over the pages, and the pages' bookkeeping on the
  * device (room for new tokens, sharing, copy on write, freeing, keeping a part
- * of the tokens), so that a whole decode step can be captured into a graph.
+ * of the tokens), so that a whole decode step can be captured into a graph.  Steps
+ * whose entries bring different numbers of tokens are packed batches, with causal
+ * attention over the pages; sequences that share a prompt read it once.
  *
  * lla.h's conventions hold: caller-owned device pointers, 16-byte aligned
  * (index arrays 4-byte); scalar arguments and pointers checked on the host

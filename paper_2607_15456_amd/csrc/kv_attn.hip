@@ -158,8 +158,10 @@ void limits(KvTileArgs& a, int cols) {
   a.large = cut(4, cus);
 }
 
-// Rows of a small tile: two products' columns where a group of heads is more than one's.
-int small_cols_of(const KvTileArgs& a) { return a.H / a.p.Hkv > 16 ? 32 : 16; }
+// Rows of a small tile: two products' columns where a group of heads is more than one's, and
+// for packed tokens of wide heads: two wavefronts a SIMD, which one column leaves room
+// for, hold no more registers than the step takes, and its masks need some.
+int small_cols_of(const KvTileArgs& a, bool packed) { return a.H / a.p.Hkv > 16 || (packed && a.p.d > 96) ? 32 : 16; }
 
 struct PackedShape {
   int64_t small_tiles, large_tiles, small_partial, large_partial;
@@ -185,7 +187,7 @@ struct PackedShape {
 // heads on 8 of 96: 108 us; with large fp32 tiles 134).
 size_t kv_prefill_shape(KvTileArgs& a) {
   limits(a, large_cols(a.p.d));
-  a.small_cols = small_cols_of(a);
+  a.small_cols = small_cols_of(a, true);
   // a single entry is of one kind of tile, so one launch does
   const bool one_large = a.B == 1 && (int64_t)a.total * (a.H / a.p.Hkv) > a.small_cols;
   a.small_rows = a.p.dtype == LLA_F32 ? kAllRows : one_large ? 0 : a.small_cols;
@@ -240,7 +242,7 @@ struct SharedShape {
 size_t kv_shared_shape(KvTileArgs& a) {
   limits(a, 0);
   const int group = a.H / a.p.Hkv;
-  a.small_cols = small_cols_of(a);
+  a.small_cols = small_cols_of(a, false);
   const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols);
   const bool all_small = a.p.dtype == LLA_F32;
   a.small_rows = all_small ? kAllRows : a.small_cols;

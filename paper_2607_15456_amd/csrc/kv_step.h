@@ -105,21 +105,23 @@ struct StepBf16 {
     for (int j = 0; j < kLoads; ++j)
       v[j] = uint4{v[j].x & keep[0], v[j].y & keep[1], v[j].z & keep[2], v[j].w & keep[3]};
   }
-  // values that are not finite become zero; whether any was
-  __device__ __forceinline__ bool drop_nonfinite() {
-    bool any = false;
+  // mask_values, and values that are not finite become zero, too; whether the lane had such
+  template <typename Seen>
+  __device__ __forceinline__ bool finite_values(const Seen& seen, int lane) {
+    uint32_t all = 0;
+    mask_values(seen, lane);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool lo = (w[i] & 0x7f80u) == 0x7f80u, hi = (w[i] & 0x7f800000u) == 0x7f800000u;
-        any |= lo || hi;
-        w[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+        const uint32_t odd = ((w[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // (exponents of ones carry over)
+        all |= odd;
+        w[i] &= ~((odd << 1) - (odd >> 15));  // (a half word of ones for its bit)
       }
       v[j] = uint4{w[0], w[1], w[2], w[3]};
     }
-    return any;
+    return all != 0;
   }
   __device__ __forceinline__ void stage_v(char* lds, int lane) const {
 #pragma unroll
@@ -221,15 +223,17 @@ struct StepF32 {
       for (int j = 0; j < kLoads; ++j) v[j][e] = in ? v[j][e] : 0.f;
     }
   }
-  __device__ __forceinline__ bool drop_nonfinite() {
+  template <typename Seen>
+  __device__ __forceinline__ bool finite_values(const Seen& seen, int lane) {
     bool any = false;
+    mask_values(seen, lane);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool bad = (__float_as_uint(v[j][e]) & 0x7f800000u) == 0x7f800000u;
-        any |= bad;
-        v[j][e] = bad ? 0.f : v[j][e];
+        const bool odd = (__float_as_uint(v[j][e]) & 0x7f800000u) == 0x7f800000u;
+        any |= odd;
+        v[j][e] = odd ? 0.f : v[j][e];
       }
     return any;
   }

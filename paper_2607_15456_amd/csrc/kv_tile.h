@@ -348,4 +348,54 @@ __device__ __forceinline__ void store_row4(const KvTileArgs& a, int64_t i, int f
   }
 }
 
+// The kernel's arguments, read again from memory: a value that is needed before and after
+// the steps need not be held meanwhile.
+__device__ __forceinline__ const KvTileArgs& args_again() {
+  typedef const KvTileArgs __attribute__((address_space(4))) Kernarg;
+  Kernarg* p = (Kernarg*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const KvTileArgs*)p;
+}
+
+// Values that are not finite, of tokens that only some of a tile's rows attend, stay out
+// of the matrix product (a weight of zero would make NaN of them).  This adds them to the
+// stored results, or partial rows, of the rows that attend them; rare, so nothing of it is
+// held in registers meanwhile.  part: the tile's partial rows, or NULL.
+template <TileMode Mode, typename T, int D, int kThreads>
+__device__ __forceinline__ void add_nonfinite(const KvTileArgs& a, const Tile& t, int kvh, int pb, int pe, float* part) {
+  constexpr int N = Elem<T>::kPer16B;
+  __syncthreads();  // the results are stored
+#pragma unroll 1
+  for (int e = threadIdx.x; e < t.rows * D; e += kThreads) {
+    const int x = e / D, f = e - x * D;
+    int64_t q_at, out_at;
+    const RowKeys rk = t.row_keys<Mode>(a, kvh, x, q_at, out_at);
+    float sum = 0.f;
+    bool any = false;
+#pragma unroll 1
+    for (int i = pb; i < pe; ++i) {
+      const int t0 = t.keys.page(i) * kPage, page = a.p.table[(int64_t)t.row * a.p.max_pages + t.keys.page(i)];
+      if (t.keys.whole(t0, kPage) || page < 0 || page >= a.p.n_pages) continue;
+      const T* v = static_cast<const T*>(a.p.v) + (((int64_t)page * a.p.Hkv + kvh) * D + f) * kPage;
+#pragma unroll 1
+      for (int k = 0; k < kPage; k += N) {
+        float y[N];
+        Elem<T>::unpack(ld16(v + k), y);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if ((__float_as_uint(y[n]) & 0x7f800000u) == 0x7f800000u && rk.seen(t0 + k + n, t.keys.sink)) {
+            sum += y[n];
+            any = true;
+          }
+      }
+    }
+    if (!any) continue;
+    const int64_t at = out_at * D + f;
+    if (part) part[x * (D + 4) + f] += sum;
+    else if (a.out_dtype == 1) static_cast<bf16_t*>(a.out)[at] = f32_to_bf16(bf16_to_f32(static_cast<bf16_t*>(a.out)[at]) + sum);
+    else static_cast<float*>(a.out)[at] += sum;
+  }
+  __syncthreads();
+}
+
 }  // namespace lla

@@ -184,15 +184,6 @@ __device__ __forceinline__ float max_halves(float x) {
 // most 2^-8 of a power below (1 operation instead of 2 for each score).
 constexpr float kFar = 65536.f;
 
-// The kernel's arguments, read again from memory: a value that is needed before and after
-// the steps need not be held meanwhile.
-__device__ __forceinline__ const KvTileArgs& args_again() {
-  typedef const KvTileArgs __attribute__((address_space(4))) Kernarg;
-  Kernarg* p = (Kernarg*)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(p));
-  return *(const KvTileArgs*)p;
-}
-
 template <int D, int Terms, TileMode Mode>
 __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_kernel(KvTileArgs args) {
   typedef LargeTile<D, Terms> L;
@@ -200,7 +191,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   constexpr int kHeadBytes = kPage * D * 2;
   __shared__ int s_first[kMostEntries + 1], s_runs[kMostEntries + 1];
   __shared__ int64_t s_wave[kThreads / kWave];
-  __shared__ int s_odd[2];  // step + 1 whose values were not all finite, of either buffer
+  __shared__ int s_odd;  // whether values of tokens that only some rows attend were not finite
   extern __shared__ __align__(16) char s_raw[];
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 32, hf = lane / 32;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -299,7 +290,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
         const int t0 = first_token(s);
         const RowKeys most{t.keys.p_max, t.keys.low_min};
         const bool odd = st.drop_nonfinite(w, lane, [&](int k) { return most.seen(t0 + k, sink); });
-        if (__any(odd) && lane == 0) s_odd[s & 1] = s + 1;
+        if (__any(odd) && lane == 0) s_odd = 1;
       }
       st.stage(s_raw + (s & 1) * L::kBuffer, w, lane);
     };
@@ -311,7 +302,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
     f32x16 o[FT];
 #pragma unroll
     for (int f = 0; f < FT; ++f) o[f] = f32x16{0.f};
-    if (tid < 2) s_odd[tid] = 0;
+    if (tid == 0) s_odd = 0;
     int now = page_of(s), next = s + 1 < end ? page_of(s + 1) : -1;
     bool whole = t.keys.whole(first_token(s), kTok);
     request(now, s);
@@ -382,23 +373,6 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], by, less));
       l += st.values(lds, ahead, c, hf, sc, o);
-      if (kMasked && s_odd[s & 1] == s + 1) {
-        // values that are not finite, left out of the product: to the rows that attend them
-        const bf16_t* v = reinterpret_cast<const bf16_t*>(v_pool + now * page_bytes) + t0 % kPage;
-#pragma unroll 1
-        for (int k = 0; k < kTok; ++k) {
-          const bool seen = rk.seen(t0 + k, sink);
-#pragma unroll
-          for (int f = 0; f < FT; ++f) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float y = bf16_to_f32(v[(32 * f + 8 * (i / 4) + 4 * hf + i % 4) * kPage + k]);
-              if (seen && (__float_as_uint(y) & 0x7f800000u) == 0x7f800000u) o[f][i] += y;
-              if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
-          }
-        }
-      }
     };
     // the next step's pages are asked for before a step and put after it
     while (s < end) {
@@ -431,37 +405,41 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
     }
 
     const KvTileArgs& a = args_again();
+    const bool odd = s_odd != 0, direct = Mode == kPacked && pb == 0 && pe == t.keys.pages;
+    float* const part = partial_row(a.large.part, item, kCols, 0, D);
     l += xor_shfl(l, 32);
     const int col = 32 * w + c;
-    if (col >= t.rows) continue;
-    int64_t q_at, out_at;
-    t.row_keys<Mode>(a, kvh, col, q_at, out_at);
-    if (t.past_bound<Mode>(a, col)) l = __builtin_nanf("");
-    if (Mode == kPacked && pb == 0 && pe == t.keys.pages) {
-      const float by = 1.f / l;
+    if (col < t.rows) {
+      int64_t q_at, out_at;
+      t.row_keys<Mode>(a, kvh, col, q_at, out_at);
+      if (t.past_bound<Mode>(a, col)) l = __builtin_nanf("");
+      if (direct) {
+        const float by = 1.f / l;
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
+        for (int f = 0; f < FT; ++f)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          f32x4 v;
+          for (int y = 0; y < 4; ++y) {
+            f32x4 v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = o[f][4 * y + e] * by;
-          store_row4(a, out_at, 32 * f + 8 * y + 4 * hf, v);
+            for (int e = 0; e < 4; ++e) v[e] = o[f][4 * y + e] * by;
+            store_row4(a, out_at, 32 * f + 8 * y + 4 * hf, v);
+          }
+        if (a.lse && hf == 0) a.lse[out_at] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+      } else {
+        float* to = part + col * (D + 4);
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            *reinterpret_cast<f32x4*>(to + 32 * f + 8 * y + 4 * hf) =
+                f32x4{o[f][4 * y], o[f][4 * y + 1], o[f][4 * y + 2], o[f][4 * y + 3]};
+        if (hf == 0) {
+          to[D] = m;
+          to[D + 1] = l;
         }
-      if (a.lse && hf == 0) a.lse[out_at] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
-    } else {
-      float* to = partial_row(a.large.part, item, kCols, col, D);
-#pragma unroll
-      for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          *reinterpret_cast<f32x4*>(to + 32 * f + 8 * y + 4 * hf) =
-              f32x4{o[f][4 * y], o[f][4 * y + 1], o[f][4 * y + 2], o[f][4 * y + 3]};
-      if (hf == 0) {
-        to[D] = m;
-        to[D + 1] = l;
       }
     }
+    if (odd) add_nonfinite<Mode, bf16_t, D, kThreads>(a, t, kvh, pb, pe, direct ? nullptr : part);
   }
 }
 

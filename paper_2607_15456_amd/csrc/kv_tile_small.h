@@ -15,34 +15,10 @@
 
 namespace lla {
 
-// Values that are not finite, which the matrix product of a step with rows that attend
-// only some of its tokens has left out: added to the rows that attend them (a product
-// with a weight of zero would give NaN to the others).  v: the step's first token of
-// feature row 0.
-template <typename T, int NT, int FT, typename Seen>
-__device__ __forceinline__ void add_nonfinite(const T* v, int count, int g, const Seen& seen, f32x4 (&o)[NT][FT]) {
-#pragma unroll 1
-  for (int k = 0; k < count; ++k) {
-    bool in[NT];
-#pragma unroll
-    for (int x = 0; x < NT; ++x) in[x] = seen(x, k);
-#pragma unroll
-    for (int f = 0; f < FT; ++f)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float y = Elem<T>::get(v, (size_t)(16 * f + 4 * g + i) * kPage + k);
-        if ((__float_as_uint(y) & 0x7f800000u) != 0x7f800000u) continue;
-#pragma unroll
-        for (int x = 0; x < NT; ++x)
-          if (in[x]) o[x][f][i] += y;
-      }
-  }
-}
-
 // Packed: entries of few rows.  Otherwise the few queries of a run over their shared
 // prompt, and every entry's own tokens, in one launch.
 template <template <int, int> class StepOf, int D, int NT, bool Packed>
-__global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void small_tile_kernel(KvTileArgs a) {
+__global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) void small_tile_kernel(KvTileArgs args) {
   typedef StepOf<D, NT> Step;
   typedef std::conditional_t<Step::kBytes == 2, bf16_t, float> T;
   constexpr int kStepBytes = Step::kTok * D * Step::kBytes;
@@ -57,72 +33,89 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 16, g = lane / 16;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   char* const lds = s_raw + w * kStepBytes;
-  const int group = a.H / a.p.Hkv, blocks = (group + kCols - 1) / kCols;
-
+  constexpr TileMode Mode = Packed ? kPacked : kOwn;  // (rows of both kinds of shared tiles are entries)
   // An entry's own tokens come first: how many tiles over prompts there are takes a count.
-  const int64_t own_items = Packed ? 0 : (int64_t)a.B * blocks * a.p.Hkv * a.own_slices;
   int tiles = -1, slices = 1;
   for (int64_t i = blockIdx.x;; i += gridDim.x) {
-    const bool own = !Packed && i < own_items;
-    if (!own && tiles < 0) {
-      if constexpr (Packed) count_packed<kThreads>(a, kCols, 0, a.small_rows, s_first, s_wave);
-      else count_shared<kThreads>(a, s_runs, s_first, nullptr, s_wave);
-      tiles = tiles_of(a.small, s_first[a.B]);
-      slices = tile_slices(a.small, (int64_t)tiles * a.p.Hkv);
-    }
-    const int64_t item = own ? i : i - own_items;
-    if (!own && item >= (int64_t)tiles * a.p.Hkv * slices) break;
-    const int kvh = (int)(item % a.p.Hkv), unit = (int)(item / a.p.Hkv), of = own ? a.B * blocks : tiles;
-    const int slice = unit / of, tile = of - 1 - (unit - slice * of);
-    float* const part = own ? a.own_part : a.small.part;
     Tile t;
-    if (own) {
-      t.at<kOwn>(a, tile / blocks, kCols, tile % blocks);
-    } else {
-      const int b = last_at_most(s_first, a.B, tile);
-      if constexpr (Packed) t.at<kPacked>(a, b, kCols, tile - s_first[b]);
-      else t.at<kPrefix>(a, b, kCols, tile - s_first[b], run_entries(a, s_runs, b));
-    }
-    const int per = slice_pages(a.small.least, t.keys.pages, own ? a.own_slices : slices), pb = slice * per,
-              pe = min(t.keys.pages, pb + per);
-    const bool direct = Packed && per >= t.keys.pages;
-    constexpr TileMode Mode = Packed ? kPacked : kOwn;  // (rows of both kinds of shared tiles are entries)
-    RowKeys rk[NT];
-    int64_t q_at[NT], out_at[NT];
-    bool in[NT];
-#pragma unroll
-    for (int x = 0; x < NT; ++x) {
-      const int col = x * kTile + c;
-      in[x] = col < t.rows;
-      rk[x] = t.row_keys<Mode>(a, kvh, min(col, t.rows - 1), q_at[x], out_at[x]);
-    }
-    if (t.state != kFine || pb >= pe) {
-      if (Packed && slice == 0 && w == 0) {
-        const float none = t.state == kNone ? __builtin_nanf("") : 0.f;
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-          if (!in[x]) continue;
-#pragma unroll
-          for (int f = 0; f < FT; ++f) store_row4(a, out_at[x], 16 * f + 4 * g, f32x4{none, none, none, none});
-          if (a.lse && g == 0) a.lse[out_at[x]] = t.state == kNone ? none : neg_inf();
-        }
+    bool own;
+    int kvh, pb, pe;
+    {
+      const KvTileArgs& a = args_again();
+      const int group = a.H / a.p.Hkv, blocks = (group + kCols - 1) / kCols;
+      const int64_t own_items = Packed ? 0 : (int64_t)a.B * blocks * a.p.Hkv * a.own_slices;
+      own = !Packed && i < own_items;
+      if (!own && tiles < 0) {
+        if constexpr (Packed) count_packed<kThreads>(a, kCols, 0, a.small_rows, s_first, s_wave);
+        else count_shared<kThreads>(a, s_runs, s_first, nullptr, s_wave);
+        tiles = tiles_of(a.small, s_first[a.B]);
+        slices = tile_slices(a.small, (int64_t)tiles * a.p.Hkv);
       }
-      continue;
+      const int64_t item = own ? i : i - own_items;
+      if (!own && item >= (int64_t)tiles * a.p.Hkv * slices) break;
+      kvh = (int)(item % a.p.Hkv);
+      const int unit = (int)(item / a.p.Hkv), of = own ? a.B * blocks : tiles;
+      const int slice = unit / of, tile = of - 1 - (unit - slice * of);
+      if (own) {
+        t.at<kOwn>(a, tile / blocks, kCols, tile % blocks);
+      } else {
+        const int b = last_at_most(s_first, a.B, tile);
+        if constexpr (Packed) t.at<kPacked>(a, b, kCols, tile - s_first[b]);
+        else t.at<kPrefix>(a, b, kCols, tile - s_first[b], run_entries(a, s_runs, b));
+      }
+      const int per = slice_pages(a.small.least, t.keys.pages, own ? a.own_slices : slices);
+      pb = slice * per;
+      pe = min(t.keys.pages, pb + per);
+      if (t.state != kFine || pb >= pe) {
+        if (Packed && slice == 0 && w == 0) {
+          const float none = t.state == kNone ? __builtin_nanf("") : 0.f;
+#pragma unroll
+          for (int x = 0; x < NT; ++x) {
+            if (x * kTile + c >= t.rows) continue;
+            int64_t q_at, out_at;
+            t.row_keys<Mode>(a, kvh, x * kTile + c, q_at, out_at);
+            for (int f = 0; f < FT; ++f) store_row4(a, out_at, 16 * f + 4 * g, f32x4{none, none, none, none});
+            if (a.lse && g == 0) a.lse[out_at] = t.state == kNone ? none : neg_inf();
+          }
+        }
+        continue;
+      }
     }
 
     Step st;
-    constexpr int kHeadBytes = kPage * D * Step::kBytes;
-    const int32_t* table = a.p.table + (int64_t)t.row * a.p.max_pages;
-    // step s of the tile's: where its page's keys and values are (-1: nowhere)
+    RowKeys rk[NT];
+    const char *k_pool, *v_pool;
+    const int32_t* table;
+    int n_pages;
+    int64_t page_bytes;
+    float qscale;
+    const void* q;
+    int64_t q_at[NT];
+    {
+      const KvTileArgs& a = args_again();
+      int64_t unused;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) rk[x] = t.row_keys<Mode>(a, kvh, min(x * kTile + c, t.rows - 1), q_at[x], unused);
+      constexpr int kHeadBytes = kPage * D * Step::kBytes;
+      k_pool = static_cast<const char*>(a.p.k) + (int64_t)kvh * kHeadBytes;
+      v_pool = static_cast<const char*>(a.p.v) + (int64_t)kvh * kHeadBytes;
+      table = a.p.table + (int64_t)t.row * a.p.max_pages;
+      n_pages = a.p.n_pages;
+      page_bytes = (int64_t)a.p.Hkv * kHeadBytes;
+      qscale = a.qscale;
+      q = a.q;
+    }
+    // step s of the tile's: where its page is in the pools (-1: nowhere)
     auto block = [&](int s) -> int64_t {
       const int page = uniform(table, t.keys.page(s / kSteps));
-      return page < 0 || page >= a.p.n_pages ? -1 : ((int64_t)page * a.p.Hkv + kvh) * kHeadBytes;
+      return (unsigned)page >= (unsigned)n_pages ? -1 : page * page_bytes;
     };
-    auto keys = [&](int64_t at) { return make_rsrc(static_cast<const char*>(a.p.k) + max(at, (int64_t)0), kHeadBytes); };
-    auto vals = [&](int64_t at) { return make_rsrc(static_cast<const char*>(a.p.v) + max(at, (int64_t)0), kHeadBytes); };
+    auto keys = [&](int64_t at) { return make_rsrc(k_pool + max(at, (int64_t)0), kPage * D * Step::kBytes); };
+    auto vals = [&](int64_t at) { return make_rsrc(v_pool + max(at, (int64_t)0), kPage * D * Step::kBytes); };
 
     int s = pb * kSteps + w;
     const int end = pe * kSteps;
+    bool odd = false;  // values that are not finite among tokens that only some rows attend
     int64_t now = -1;
     float m[NT], l[NT];
     f32x4 o[NT][FT];
@@ -140,7 +133,9 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
       st.load_v(vals(now), tok, lane);
     }
 #pragma unroll
-    for (int x = 0; x < NT; ++x) st.load_q(x, static_cast<const T*>(a.q) + q_at[x], g, in[x]);
+    for (int x = 0; x < NT; ++x) st.load_q(x, static_cast<const T*>(q) + q_at[x], g, x * kTile + c < t.rows);
+    // A step's keys are requested as soon as the keys before have left their registers for
+    // LDS, its values likewise.
     for (; s < end; s += W) {
       const bool more = s + W < end;
       const int tok = (s + W) % kSteps * Step::kTok;
@@ -172,7 +167,7 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
 #pragma unroll
           for (int i = 0; i < 4; ++i) pm = fmaxf(pm, sc[x][y][i]);
         pm = fmaxf(pm, xor_shfl(pm, 16));
-        pm = fmaxf(pm, xor_shfl(pm, 32)) * a.qscale;
+        pm = fmaxf(pm, xor_shfl(pm, 32)) * qscale;
         if (__any(pm > m[x] + kLazy)) {
           const float to = fmaxf(m[x], pm);
           const float alpha = m[x] == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(m[x] - to);
@@ -186,35 +181,33 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
         for (int y = 0; y < kTiles; ++y)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            sc[x][y][i] = __builtin_amdgcn_exp2f(below(sc[x][y][i], a.qscale, base));
+            sc[x][y][i] = __builtin_amdgcn_exp2f(below(sc[x][y][i], qscale, base));
             l[x] += sc[x][y][i];
           }
       }
-      bool odd = false;  // values that are not finite among tokens that only some rows attend
+      // Values of tokens that not all rows attend: weights of zero keep them out of the rows
+      // that do not, if they are finite.  Shared tiles' rows all attend the same.
       if (!whole) {
         const RowKeys most{t.keys.p_max, t.keys.low_min};
-        st.mask_values([&](int k) { return good && most.seen(t0 + k, t.keys.sink); }, lane);
-        if (Packed) odd = __any(st.drop_nonfinite());
+        auto attended = [&](int k) { return good && most.seen(t0 + k, t.keys.sink); };
+        if constexpr (Packed) odd |= st.finite_values(attended, lane);
+        else st.mask_values(attended, lane);
       }
       st.stage_v(lds, lane);
       if (more) st.load_v(vals(next), tok, lane);
       wave_lds_order();
       st.values(lds, c, g, sc, o);
       wave_lds_order();
-      if (Packed && odd)
-        add_nonfinite<T, NT, FT>(reinterpret_cast<const T*>(static_cast<const char*>(a.p.v) + now) + t0 % kPage, Step::kTok,
-                                 g, [&](int x, int k) { return rk[x].seen(t0 + k, t.keys.sink); }, o);
       now = next;
     }
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
       l[x] += xor_shfl(l[x], 16);
       l[x] += xor_shfl(l[x], 32);
-      if (in[x] && t.past_bound<Mode>(a, x * kTile + c)) l[x] = __builtin_nanf("");
     }
 
     // join the wavefronts, the upper half into the lower
-    __syncthreads();
+    const bool any_odd = __syncthreads_or(odd);
     for (int half = W / 2; half >= 1; half /= 2) {
       if (w >= half && w < 2 * half) {
 #pragma unroll
@@ -239,16 +232,24 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
       }
       __syncthreads();
     }
+    const KvTileArgs& a = args_again();
+    const bool whole = Packed && pb == 0 && pe == t.keys.pages;
+    const int64_t first_own = Packed ? 0 : (int64_t)a.B * ((a.H / a.p.Hkv + kCols - 1) / kCols) * a.p.Hkv * a.own_slices;
+    float* const part = partial_row(own ? a.own_part : a.small.part, own ? i : i - first_own, kCols, 0, D);
     if (w == 0) {
 #pragma unroll
       for (int x = 0; x < NT; ++x) {
-        if (!in[x]) continue;
-        if (direct) {
+        const int col = x * kTile + c;
+        if (col >= t.rows) continue;
+        if (t.past_bound<Mode>(a, col)) l[x] = __builtin_nanf("");
+        if (whole) {
+          int64_t q_unused, out_at;
+          t.row_keys<Mode>(a, kvh, col, q_unused, out_at);
 #pragma unroll
-          for (int f = 0; f < FT; ++f) store_row4(a, out_at[x], 16 * f + 4 * g, o[x][f] / l[x]);
-          if (a.lse && g == 0) a.lse[out_at[x]] = ((m[x] == neg_inf() ? 0.f : m[x]) + __builtin_amdgcn_logf(l[x])) * kLn2;
+          for (int f = 0; f < FT; ++f) store_row4(a, out_at, 16 * f + 4 * g, o[x][f] / l[x]);
+          if (a.lse && g == 0) a.lse[out_at] = ((m[x] == neg_inf() ? 0.f : m[x]) + __builtin_amdgcn_logf(l[x])) * kLn2;
         } else {
-          float* to = partial_row(part, item, kCols, x * kTile + c, D);
+          float* to = part + col * (D + 4);
 #pragma unroll
           for (int f = 0; f < FT; ++f) *reinterpret_cast<f32x4*>(to + 16 * f + 4 * g) = o[x][f];
           if (g == 0) {
@@ -257,6 +258,9 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
           }
         }
       }
+    }
+    if constexpr (Packed) {
+      if (any_odd) add_nonfinite<kPacked, T, D, kThreads>(a, t, kvh, pb, pe, whole ? nullptr : part);
     }
   }
 }
@@ -271,16 +275,23 @@ hipError_t launch_small(const KvTileArgs& a, unsigned grid, hipStream_t stream) 
 
 template <int NT, bool Packed, template <int, int> class StepOf>
 hipError_t launch_small_width(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
+  constexpr bool kNarrow = Packed && NT == 1;  // (wide heads of packed tokens take two tiles)
   switch (a.p.d) {
     case 32: return launch_small<StepOf, 32, NT, Packed>(a, grid, stream);
     case 64: return launch_small<StepOf, 64, NT, Packed>(a, grid, stream);
     case 96: return launch_small<StepOf, 96, NT, Packed>(a, grid, stream);
-    case 128: return launch_small<StepOf, 128, NT, Packed>(a, grid, stream);
-    case 160: return launch_small<StepOf, 160, NT, Packed>(a, grid, stream);
-    case 192: return launch_small<StepOf, 192, NT, Packed>(a, grid, stream);
-    case 224: return launch_small<StepOf, 224, NT, Packed>(a, grid, stream);
-    default: return launch_small<StepOf, 256, NT, Packed>(a, grid, stream);
+    default: break;
   }
+  if constexpr (!kNarrow) {
+    switch (a.p.d) {
+      case 128: return launch_small<StepOf, 128, NT, Packed>(a, grid, stream);
+      case 160: return launch_small<StepOf, 160, NT, Packed>(a, grid, stream);
+      case 192: return launch_small<StepOf, 192, NT, Packed>(a, grid, stream);
+      case 224: return launch_small<StepOf, 224, NT, Packed>(a, grid, stream);
+      default: return launch_small<StepOf, 256, NT, Packed>(a, grid, stream);
+    }
+  }
+  return hipErrorInvalidValue;
 }
 template <int NT, bool Packed>
 hipError_t launch_small_type(const KvTileArgs& a, unsigned grid, hipStream_t stream) {

@@ -11,6 +11,16 @@ A decode step of a batch, every call enqueued and none waiting for the host::
     kv.write(k, v, k_pages[l], v_pages[l], pages.table, start, rows=rows, freq=freq)
     o = kv.decode_attn(q[:, 0], k_pages[l], v_pages[l], pages.table, pages.length, rows=rows, n_ctx=n)
 
+A step whose entries bring any number of tokens each, packed one after another, and a
+decode step of sequences that share a long prompt::
+
+    at = kv.slots(pages, start, n_new, total, rows=rows)
+    kv.write_slots(k, v, k_pages[l], v_pages[l], at.slot, pos=at.pos, freq=freq)
+    o = kv.prefill_attn(q, k_pages[l], v_pages[l], pages.table, at.offset, start, rows=rows, n_ctx=n)
+
+    lead, shared = kv.shared_prefix(pages, rows)
+    o = kv.decode_attn_shared(q, k_pages[l], v_pages[l], pages.table, pages.length, lead, shared, rows=rows, n_ctx=n)
+
 rope is differentiable; no gradient passes through the cache.
 
 Rows of -1 are padding in every call: a step captured for a fixed number of rows
