@@ -368,7 +368,7 @@ lla_status lla_kv_prefill_workspace_bytes(int dtype, int out_dtype, int B, int t
  * and are then summed as rounded (a weight is off by at most 2^-8 of itself, their sum
  * not at all).
  * Requires 1 <= B <= LLA_KV_MAX_ROWS, 1 <= total < 2^24, H a multiple of H_kv >= 1,
- * total*H < 2^31, sink >= 0, window >= 0, sink = 0 without a window.
+ * total*H < 2^30, sink >= 0, window >= 0, sink = 0 without a window.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
  */
 lla_status lla_kv_prefill_attn(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head, int n_seqs,

@@ -17,6 +17,7 @@ constexpr int kMaxPages = 1 << 20;   // pages of one sequence
 constexpr int kMaxPool = 1 << 30;    // pages of a pool
 constexpr int kMaxGridY = 65535;     // workgroups along a grid's second and third dimension
 constexpr int kMaxGridX = (1 << 24) - 1;  // and its first: below 2^32 threads, 256 a workgroup
+constexpr int kMaxPackedRows = 1 << 30;   // tokens times heads: tiles and what they are cut into are counted in 32 bits
 constexpr double kLog2e = 1.4426950408889634;
 
 bool ptr_ok(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -80,7 +81,10 @@ bool workspace_ok(const void* p, size_t bytes, size_t need) {
 }
 bool packed_ok(int dtype, int B, int total, int H, int H_kv, int d_head, int n_ctx, int sink, int window) {
   return decode_ok(dtype, 1, H, H_kv, d_head, n_ctx, sink, window) && B >= 1 && B <= LLA_KV_MAX_ROWS && total >= 1 &&
-         total <= kMaxGridX && total <= std::numeric_limits<int>::max() / H;
+         total <= kMaxGridX && total < kMaxPackedRows / H;
+}
+bool shared_ok(int dtype, int B, int H, int H_kv, int d_head, int n_ctx) {
+  return B <= LLA_KV_MAX_ROWS && decode_ok(dtype, B, H, H_kv, d_head, n_ctx, 0, 0);
 }
 lla::KvTileArgs tile_args(int dtype, int out_dtype, int B, int total, int H, int H_kv, int d_head, int n_ctx, int sink,
                           int window) {
@@ -446,7 +450,7 @@ lla_status lla_pages_shared(int B, int least, const int32_t* rows, int n_seqs, i
 }
 
 lla_status lla_kv_shared_workspace_bytes(int dtype, int B, int H, int H_kv, int d_head, int n_ctx, size_t* bytes) {
-  if (!packed_ok(dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0) || !bytes) return LLA_ERR_INVALID_ARG;
+  if (!shared_ok(dtype, B, H, H_kv, d_head, n_ctx) || !bytes) return LLA_ERR_INVALID_ARG;
   *bytes = lla::kv_shared_workspace(tile_args(dtype, dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0));
   return LLA_OK;
 }
@@ -457,7 +461,7 @@ lla_status lla_kv_decode_attn_shared(int dtype, int out_dtype, int B, int H, int
                                      const int32_t* shared, const void* q, const void* k_pages,
                                      const void* v_pages, float scale, void* out, float* lse,
                                      void* workspace, size_t ws_bytes, void* stream) {
-  if (!packed_ok(dtype, B, B, H, H_kv, d_head, n_ctx, 0, 0) || !dtype_ok(out_dtype) ||
+  if (!shared_ok(dtype, B, H, H_kv, d_head, n_ctx) || !dtype_ok(out_dtype) ||
       !tables_ok(n_seqs, max_pages, n_pages) || n_ctx > (int64_t)max_pages * LLA_PAGE_TOKENS || !scale_ok(scale))
     return LLA_ERR_INVALID_ARG;
   if (!idx_ok(table) || !idx_ok(length) || !opt_idx_ok(rows) || !idx_ok(lead) || !idx_ok(shared) || !ptr_ok(q) ||

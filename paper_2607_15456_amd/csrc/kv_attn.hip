@@ -46,7 +46,7 @@ struct Slices {
   __device__ __forceinline__ Slices(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices, const KvTileCut& cut,
                                     int cols, int kvh, int x) {
     const int per = slice_pages(cut.least, t.keys.pages, slices), row = a.p.d + 4;
-    at = cut.part + (item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
+    at = cut.part + ((int64_t)item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
     stride = (int64_t)tiles * a.p.Hkv * cols * row;
     count = (t.keys.pages + per - 1) / per;
   }
@@ -57,20 +57,20 @@ constexpr int kJoinRows = 32;  // of a tile, that a workgroup joins at a time
 // Packed tokens: the tiles that were cut, a workgroup 32 rows of one.
 __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int large_cols) {
   __shared__ int s_small[kMostEntries + 1], s_large[kMostEntries + 1];
-  __shared__ int64_t s_wave[kThreads / kWave];
+  __shared__ int s_wave[kThreads / kWave];
   count_packed<kThreads>(a, a.small_cols, 0, a.small_rows, s_small, s_wave);
   count_packed<kThreads>(a, large_cols, a.small_rows, kAllRows, s_large, s_wave);
-  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, (int64_t)small * a.p.Hkv);
-  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, (int64_t)large * a.p.Hkv);
+  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, small * a.p.Hkv);
+  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, large * a.p.Hkv);
   const int chunks = large_cols / kJoinRows;
-  const int64_t of_small = small_slices > 1 ? (int64_t)small * a.p.Hkv : 0;
-  const int64_t of_large = large_slices > 1 ? (int64_t)large * a.p.Hkv * chunks : 0;
+  const int of_small = small_slices > 1 ? small * a.p.Hkv : 0;
+  const int of_large = large_slices > 1 ? large * a.p.Hkv * chunks : 0;
   const int lanes = a.p.d / 4, r = threadIdx.x / lanes, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
   if (r >= step) return;
-  for (int64_t i = blockIdx.x; i < of_small + of_large; i += gridDim.x) {
+  for (int i = blockIdx.x; i < of_small + of_large; i += gridDim.x) {
     const bool is_small = i < of_small;
-    const int64_t j = is_small ? i : i - of_small, unit = is_small ? j : j / chunks;
-    const int chunk = (int)(j - (is_small ? j : unit * chunks)), kvh = (int)(unit % a.p.Hkv), tile = (int)(unit / a.p.Hkv);
+    const int j = is_small ? i : i - of_small, unit = is_small ? j : j / chunks, chunk = is_small ? 0 : j - unit * chunks;
+    const int tile = unit / a.p.Hkv, kvh = unit - tile * a.p.Hkv;
     const int* first = is_small ? s_small : s_large;
     const int b = last_at_most(first, a.B, tile), cols = is_small ? a.small_cols : large_cols;
     Tile t;
@@ -93,16 +93,16 @@ __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int
 // Shared prompts: every (entry, query head), of its prompt's slices and its own.
 __global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
   __shared__ int s_runs[kMostEntries + 1], s_small[kMostEntries + 1], s_large[kMostEntries + 1];
-  __shared__ int64_t s_wave[kThreads / kWave];
+  __shared__ int s_wave[kThreads / kWave];
   count_shared<kThreads>(a, s_runs, s_small, s_large, s_wave);
-  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, (int64_t)small * a.p.Hkv);
-  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, (int64_t)large * a.p.Hkv);
+  const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, small * a.p.Hkv);
+  const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, large * a.p.Hkv);
   const int group = a.H / a.p.Hkv, cols = a.small_cols, blocks = (group + cols - 1) / cols;
   const int lanes = a.p.d / 4, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
-  const int64_t rows = (int64_t)a.B * a.H;
+  const int rows = a.B * a.H;  // (below 2^31, as every number of tiles and their slices)
   if ((int)threadIdx.x / lanes >= step) return;
-  for (int64_t i = (int64_t)blockIdx.x * step + threadIdx.x / lanes; i < rows; i += (int64_t)gridDim.x * step) {
-    const int b = (int)(i / a.H), h = (int)(i - (int64_t)b * a.H), kvh = h / group, r = h - kvh * group;
+  for (int64_t at = (int64_t)blockIdx.x * step + threadIdx.x / lanes; at < rows; at += (int64_t)gridDim.x * step) {
+    const int i = (int)at, b = i / a.H, h = i - b * a.H, kvh = h / group, r = h - kvh * group;
     const int shared = a.shared[b];
     Tile own;
     own.at<kOwn>(a, b, cols, r / cols);
@@ -201,8 +201,8 @@ size_t kv_prefill_workspace(const KvTileArgs& a) {
 hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
   KvTileArgs a = args;
   const PackedShape s(a);
-  a.small.tiles = s.small_tiles;
-  a.large.tiles = s.large_tiles;
+  a.small.tiles = (int)s.small_tiles;
+  a.large.tiles = (int)s.large_tiles;
   a.large.part = a.small.part + s.small_partial * a.small_cols * (a.p.d + 4);
   hipError_t e = hipSuccess;
   // (a workgroup takes another tile where there are more)
@@ -265,8 +265,8 @@ size_t kv_shared_workspace(const KvTileArgs& a) {
 hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
   KvTileArgs a = args;
   const SharedShape s(a);
-  a.small.tiles = s.small_tiles;
-  a.large.tiles = s.large_tiles;
+  a.small.tiles = (int)s.small_tiles;
+  a.large.tiles = (int)s.large_tiles;
   a.own_part = a.small.part + s.small * a.small_cols * (a.p.d + 4);
   a.large.part = a.own_part + s.own * a.small_cols * (a.p.d + 4);
   auto grid = [](int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 16); };

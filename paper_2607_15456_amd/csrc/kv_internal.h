@@ -72,8 +72,7 @@ size_t kv_decode_workspace(const KvDecodeArgs& a);
 // at least, the workgroups that they are shared out to, the tiles that there is room for
 // (more are of offsets that decrease, and left out), and their partial rows.
 struct KvTileCut {
-  int most, least, wgs;
-  int64_t tiles;
+  int most, least, wgs, tiles;
   float* part;
 };
 

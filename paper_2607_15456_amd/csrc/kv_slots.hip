@@ -21,23 +21,22 @@ constexpr int kThreads = 256;
 __global__ __launch_bounds__(kThreads) void slots_kernel(KvSlotsArgs a) {
   constexpr int kEach = kMostEntries / kThreads;
   __shared__ int s_off[kMostEntries + 1];
-  __shared__ int64_t s_wave[kThreads / kWave];
+  __shared__ int s_wave[kThreads / kWave];
   const int tid = threadIdx.x;
-  int n[kEach];
-  int64_t sum = 0;
+  int n[kEach], sum = 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int b = tid * kEach + i;
-    n[i] = b < a.B ? max(0, a.n_new[b]) : 0;
+    n[i] = b < a.B ? max(0, min(a.n_new[b], a.total)) : 0;  // (a length past the room ends there)
     sum += n[i];
   }
-  int64_t at = prefix_sum<kThreads>(sum, s_wave);
+  int at = prefix_sum<kThreads>(sum, s_wave);
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int b = tid * kEach + i;
-    if (b < a.B) s_off[b] = (int)min(at, (int64_t)a.total);
-    at += n[i];
-    if (b == a.B - 1) s_off[a.B] = (int)min(at, (int64_t)a.total);
+    if (b < a.B) s_off[b] = min(at, a.total);
+    at = add_up(at, n[i]);
+    if (b == a.B - 1) s_off[a.B] = min(at, a.total);
   }
   __syncthreads();
   if (blockIdx.x == 0)

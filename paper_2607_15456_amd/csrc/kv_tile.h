@@ -53,23 +53,28 @@ struct RowKeys {
 // is out of its range.
 enum TileState { kFine, kZeros, kNone };
 
-// Sum over the workgroup of v's of lower threads.
-template <int kThreads, typename V>
-__device__ __forceinline__ V prefix_sum(V v, V* s_wave) {
+// Sums stop here: counts of sound arguments stay below, others' do no harm.
+constexpr int kMostSum = 1 << 30;
+__device__ __forceinline__ int add_up(int x, int y) { return min(x + y, kMostSum); }
+
+// Sum over the workgroup of v's of lower threads (0 <= v <= kMostSum).
+template <int kThreads>
+__device__ __forceinline__ int prefix_sum(int v, int* s_wave) {
   const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-  V x = v;
+  int x = v;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
-    const V y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
+    const int y = __shfl_up(x, o, kWave);
+    if (lane >= o) x = add_up(x, y);
   }
+  const int lower = __shfl_up(x, 1, kWave);
   __syncthreads();
   if (lane == kWave - 1) s_wave[w] = x;
   __syncthreads();
-  V before = 0;
+  int before = 0;
 #pragma unroll
-  for (int i = 0; i < kThreads / kWave; ++i) before += i < w ? s_wave[i] : 0;
-  return before + x - v;
+  for (int i = 0; i < kThreads / kWave; ++i) before = add_up(before, i < w ? s_wave[i] : 0);
+  return add_up(before, lane ? lower : 0);
 }
 
 // The largest b in [0, n) with s_at[b] <= x (s_at[0] <= x).
@@ -92,18 +97,17 @@ struct EntryCounts {
   static constexpr int kEach = (kMostEntries + kThreads - 1) / kThreads;
   int n[kEach];
   __device__ __forceinline__ static int entry(int i) { return threadIdx.x * kEach + i; }
-  // (sums past 32 bits, of offsets that decrease, stop there)
-  __device__ __forceinline__ void sum(int B, int* s_first, int64_t* s_wave) const {
-    int64_t total = 0;
+  __device__ __forceinline__ void sum(int B, int* s_first, int* s_wave) const {
+    int total = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) total += n[i];
-    int64_t at = prefix_sum<kThreads>(total, s_wave);
+    for (int i = 0; i < kEach; ++i) total = add_up(total, n[i]);
+    int at = prefix_sum<kThreads>(total, s_wave);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int b = entry(i);
-      if (b < B) s_first[b] = (int)min(at, (int64_t)kAllRows);
-      at += n[i];
-      if (b == B - 1) s_first[B] = (int)min(at, (int64_t)kAllRows);
+      if (b < B) s_first[b] = at;
+      at = add_up(at, n[i]);
+      if (b == B - 1) s_first[B] = at;
     }
     __syncthreads();
   }
@@ -111,7 +115,7 @@ struct EntryCounts {
 
 // Packed entries with more than `over` and at most `upto` rows.
 template <int kThreads>
-__device__ __forceinline__ void count_packed(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int64_t* s_wave) {
+__device__ __forceinline__ void count_packed(const KvTileArgs& a, int cols, int over, int upto, int* s_first, int* s_wave) {
   const int group = a.H / a.p.Hkv;
   EntryCounts<kThreads> c;
 #pragma unroll
@@ -188,7 +192,7 @@ __host__ __device__ __forceinline__ int tile_entries(int group, int cols) { retu
 // ones, and the others, where an array for them is given.
 template <int kThreads>
 __device__ __forceinline__ void count_shared(const KvTileArgs& a, int* s_runs, int* s_small, int* s_large,
-                                             int64_t* s_wave) {
+                                             int* s_wave) {
   const int group = a.H / a.p.Hkv, each = tile_entries(group, a.prefix_cols);
   EntryCounts<kThreads> c, small, large;
   bool begins[c.kEach];
@@ -226,12 +230,12 @@ __device__ __forceinline__ int run_entries(const KvTileArgs& a, const int* s_run
 }
 
 // The tiles that are worked on, of those that were counted.
-__device__ __forceinline__ int tiles_of(const KvTileCut& cut, int counted) { return (int)min((int64_t)counted, cut.tiles); }
+__device__ __forceinline__ int tiles_of(const KvTileCut& cut, int counted) { return min(counted, cut.tiles); }
 // Slices that every tile may be cut into, where there are fewer tiles than workgroups:
 // as many as give each a workgroup, or so many that two rounds of workgroups do better.
-__device__ __forceinline__ int tile_slices(const KvTileCut& cut, int64_t units) {
-  if (units == 0 || cut.most == 1) return 1;
-  const int one = (int)max((int64_t)1, cut.wgs / units), two = (int)(2 * cut.wgs / units);
+__device__ __forceinline__ int tile_slices(const KvTileCut& cut, int units) {
+  if (units <= 0 || cut.most == 1 || units >= 2 * cut.wgs) return 1;
+  const int one = max(1, cut.wgs / units), two = 2 * cut.wgs / units;
   return min(cut.most, 9 * two > 20 * one ? two : one);
 }
 __device__ __forceinline__ int slice_pages(int least, int pages, int slices) {
@@ -330,8 +334,8 @@ __device__ __forceinline__ float* partial_row(float* part, int64_t item, int col
 // Number of (slice, tile, key head) among the call's work: heavy tiles of a prompt, its
 // last, first, and one key head's work a multiple of the key heads apart, so on one XCD
 // where 8 divides them.
-__device__ __forceinline__ int64_t item_of(const KvTileArgs& a, int tiles, int slice, int tile, int kvh) {
-  return ((int64_t)slice * tiles + (tiles - 1 - tile)) * a.p.Hkv + kvh;
+__device__ __forceinline__ int item_of(const KvTileArgs& a, int tiles, int slice, int tile, int kvh) {
+  return (slice * tiles + (tiles - 1 - tile)) * a.p.Hkv + kvh;
 }
 
 // Four features from f on of result row i.

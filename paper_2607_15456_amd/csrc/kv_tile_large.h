@@ -190,7 +190,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   constexpr int kCols = L::kCols, kThreads = L::kThreads, KT = L::KT, FT = L::FT, kTok = L::kTok;
   constexpr int kHeadBytes = kPage * D * 2;
   __shared__ int s_first[kMostEntries + 1], s_runs[kMostEntries + 1];
-  __shared__ int64_t s_wave[kThreads / kWave];
+  __shared__ int s_wave[kThreads / kWave];
   __shared__ int s_odd;  // whether values of tokens that only some rows attend were not finite
   extern __shared__ __align__(16) char s_raw[];
   const int tid = threadIdx.x, lane = tid % kWave, c = lane % 32, hf = lane / 32;
@@ -207,15 +207,15 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   } else {
     count_shared<kThreads>(args, s_runs, nullptr, s_first, s_wave);
   }
-  for (int64_t item = blockIdx.x;; item += gridDim.x) {
+  for (int item = blockIdx.x;; item += gridDim.x) {
     Tile t;
     int kvh, pb, pe;
     {
       const KvTileArgs& a = args_again();
-      const int tiles = tiles_of(a.large, s_first[a.B]), slices = tile_slices(a.large, (int64_t)tiles * a.p.Hkv);
-      if (item >= (int64_t)tiles * a.p.Hkv * slices) break;
-      const int unit = (int)(item / a.p.Hkv), slice = unit / tiles, tile = tiles - 1 - (unit - slice * tiles);
-      kvh = (int)(item % a.p.Hkv);
+      const int tiles = tiles_of(a.large, s_first[a.B]), slices = tile_slices(a.large, tiles * a.p.Hkv);
+      if (item >= tiles * a.p.Hkv * slices) break;
+      const int unit = item / a.p.Hkv, slice = unit / tiles, tile = tiles - 1 - (unit - slice * tiles);
+      kvh = item - unit * a.p.Hkv;
       int b = last_at_most(s_first, a.B, tile), nth = tile - s_first[b];
       if constexpr (Mode == kPacked) {
         if (slices == 1 && a.B > 1) HeavyFirst{s_first, s_runs, a.B}.find(unit, last_from, b, nth);

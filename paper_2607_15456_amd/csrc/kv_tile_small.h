@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   constexpr int FT = D / 16, kSteps = kPage / Step::kTok, kTiles = Step::kTiles;
   constexpr int kRow = D + 4, kCols = NT * kTile, kThreads = kWaves * kWave, W = kWaves;
   __shared__ int s_first[kMostEntries + 1], s_runs[Packed ? 1 : kMostEntries + 1];
-  __shared__ int64_t s_wave[kThreads / kWave];
+  __shared__ int s_wave[kThreads / kWave];
   // the wavefronts' steps, then what they join
   extern __shared__ __align__(16) char s_raw[];
   float* const s_o = reinterpret_cast<float*>(s_raw);
@@ -36,25 +36,25 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
   constexpr TileMode Mode = Packed ? kPacked : kOwn;  // (rows of both kinds of shared tiles are entries)
   // An entry's own tokens come first: how many tiles over prompts there are takes a count.
   int tiles = -1, slices = 1;
-  for (int64_t i = blockIdx.x;; i += gridDim.x) {
+  for (int i = blockIdx.x;; i += gridDim.x) {
     Tile t;
     bool own;
     int kvh, pb, pe;
     {
       const KvTileArgs& a = args_again();
       const int group = a.H / a.p.Hkv, blocks = (group + kCols - 1) / kCols;
-      const int64_t own_items = Packed ? 0 : (int64_t)a.B * blocks * a.p.Hkv * a.own_slices;
+      const int own_items = Packed ? 0 : a.B * blocks * a.p.Hkv * a.own_slices;
       own = !Packed && i < own_items;
       if (!own && tiles < 0) {
         if constexpr (Packed) count_packed<kThreads>(a, kCols, 0, a.small_rows, s_first, s_wave);
         else count_shared<kThreads>(a, s_runs, s_first, nullptr, s_wave);
         tiles = tiles_of(a.small, s_first[a.B]);
-        slices = tile_slices(a.small, (int64_t)tiles * a.p.Hkv);
+        slices = tile_slices(a.small, tiles * a.p.Hkv);
       }
-      const int64_t item = own ? i : i - own_items;
-      if (!own && item >= (int64_t)tiles * a.p.Hkv * slices) break;
-      kvh = (int)(item % a.p.Hkv);
-      const int unit = (int)(item / a.p.Hkv), of = own ? a.B * blocks : tiles;
+      const int item = own ? i : i - own_items;
+      if (!own && item >= tiles * a.p.Hkv * slices) break;
+      const int unit = item / a.p.Hkv, of = own ? a.B * blocks : tiles;
+      kvh = item - unit * a.p.Hkv;
       const int slice = unit / of, tile = of - 1 - (unit - slice * of);
       if (own) {
         t.at<kOwn>(a, tile / blocks, kCols, tile % blocks);
@@ -234,8 +234,8 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
     }
     const KvTileArgs& a = args_again();
     const bool whole = Packed && pb == 0 && pe == t.keys.pages;
-    const int64_t first_own = Packed ? 0 : (int64_t)a.B * ((a.H / a.p.Hkv + kCols - 1) / kCols) * a.p.Hkv * a.own_slices;
-    float* const part = partial_row(own ? a.own_part : a.small.part, own ? i : i - first_own, kCols, 0, D);
+    const int own_items = Packed ? 0 : a.B * ((a.H / a.p.Hkv + kCols - 1) / kCols) * a.p.Hkv * a.own_slices;
+    float* const part = partial_row(own ? a.own_part : a.small.part, own ? i : i - own_items, kCols, 0, D);
     if (w == 0) {
 #pragma unroll
       for (int x = 0; x < NT; ++x) {

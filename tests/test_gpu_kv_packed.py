@@ -731,6 +731,38 @@ def test_captured_steps(dtype, shared):
         (xs.float() @ xs.float().transpose(1, 2)).sum().item()  # the program's own work
 
 
+def test_captured_calls_share_a_workspace():
+    """Two graphs with one workspace, replayed in turn with the program's own work between: nothing is kept in it."""
+    table, n_pages = pages_for([3000, 2500, 700], np.random.default_rng(4))
+    kp, vp = pool(1, n_pages, 2, 128, BF)
+    t, off, start = ints(table), ints([0, 129, 130, 160]), ints([2871, 2499, 670])
+    length, lead, shared = ints([3000, 2500, 700]), ints([0, 0, 0]), ints([640, 640, 640])
+    need = max(kv.prefill_workspace_bytes(BF, 3, 160, 8, 2, 128, 3008), kv.shared_workspace_bytes(BF, 3, 8, 2, 128, 3008))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    q, one = normal((160, 8, 128), 2, BF), normal((3, 8, 128), 3, BF)
+    calls = [lambda **kw: kv.prefill_attn(q, kp, vp, t, off, start, n_ctx=3008, **kw),
+             lambda **kw: kv.decode_attn_shared(one, kp, vp, t, length, lead, shared, n_ctx=3008, **kw)]
+    outs = [torch.empty((160, 8, 128), device=DEV), torch.empty((3, 8, 128), device=DEV)]
+    graphs, side = [], torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for call, out in zip(calls, outs):
+        with torch.cuda.stream(side):
+            call(out=out, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call(out=out, workspace=ws)
+        graphs.append(g)
+    for i in range(4):
+        q.copy_(normal((160, 8, 128), 20 + i, BF)), one.copy_(normal((3, 8, 128), 30 + i, BF))
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        want = [call() for call in calls]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), i
+        (kp[0].float() @ vp[0].float()).sum().item()
+
+
 def test_other_streams_and_two_at_once():
     """Calls on side streams with workspaces of their own do not disturb each other."""
     dtype = BF

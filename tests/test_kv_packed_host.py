@@ -72,7 +72,11 @@ def test_more_work_than_a_launch_takes_is_refused():
     assert fn(*{**good, "total": 1 << 24, "H_kv": 64}.values()) == lla.LLA_ERR_INVALID_ARG
     fn = kv.lib().lla_kv_prefill_attn
     good = CALLS["lla_kv_prefill_attn"][0]
-    assert fn(*{**good, "total": 1 << 23, "H": 256, "H_kv": 256}.values()) == lla.LLA_ERR_INVALID_ARG
+    for H in (256, 128):
+        assert fn(*{**good, "total": 1 << 23, "H": H, "H_kv": H}.values()) == lla.LLA_ERR_INVALID_ARG
+    fn = kv.lib().lla_kv_decode_attn_shared
+    good = CALLS["lla_kv_decode_attn_shared"][0]
+    assert fn(*{**good, "B": 1024, "H": 1 << 14}.values()) == lla.LLA_ERR_INVALID_ARG
 
 
 SIZES = [1, 2, 3, 7, 8, 16, 31, 64, 200, 513, 1024]
