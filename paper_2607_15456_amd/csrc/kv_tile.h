@@ -144,7 +144,8 @@ __device__ __forceinline__ int wave_sum(int v) {
 // The x-th tile of a packed batch, those that stand last in their sequences first: what
 // a causal tile costs goes by its place, and a heavy one that begins late would run
 // alone at the end.  Tiles are numbered by their places' tile in the sequence, v = s_from[b] + nth;
-// at_least(v) counts those at v or behind.  Every wavefront of the workgroup finds it.
+// at_least(v) counts those at v or behind; none is behind `most`.  Every wavefront of the
+// workgroup finds it.
 struct HeavyFirst {
   const int *s_first, *s_from;
   int B;
@@ -165,7 +166,7 @@ struct HeavyFirst {
       if (at_least(mid) > x) lo = mid;
       else hi = mid - 1;
     }
-    int skip = x - at_least(lo + 1);  // of the entries with a tile at lo
+    int skip = max(0, x - at_least(lo + 1));  // of the entries with a tile at lo
     entry = nth = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
       const int b = b0 + threadIdx.x % kWave;

@@ -200,8 +200,9 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   const int group = args.H / args.p.Hkv;
   int last_from = 0;  // the last tile's number in its sequence, at most
   if constexpr (Mode == kPacked) {
+    // (a start past the bound counts as at it: the search for a tile ends at last_from)
     for (int b = tid; b < args.B; b += kThreads)
-      s_runs[b] = (int)min((int64_t)max(0, args.start[b]) * group / kCols, kFarTile);
+      s_runs[b] = (int)min((int64_t)max(0, min(args.start[b], args.n_ctx)) * group / kCols, kFarTile);
     count_packed<kThreads>(args, kCols, args.small_rows, 0x7fffffff, s_first, s_wave);
     last_from = (int)(min((int64_t)args.n_ctx * group / kCols, kFarTile) + (int64_t)args.total * group / kCols) + 1;
   } else {

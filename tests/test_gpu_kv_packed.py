@@ -395,6 +395,25 @@ def test_prefill_offsets_that_decrease_do_no_harm(dtype, offsets):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("starts", [[0, 100000, 0], [1 << 30, 5, (1 << 31) - 1], [700, 1 << 24, 1 << 26]])
+def test_prefill_places_far_past_the_bound(dtype, starts):
+    """NaN, and nothing else of the batch is harmed: the order of the tiles goes by places within the bound."""
+    new, n_ctx = [300, 280, 310], 200
+    table, n_pages = pages_for([700] * 3, np.random.default_rng(0))
+    kp, vp = pool(1, n_pages, 2, 64, dtype)
+    q = normal((sum(new), 4, 64), 2, dtype)
+    offset = np.concatenate(([0], np.cumsum(new)))
+    out = kv.prefill_attn(q, kp, vp, ints(table), ints(offset), ints(starts), n_ctx=n_ctx)
+    for b in range(3):
+        fine = max(0, min(new[b], n_ctx - starts[b]))
+        assert out[offset[b] + fine:offset[b + 1]].isnan().all()
+        if fine:
+            rows = slice(offset[b], offset[b] + fine)
+            ref = prefill_reference(q[rows], kp, vp, table[b:b + 1], [0, fine], [starts[b]], None, 1 / 8, 0, 0, dtype, F32)
+            near(out[rows], ref[0], ref[2], f"entry {b}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("n,start", [(2, 70), (40, 50), (300, 100)])
 def test_prefill_masked_places_may_hold_anything(dtype, bad, n, start):
