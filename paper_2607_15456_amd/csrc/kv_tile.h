@@ -53,8 +53,9 @@ struct RowKeys {
 // is out of its range.
 enum TileState { kFine, kZeros, kNone };
 
-// Sums stop here: counts of sound arguments stay below, others' do no harm.
-constexpr int kMostSum = 1 << 30;
+// Sums stop here: counts of sound arguments stay below, others' do no harm.  Two sums
+// that have stopped add up to less than 2^31.
+constexpr int kMostSum = (1 << 30) - 1;
 __device__ __forceinline__ int add_up(int x, int y) { return min(x + y, kMostSum); }
 
 // Sum over the workgroup of v's of lower threads (0 <= v <= kMostSum).
