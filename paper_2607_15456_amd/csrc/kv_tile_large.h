@@ -303,6 +303,7 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
     f32x16 o[FT];
 #pragma unroll
     for (int f = 0; f < FT; ++f) o[f] = f32x16{0.f};
+    // (the last tile's is 0 here, or all have read it: a barrier of add_nonfinite's is between)
     if (tid == 0) s_odd = 0;
     int now = page_of(s), next = s + 1 < end ? page_of(s + 1) : -1;
     bool whole = t.keys.whole(first_token(s), kTok);

@@ -10,9 +10,15 @@ import pytest
 import torch
 
 from paper_2607_15456_amd import kv
-from tests.test_gpu_kv_packed import DEV, ints
+from tests.helpers import f64
+from tests.test_gpu_kv_packed import BF, DEV, F32, bounds, ints, near, normal, pages_for, places, pool, prefill_reference
 
 pytestmark = pytest.mark.gpu
+
+
+def pages_for_all(ends):
+    """A table of pages for sequences of these ends, in any order."""
+    return pages_for(ends, np.random.default_rng(len(ends)))
 
 
 @pytest.mark.parametrize("B,total,least", [(1024, 1 << 22, 1 << 22), (512, 1 << 23, 1 << 23), (1024, (1 << 24) - 1, 1 << 30),
@@ -37,3 +43,96 @@ def test_slots_whose_lengths_add_up_past_32_bits(B, total, least):
     assert torch.equal(got.entry.long(), torch.where(some, entry, -1))
     assert torch.equal(got.pos.long(), torch.where(some, place, -1))
     assert torch.equal(got.slot, torch.where(some & (place < 128), 64 * entry + place % 64, -1))
+
+
+# ---------------------------------------------------------------------------
+# more tiles than a launch has workgroups
+# ---------------------------------------------------------------------------
+
+def same_bits(x, y):
+    return torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,out_dtype,H,n,copies", [(BF, BF, 64, 257, 256), (BF, F32, 64, 257, 256), (BF, F32, 128, 3, 256),
+                                                        (F32, F32, 128, 17, 128)])
+def test_prefill_of_more_tiles_than_workgroups(dtype, out_dtype, H, n, copies):
+    """A workgroup that takes a second tile leaves nothing of the first one in it, values that are not finite among
+    them: four entries, one with such values, and copies of them that have to have the same bits."""
+    d, starts = 32, [0, 5, 64, 100]
+    table, n_pages = pages_for_all([s + n for s in starts])
+    kp, vp = pool(1, n_pages, H, d, dtype)
+    clean = vp.clone()
+    vp[table[2, (64 + n // 2) // 64], :, 7, (64 + n // 2) % 64] = float("nan")  # of entry 2's token n // 2
+    q = normal((4 * n, H, d), 3, dtype)
+    t, st = ints(np.tile(table, (copies, 1))), ints(starts * copies)
+    offset = ints(np.arange(4 * copies + 1) * n)
+    assert 4 * copies * -(-n // (256 if dtype == BF else 16)) * H > 1 << 16
+    out = kv.prefill_attn(q.repeat(copies, 1, 1), kp, vp, t, offset, st, n_ctx=64 * table.shape[1], out_dtype=out_dtype)
+    one = out[:4 * n].clone()
+    for i in range(copies):
+        assert same_bits(out[4 * n * i:4 * n * (i + 1)], one), i
+    bad = torch.zeros_like(one, dtype=torch.bool)
+    bad[2 * n + n // 2:3 * n, :, 7] = True
+    assert torch.equal(one.isfinite(), ~bad)
+    heads = [0, 1, H - 1]
+    ref = prefill_reference(q[:, heads].contiguous(), kp[:, heads], clean[:, heads], table, np.arange(5) * n, starts, None, d ** -0.5,
+                            0, 0, dtype, out_dtype)
+    ok = (~bad)[:, heads].cpu().numpy()
+    got = one[:, heads].cpu()
+    near(got[torch.as_tensor(ok)], ref[0][ok], ref[2][ok], f"{dtype} {out_dtype} {n}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_shared_decode_of_more_tiles_than_workgroups(dtype):
+    H, d, B = 128, 32, 1024
+    table, n_pages = pages_for_all([70, 90, 130, 65])
+    kp, vp = pool(1, n_pages, H, d, dtype)
+    q = normal((4, H, d), 3, dtype)
+    rows, length = ints(list(range(4)) * (B // 4)), ints([70, 90, 130, 65])
+    lead, shared = ints([4 * (b // 4) for b in range(B)]), ints([50] * B)
+    assert B * H > 1 << 16
+    out = kv.decode_attn_shared(q.repeat(B // 4, 1, 1), kp, vp, ints(table), length, lead, shared, n_ctx=192, rows=rows)
+    assert same_bits(out, out[:4].repeat(B // 4, 1, 1))
+    kn, vn, qn = f64(kp), f64(vp), f64(q)
+    for b, end in enumerate([70, 90, 130, 65]):
+        for h in (0, H - 1):
+            k, v = places(table, b, end, kn, vn, h)
+            k[:50], v[:50] = places(table, 0, 50, kn, vn, h)
+            ref, _, tol, _ = bounds(qn[b, h:h + 1], k, v, np.ones((1, end), dtype=bool), d ** -0.5, dtype, F32, 0.0)
+            near(out[b, h:h + 1], ref, tol, f"entry {b} head {h}")
+
+
+# ---------------------------------------------------------------------------
+# batches of hundreds of entries
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("B,n_ctx,kind", [(65, 256, "mixed"), (130, 256, "tied"), (1024, 256, "mixed"), (1024, 192, "tied"),
+                                          (300, 1000, "mixed"), (70, 1000, "tied")])
+def test_prefill_of_many_entries(dtype, out_dtype, B, n_ctx, kind):
+    """Empty entries, single tokens, few and many tokens at places that spread, or that are all the same, so
+    that the order of the tiles goes by the entries' numbers alone.  Up to 256 places no tile is cut."""
+    rng = np.random.default_rng(B + n_ctx)
+    H, H_kv, d = 2, 2, 32
+    if kind == "tied":
+        new, start = np.full(B, 40), np.full(B, n_ctx - 40)
+        new[5], new[B - 2] = 1, 0
+    else:
+        new = rng.choice([0, 1, 3, 16, 17, 30, 60], B)
+        new[rng.integers(0, B, 3)] = 190
+        start = rng.integers(0, n_ctx - new + 1)
+    assert kind != "tied" or (new * H // H_kv > 16).sum() > 64
+    seqs = 5  # whose pages all entries read
+    table, n_pages = pages_for_all([n_ctx] * seqs)
+    rows = rng.integers(0, seqs, B)
+    kp, vp = pool(7, n_pages, H_kv, d, dtype)
+    total = int(new.sum())
+    q = normal((total + 3, H, d), 8, dtype)
+    offset = np.concatenate(([0], np.cumsum(new)))
+    out = torch.full((total + 3, H, d), 7.0, dtype=out_dtype, device=DEV)
+    lse = torch.full((total + 3, H), 7.0, dtype=F32, device=DEV)
+    kv.prefill_attn(q, kp, vp, ints(table), ints(offset), ints(start), n_ctx=n_ctx, rows=ints(rows), out=out, lse=lse)
+    ref, ref_lse, tol, lse_tol = prefill_reference(q, kp, vp, table, offset, start, rows, d ** -0.5, 0, 0, dtype, out_dtype)
+    near(out[:total], ref[:total], tol[:total], f"{B} entries, {kind}")
+    near(lse[:total], ref_lse[:total], lse_tol[:total], f"{B} entries, {kind}, lse")
+    assert (out[total:] == 7).all() and (lse[total:] == 7).all()
