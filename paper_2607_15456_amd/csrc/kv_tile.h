@@ -363,6 +363,14 @@ __device__ __forceinline__ const KvTileArgs& args_again() {
   return *(const KvTileArgs*)p;
 }
 
+// A pointer that is the same in all lanes, in scalar registers.
+template <typename T>
+__device__ __forceinline__ const T* scalar(const T* p) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return reinterpret_cast<const T*>(((uint64_t)hi << 32) | lo);
+}
+
 // Values that are not finite, of tokens that only some of a tile's rows attend, stay out
 // of the matrix product (a weight of zero would make NaN of them).  This adds them to the
 // stored results, or partial rows, of the rows that attend them; rare, so nothing of it is

@@ -97,11 +97,12 @@ __global__ __launch_bounds__(kWaves* kWave, D <= 128 && NT * D <= 128 ? 2 : 1) v
 #pragma unroll
       for (int x = 0; x < NT; ++x) rk[x] = t.row_keys<Mode>(a, kvh, min(x * kTile + c, t.rows - 1), q_at[x], unused);
       constexpr int kHeadBytes = kPage * D * Step::kBytes;
-      k_pool = static_cast<const char*>(a.p.k) + (int64_t)kvh * kHeadBytes;
-      v_pool = static_cast<const char*>(a.p.v) + (int64_t)kvh * kHeadBytes;
-      table = a.p.table + (int64_t)t.row * a.p.max_pages;
-      n_pages = a.p.n_pages;
-      page_bytes = (int64_t)a.p.Hkv * kHeadBytes;
+      // (all of a workgroup's lanes agree on them: a page's resource stays in scalar registers)
+      k_pool = scalar(static_cast<const char*>(a.p.k) + (int64_t)kvh * kHeadBytes);
+      v_pool = scalar(static_cast<const char*>(a.p.v) + (int64_t)kvh * kHeadBytes);
+      table = scalar(a.p.table + (int64_t)t.row * a.p.max_pages);
+      n_pages = __builtin_amdgcn_readfirstlane(a.p.n_pages);
+      page_bytes = (int64_t)__builtin_amdgcn_readfirstlane(a.p.Hkv) * kHeadBytes;
       qscale = a.qscale;
       q = a.q;
     }
