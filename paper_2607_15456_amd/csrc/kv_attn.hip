@@ -11,50 +11,52 @@ namespace lla {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256;
 constexpr float kLn2 = 0.69314718055994531f;
 
 // A result from its partial rows: d / 4 neighbouring threads hold four features each, and
-// all of them the maximum and the sum.
-struct Joined {
-  float m = neg_inf(), l = 0.f;
-  f32x4 o = f32x4{0.f};
-  // `count` partial rows from `at`, `stride` floats apart
-  __device__ __forceinline__ void add(const float* at, int64_t stride, int count, int d, int f) {
+// all of them the maximum and the sum.  `count` partial rows from `at`, `stride` floats apart, join it.
+__device__ __forceinline__ void join_slices(float& m, float& l, f32x4& o, const float* at, int64_t stride, int count, int d, int f) {
 #pragma unroll 4
-    for (int s = 0; s < count; ++s) {
-      const float* part = at + s * stride;
-      const float m2 = part[d], l2 = part[d + 1], to = fmaxf(m, m2), base = to == neg_inf() ? 0.f : to;
-      const f32x4 o2 = *reinterpret_cast<const f32x4*>(part + f);
-      const float x = __builtin_amdgcn_exp2f(m - base), y = __builtin_amdgcn_exp2f(m2 - base);
-      m = to;
-      l = l * x + l2 * y;
-      o = o * x + o2 * y;
-    }
+  for (int s = 0; s < count; ++s) {
+    const float* part = at + s * stride;
+    const float m2 = part[d], l2 = part[d + 1], to = fmaxf(m, m2), base = to == neg_inf() ? 0.f : to;
+    const f32x4 o2 = *reinterpret_cast<const f32x4*>(part + f);
+    const float x = __builtin_amdgcn_exp2f(m - base), y = __builtin_amdgcn_exp2f(m2 - base);
+    m = to;
+    l = l * x + l2 * y;
+    o = o * x + o2 * y;
   }
-  __device__ __forceinline__ void store(const KvTileArgs& a, int64_t row, int f) const {
-    store_row4(a, row, f, o / l);
-    if (a.lse && f == 0) a.lse[row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
-  }
-};
+}
+__device__ __forceinline__ void store_joined(const KvTileArgs& a, int64_t row, int f, float m, float l, f32x4 o) {
+  store_row4(a, row, f, o / l);
+  if (a.lse && f == 0) a.lse[row] = ((m == neg_inf() ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+}
 
-// Partial rows of a tile's row x: from slice 0's, how far apart and how many.
+// Partial rows of a tile's row: from slice 0's, how far apart and how many.
 struct Slices {
   const float* at;
   int64_t stride;
   int count;
-  __device__ __forceinline__ Slices(const KvTileArgs& a, const Tile& t, int tiles, int tile, int slices, const KvTileCut& cut,
-                                    int cols, int kvh, int x) {
-    const int per = slice_pages(cut.least, t.keys.pages, slices), row = a.p.d + 4;
-    at = cut.part + ((int64_t)item_of(a, tiles, 0, tile, kvh) * cols + x) * row;
-    stride = (int64_t)tiles * a.p.Hkv * cols * row;
-    count = (t.keys.pages + per - 1) / per;
-  }
 };
+// Of row x of a tile of `cols` rows and `pages` pages, number `tile` of `tiles` that are cut into `slices`.
+__device__ __forceinline__ Slices slices_of(const KvTileArgs& a, int pages, int least, const float* part, int tiles, int tile,
+                                            int slices, int cols, int kvh, int x) {
+  const int per = slice_pages(least, pages, slices), row = a.p.d + 4;
+  return {part + ((int64_t)item_of(a, tiles, 0, tile, kvh) * cols + x) * row, (int64_t)tiles * a.p.Hkv * cols * row,
+          (pages + per - 1) / per};
+}
 
-constexpr int kJoinRows = 32;  // of a tile, that a workgroup joins at a time
+// Rows of a tile that a workgroup joins at a time: one a thread, d / 4 threads for each.
+__host__ __device__ __forceinline__ int join_rows(int d) { return kThreads / (d / 4); }
+__host__ __device__ __forceinline__ int join_chunks(int d, int cols) { return (cols + join_rows(d) - 1) / join_rows(d); }
 
-// Packed tokens: the tiles that were cut, a workgroup 32 rows of one.
+// What differs between the kinds of tiles is chosen value by value, and a result's sums are
+// values of their own: a choice between structures, or a structure read in part,
+// is kept in memory, for which a workgroup reads its dispatch packet from the host's memory (11 us
+// of the join's 22 after a piece of 512 tokens over 15,001).
+
+// Packed tokens: the tiles that were cut, a workgroup some rows of one.
 __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int large_cols) {
   __shared__ int s_small[kMostEntries + 1], s_large[kMostEntries + 1];
   __shared__ int s_wave[kThreads / kWave];
@@ -62,31 +64,29 @@ __global__ __launch_bounds__(kThreads) void join_packed_kernel(KvTileArgs a, int
   count_packed<kThreads>(a, large_cols, a.small_rows, kAllRows, s_large, s_wave);
   const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, small * a.p.Hkv);
   const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, large * a.p.Hkv);
-  const int chunks = large_cols / kJoinRows;
-  const int of_small = small_slices > 1 ? small * a.p.Hkv : 0;
-  const int of_large = large_slices > 1 ? large * a.p.Hkv * chunks : 0;
-  const int lanes = a.p.d / 4, r = threadIdx.x / lanes, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
-  if (r >= step) return;
+  const int of_small = small_slices > 1 ? small * a.p.Hkv * join_chunks(a.p.d, a.small_cols) : 0;
+  const int of_large = large_slices > 1 ? large * a.p.Hkv * join_chunks(a.p.d, large_cols) : 0;
+  const int lanes = a.p.d / 4, r = threadIdx.x / lanes, f = 4 * (threadIdx.x % lanes);
+  if (r >= join_rows(a.p.d)) return;
+#pragma unroll 1
   for (int i = blockIdx.x; i < of_small + of_large; i += gridDim.x) {
     const bool is_small = i < of_small;
-    const int j = is_small ? i : i - of_small, unit = is_small ? j : j / chunks, chunk = is_small ? 0 : j - unit * chunks;
-    const int tile = unit / a.p.Hkv, kvh = unit - tile * a.p.Hkv;
-    const int* first = is_small ? s_small : s_large;
-    const int b = last_at_most(first, a.B, tile), cols = is_small ? a.small_cols : large_cols;
+    const int cols = is_small ? a.small_cols : large_cols, chunks = join_chunks(a.p.d, cols), j = is_small ? i : i - of_small;
+    const int unit = j / chunks, tile = unit / a.p.Hkv, kvh = unit - tile * a.p.Hkv;
+    const int x = (j - unit * chunks) * join_rows(a.p.d) + r;
+    const int b = is_small ? last_at_most(s_small, a.B, tile) : last_at_most(s_large, a.B, tile);
     Tile t;
-    t.at<kPacked>(a, b, cols, tile - first[b]);
-    if (t.state != kFine) continue;
-    const int end = min(t.rows, (chunk + 1) * kJoinRows);
-    for (int x = chunk * kJoinRows + r; x < end; x += step) {
-      const Slices in = is_small ? Slices(a, t, small, tile, small_slices, a.small, cols, kvh, x)
-                                 : Slices(a, t, large, tile, large_slices, a.large, cols, kvh, x);
-      if (in.count <= 1) break;  // (written by the tile itself)
-      Joined row;
-      row.add(in.at, in.stride, in.count, a.p.d, f);
-      int64_t q_at, out_at;
-      t.row_keys<kPacked>(a, kvh, x, q_at, out_at);
-      row.store(a, out_at, f);
-    }
+    t.at<kPacked>(a, b, cols, tile - (is_small ? s_small[b] : s_large[b]));
+    if (t.state != kFine || x >= t.rows) continue;
+    const Slices in = slices_of(a, t.keys.pages, is_small ? a.small.least : a.large.least, is_small ? a.small.part : a.large.part,
+                                is_small ? small : large, tile, is_small ? small_slices : large_slices, cols, kvh, x);
+    if (in.count <= 1) continue;  // (written by the tile itself)
+    float m = neg_inf(), l = 0.f;
+    f32x4 o = f32x4{0.f};
+    join_slices(m, l, o, in.at, in.stride, in.count, a.p.d, f);
+    int64_t q_at, out_at;
+    t.row_keys<kPacked>(a, kvh, x, q_at, out_at);
+    store_joined(a, out_at, f, m, l, o);
   }
 }
 
@@ -98,40 +98,56 @@ __global__ __launch_bounds__(kThreads) void join_shared_kernel(KvTileArgs a) {
   const int small = tiles_of(a.small, s_small[a.B]), small_slices = tile_slices(a.small, small * a.p.Hkv);
   const int large = tiles_of(a.large, s_large[a.B]), large_slices = tile_slices(a.large, large * a.p.Hkv);
   const int group = a.H / a.p.Hkv, cols = a.small_cols, blocks = (group + cols - 1) / cols;
-  const int lanes = a.p.d / 4, f = 4 * (threadIdx.x % lanes), step = kThreads / lanes;
+  const int lanes = a.p.d / 4, f = 4 * (threadIdx.x % lanes), step = join_rows(a.p.d);
   const int rows = a.B * a.H;  // (below 2^31, as every number of tiles and their slices)
   if ((int)threadIdx.x / lanes >= step) return;
+#pragma unroll 1
   for (int64_t at = (int64_t)blockIdx.x * step + threadIdx.x / lanes; at < rows; at += (int64_t)gridDim.x * step) {
     const int i = (int)at, b = i / a.H, h = i - b * a.H, kvh = h / group, r = h - kvh * group;
-    const int shared = a.shared[b];
-    Tile own;
-    own.at<kOwn>(a, b, cols, r / cols);
-    TileState state = own.state;
-    Joined row;
-    if (state == kFine && shared > 0) {
-      // the tile that b's queries are of begins at the last entry up to b that goes on with none
-      const int e = last_at_most(s_runs, a.B, s_runs[b + 1] - 1), many = run_entries(a, s_runs, e);
-      const bool is_small = s_small[e + 1] > s_small[e];
-      const int of = is_small ? cols : a.prefix_cols, col = (b - e) * group + r, nth = col / of, x = col - nth * of;
-      Tile t;
-      t.at<kPrefix>(a, e, of, nth, many);
-      const Slices in = is_small ? Slices(a, t, small, s_small[e] + nth, small_slices, a.small, of, kvh, x)
-                                 : Slices(a, t, large, s_large[e] + nth, large_slices, a.large, of, kvh, x);
-      if (t.state == kFine) row.add(in.at, in.stride, in.count, a.p.d, f);
-      else state = kNone;
+    const int own_block = r / cols;
+    Tile t;
+    t.at<kOwn>(a, b, cols, own_block);
+    TileState state = t.state;
+    const int own_pages = t.keys.pages;
+    float m = neg_inf(), l = 0.f;
+    f32x4 o = f32x4{0.f};
+    // the prompt's slices, then its own
+#pragma unroll 1
+    for (int mine = a.shared[b] <= 0; mine < 2 && state == kFine; ++mine) {
+      int least = a.small.least, tiles = a.B * blocks, tile = b * blocks + own_block, slices = a.own_slices, of = cols,
+          x = r - own_block * cols, pages = own_pages;
+      const float* part = a.own_part;
+      if (!mine) {
+        // the tile that b's queries are of begins at the last entry up to b that goes on with none
+        const int e = last_at_most(s_runs, a.B, s_runs[b + 1] - 1);
+        const bool is_small = s_small[e + 1] > s_small[e];
+        of = is_small ? cols : a.prefix_cols;
+        const int col = (b - e) * group + r, nth = col / of;
+        x = col - nth * of;
+        t.at<kPrefix>(a, e, of, nth, b - e + 1);  // (its rows up to b's)
+        state = t.state;
+        if (state != kFine) break;
+        pages = t.keys.pages;
+        tile = (is_small ? s_small[e] : s_large[e]) + nth;
+        tiles = is_small ? small : large;
+        slices = is_small ? small_slices : large_slices;
+        least = is_small ? a.small.least : a.large.least;
+        part = is_small ? a.small.part : a.large.part;
+      }
+      const Slices in = slices_of(a, pages, least, part, tiles, tile, slices, of, kvh, x);
+      join_slices(m, l, o, in.at, in.stride, in.count, a.p.d, f);
     }
-    if (state != kFine) {
-      const float none = state == kNone ? __builtin_nanf("") : 0.f;
-      store_row4(a, i, f, f32x4{none, none, none, none});
-      if (a.lse && f == 0) a.lse[i] = state == kNone ? none : neg_inf();
+    if (state == kFine) {
+      store_joined(a, i, f, m, l, o);
       continue;
     }
-    const KvTileCut cut{0, a.small.least, 0, 0, a.own_part};
-    const Slices in(a, own, a.B * blocks, b * blocks + r / cols, a.own_slices, cut, cols, kvh, r % cols);
-    row.add(in.at, in.stride, in.count, a.p.d, f);
-    row.store(a, i, f);
+    const float none = state == kNone ? __builtin_nanf("") : 0.f;
+    store_row4(a, i, f, f32x4{none, none, none, none});
+    if (a.lse && f == 0) a.lse[i] = state == kNone ? none : neg_inf();
   }
 }
+
+constexpr int kMostJoins = 1024;  // workgroups of a join
 
 int64_t blocks_of(int64_t rows, int cols) { return (rows + cols - 1) / cols; }
 // Most pages that a tile of `cols` rows reads.
@@ -211,8 +227,8 @@ hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
   if (e != hipSuccess) return e;
   if (s.small_tiles) e = launch_small_packed(a, grid(s.small_tiles, std::min<int64_t>(s.small_partial, a.small.wgs)), stream);
   if (e != hipSuccess || s.small_partial + s.large_partial == 0) return e;
-  const int64_t joins = s.small_partial + s.large_partial * (large_cols(a.p.d) / kJoinRows);
-  hipLaunchKernelGGL(join_packed_kernel, dim3((unsigned)std::min<int64_t>(joins, 1024)), dim3(kThreads), 0, stream, a,
+  const int64_t joins = s.small_partial * join_chunks(a.p.d, a.small_cols) + s.large_partial * join_chunks(a.p.d, large_cols(a.p.d));
+  hipLaunchKernelGGL(join_packed_kernel, dim3((unsigned)std::min<int64_t>(joins, kMostJoins)), dim3(kThreads), 0, stream, a,
                      large_cols(a.p.d));
   return hipGetLastError();
 }
@@ -275,8 +291,8 @@ hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
   if (e != hipSuccess) return e;
   e = launch_small_shared(a, grid(s.small + s.own), stream);
   if (e != hipSuccess) return e;
-  const int64_t joins = blocks_of((int64_t)a.B * a.H, kThreads / (a.p.d / 4));
-  hipLaunchKernelGGL(join_shared_kernel, dim3((unsigned)std::min<int64_t>(joins, 1024)), dim3(kThreads), 0, stream, a);
+  const int64_t joins = blocks_of((int64_t)a.B * a.H, join_rows(a.p.d));
+  hipLaunchKernelGGL(join_shared_kernel, dim3((unsigned)std::min<int64_t>(joins, kMostJoins)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

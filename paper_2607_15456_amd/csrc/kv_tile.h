@@ -221,7 +221,8 @@ __device__ __forceinline__ void count_shared(const KvTileArgs& a, int* s_runs, i
     const int most = a.small_rows / group, blocks = (group + a.prefix_cols - 1) / a.prefix_cols;
     const bool few = a.small_rows == kAllRows ||
                      (most >= 1 && (b + most >= a.B || s_runs[b + most + 1] > s_runs[b + 1]));
-    (few ? small : large).n[i] = blocks;
+    small.n[i] = few ? blocks : 0;  // (a choice between the two would put both into memory)
+    large.n[i] = few ? 0 : blocks;
   }
   if (s_small) small.sum(a.B, s_small, s_wave);
   if (s_large) large.sum(a.B, s_large, s_wave);
