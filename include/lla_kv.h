@@ -363,10 +363,8 @@ lla_status lla_kv_prefill_workspace_bytes(int dtype, int out_dtype, int B, int t
  * tokens of its batch too: values that are not finite make results not finite (NaN
  * or infinite) of the tokens that attend them, in their own feature.
  * Offsets that decrease leave some of the tokens undone and do no other harm.
- * bf16: products are exact; with out_dtype LLA_F32 the softmax weights enter their
- * product with the values with their 24 bits; with LLA_BF16 they may be rounded to bf16,
- * and are then summed as rounded (a weight is off by at most 2^-8 of itself, their sum
- * not at all).
+ * bf16: products are exact, and the softmax weights enter their product with the values
+ * with their 24 bits, whatever out_dtype: results in bf16 are those in fp32, rounded once.
  * Requires 1 <= B <= LLA_KV_MAX_ROWS, 1 <= total < 2^24, H a multiple of H_kv >= 1,
  * total*H < 2^30, sink >= 0, window >= 0, sink = 0 without a window.
  * Errors: LLA_ERR_INVALID_ARG, LLA_ERR_WORKSPACE, LLA_ERR_HIP.
@@ -407,8 +405,7 @@ lla_status lla_kv_shared_workspace_bytes(int dtype, int B, int H, int H_kv, int 
  * the places from shared[b] to its length through its own pages.  (lla_pages_shared
  * finds both; a program that knows its prompts may give other numbers, down to a place
  * inside a page.)  Arguments and results are otherwise those of lla_kv_decode_attn without
- * a window; with out_dtype LLA_BF16 weights over a shared prompt may enter their product
- * with 16 bits.
+ * a window.
  *   lead, shared  int32 [B]
  * An entry with shared[b] < 0 or above its length, or with shared[b] > 0 and a lead[b]
  * outside [0, B), whose row is out of range, or that has fewer places, gets NaN.

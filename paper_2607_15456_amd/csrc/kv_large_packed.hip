@@ -7,9 +7,7 @@ namespace lla {
 
 hipError_t launch_large_packed(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
   if (a.p.d > 128) return launch_large_packed_wide(a, grid, stream);
-  // results in bf16 take weights rounded to it
-  return a.out_dtype == LLA_BF16 ? launch_large_narrow<1, kPacked>(a, grid, stream)
-                                 : launch_large_narrow<3, kPacked>(a, grid, stream);
+  return launch_large_narrow<kPacked>(a, grid, stream);
 }
 
 }  // namespace lla

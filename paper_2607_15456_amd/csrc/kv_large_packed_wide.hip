@@ -6,8 +6,7 @@
 namespace lla {
 
 hipError_t launch_large_packed_wide(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
-  return a.out_dtype == LLA_BF16 ? launch_large_wide<1, kPacked>(a, grid, stream)
-                                 : launch_large_wide<3, kPacked>(a, grid, stream);
+  return launch_large_wide<kPacked>(a, grid, stream);
 }
 
 }  // namespace lla

@@ -27,10 +27,8 @@
 namespace lla {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Terms: bf16 numbers that a weight enters its product as (1: rounded; 2: 16 bits; 3: all 24).
-template <int D, int Terms>
+template <int D>
 struct LargeTile {
   static constexpr int kWaves = D <= 128 ? 8 : 4, kThreads = kWaves * kWave, kCols = kWaves * 32;
   static constexpr int kTok = D <= 128 ? 64 : 32, kSteps = kPage / kTok;
@@ -137,35 +135,33 @@ struct LargeTile {
   __device__ __forceinline__ static uint4 value_operand(const char* lds, int c, int hf, int n) {
     return *reinterpret_cast<const uint4*>(lds + val_at(32 * (n % FT) + c, 2 * (n / FT) + hf));
   }
-  // o += V^T P^T; returns the sum of this lane's weights as they entered it.
+  // o += V^T P^T; returns the sum of this lane's weights.  A weight enters the product with its 24 bits, as three bf16:
+  // rounded to one or two it would save half or a quarter of the step's products (4 prompts of 4096
+  // tokens, 16 heads of 128: 348, 450 and 548 us with one, two and three), and would make what an
+  // entry gets go by the kind of tile that its batch gives it.
   template <int kAhead>
   __device__ __forceinline__ float values(const char* lds, const uint4 (&ahead)[kAhead], int c, int hf, const f32x16 (&p)[KT],
                                           f32x16 (&o)[FT]) const {
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < 2 * KT; ++u) {
-      bf16x8 w[Terms];
+      bf16x8 w[3];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float x = p[u / 2][8 * (u % 2) + e];
-        if constexpr (Terms > 1) sum += x;
+        sum += x;
 #pragma unroll
-        for (int n = 0; n < Terms; ++n) {
+        for (int n = 0; n < 3; ++n) {
           w[n][e] = (__bf16)x;
           x -= (float)w[n][e];
         }
-      }
-      if constexpr (Terms == 1) {
-        const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[0][2 * e], w[0][2 * e + 1]}, one, sum, false);
       }
 #pragma unroll
       for (int f = 0; f < FT; ++f) {
         const int i = u * FT + f;
         const uint4 x = i < kAhead ? ahead[i < kAhead ? i : 0] : value_operand(lds, c, hf, i);
 #pragma unroll
-        for (int n = 0; n < Terms; ++n)
+        for (int n = 0; n < 3; ++n)
           o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), w[n], o[f], 0, 0, 0);
       }
     }
@@ -184,9 +180,9 @@ __device__ __forceinline__ float max_halves(float x) {
 // most 2^-8 of a power below (1 operation instead of 2 for each score).
 constexpr float kFar = 65536.f;
 
-template <int D, int Terms, TileMode Mode>
-__global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_kernel(KvTileArgs args) {
-  typedef LargeTile<D, Terms> L;
+template <int D, TileMode Mode>
+__global__ __launch_bounds__(LargeTile<D>::kThreads) void large_tile_kernel(KvTileArgs args) {
+  typedef LargeTile<D> L;
   constexpr int kCols = L::kCols, kThreads = L::kThreads, KT = L::KT, FT = L::FT, kTok = L::kTok;
   constexpr int kHeadBytes = kPage * D * 2;
   __shared__ int s_first[kMostEntries + 1], s_runs[kMostEntries + 1];
@@ -445,29 +441,29 @@ __global__ __launch_bounds__((LargeTile<D, Terms>::kThreads)) void large_tile_ke
   }
 }
 
-template <int D, int Terms, TileMode Mode>
+template <int D, TileMode Mode>
 hipError_t launch_large(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
-  typedef LargeTile<D, Terms> L;
-  hipLaunchKernelGGL((large_tile_kernel<D, Terms, Mode>), dim3(grid), dim3(L::kThreads), 2 * L::kBuffer, stream, a);
+  typedef LargeTile<D> L;
+  hipLaunchKernelGGL((large_tile_kernel<D, Mode>), dim3(grid), dim3(L::kThreads), 2 * L::kBuffer, stream, a);
   return hipGetLastError();
 }
 // Widths of up to 128, and above, which are built apart.
-template <int Terms, TileMode Mode>
+template <TileMode Mode>
 hipError_t launch_large_narrow(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
   switch (a.p.d) {
-    case 32: return launch_large<32, Terms, Mode>(a, grid, stream);
-    case 64: return launch_large<64, Terms, Mode>(a, grid, stream);
-    case 96: return launch_large<96, Terms, Mode>(a, grid, stream);
-    default: return launch_large<128, Terms, Mode>(a, grid, stream);
+    case 32: return launch_large<32, Mode>(a, grid, stream);
+    case 64: return launch_large<64, Mode>(a, grid, stream);
+    case 96: return launch_large<96, Mode>(a, grid, stream);
+    default: return launch_large<128, Mode>(a, grid, stream);
   }
 }
-template <int Terms, TileMode Mode>
+template <TileMode Mode>
 hipError_t launch_large_wide(const KvTileArgs& a, unsigned grid, hipStream_t stream) {
   switch (a.p.d) {
-    case 160: return launch_large<160, Terms, Mode>(a, grid, stream);
-    case 192: return launch_large<192, Terms, Mode>(a, grid, stream);
-    case 224: return launch_large<224, Terms, Mode>(a, grid, stream);
-    default: return launch_large<256, Terms, Mode>(a, grid, stream);
+    case 160: return launch_large<160, Mode>(a, grid, stream);
+    case 192: return launch_large<192, Mode>(a, grid, stream);
+    case 224: return launch_large<224, Mode>(a, grid, stream);
+    default: return launch_large<256, Mode>(a, grid, stream);
   }
 }
 

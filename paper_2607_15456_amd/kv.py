@@ -577,8 +577,7 @@ def prefill_attn(q, k_pages, v_pages, table, offset, start, *, n_ctx: int, rows=
     of sequences rows[b] (None: b) and attend every place up to their own, below n_ctx,
     or with ``window`` of these the first ``sink`` and the last ``window``.  Their keys
     and values must have been written.  Entries of row -1 or start -1 give zeros, rows
-    that are no entry's are left as they are.  With out_dtype bfloat16 the softmax weights
-    are rounded to it for their product.  lse: float32 [total, H] or None; workspace:
+    that are no entry's are left as they are.  lse: float32 [total, H] or None; workspace:
     uint8 of prefill_workspace_bytes(...) (allocated here if None).  Returns out [total,
     H, d]."""
     dev = q.device

@@ -136,3 +136,46 @@ def test_prefill_of_many_entries(dtype, out_dtype, B, n_ctx, kind):
     near(out[:total], ref[:total], tol[:total], f"{B} entries, {kind}")
     near(lse[:total], ref_lse[:total], lse_tol[:total], f"{B} entries, {kind}, lse")
     assert (out[total:] == 7).all() and (lse[total:] == 7).all()
+
+
+# ---------------------------------------------------------------------------
+# weights keep all of their bits
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_results_in_bf16_are_those_in_fp32_rounded_once(dtype, d):
+    """Whatever kind of tile an entry is of, and whatever else is in its batch: nothing but the results' rounding
+    goes by the results' type."""
+    ends = [700, 300, 64, 1500]
+    table, n_pages = pages_for_all(ends)
+    kp, vp = pool(d, n_pages, 2, d, dtype)
+    t = ints(table)
+    for new in ([300, 1, 5, 40], [1, 1, 64, 1], [0, 0, 0, 900]):
+        q, start = normal((sum(new), 8, d), 5, dtype), [e - n for e, n in zip(ends, new)]
+        offset = ints(np.concatenate(([0], np.cumsum(new))))
+        for sink, window in ((0, 0), (3, 130)):
+            one, two = (kv.prefill_attn(q, kp, vp, t, offset, ints(start), n_ctx=1536, sink=sink, window=window, out_dtype=o)
+                        for o in (F32, BF))
+            assert one.isfinite().all() and torch.equal(one.to(BF), two), (new, sink)
+    q = normal((300, 8, d), 6, dtype)
+    for B in (3, 130, 300):  # answers to one prompt
+        args = (q[:B], kp, vp, t, ints([1500] * 4), ints([0] * B), ints([640] * B))
+        one, two = (kv.decode_attn_shared(*args, n_ctx=1536, rows=ints([3] * B), out_dtype=o) for o in (F32, BF))
+        assert one.isfinite().all() and torch.equal(one.to(BF), two), B
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+def test_a_token_does_not_depend_on_its_batch(out_dtype):
+    """The same entry alone, with more room, and among others: each time within what sums in 32 bits allow, which no
+    rounding of weights to fewer bits is."""
+    d, H = 128, 4
+    table, n_pages = pages_for_all([900, 1000, 800])
+    kp, vp = pool(3, n_pages, 1, d, BF)
+    q = normal((700, H, d), 4, BF)
+    t = ints(table)
+    ref, _, tol, _ = prefill_reference(q[:6], kp, vp, table[:1], [0, 6], [890], None, d ** -0.5, 0, 0, BF, F32)
+    calls = [(6, [0, 6], [890]), (700, [0, 6], [890]), (306, [0, 6, 306], [890, 700]), (6, [0, 6, 6, 6], [890, 0, 0])]
+    for total, offset, start in calls:
+        out = kv.prefill_attn(q[:total], kp, vp, t, ints(offset), ints(start), n_ctx=1024, out_dtype=out_dtype)[:6]
+        near(out, ref, tol if out_dtype == F32 else tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref), f"{total} {offset}")
