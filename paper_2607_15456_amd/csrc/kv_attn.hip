@@ -241,9 +241,9 @@ struct SharedShape {
     const int group = a.H / a.p.Hkv;
     const int64_t rows = (int64_t)a.B * group, blocks = blocks_of(group, a.prefix_cols);
     auto items = [&](const KvTileCut& cut, int64_t tiles) { return std::max(partial_tiles(a, cut, tiles), tiles * a.p.Hkv); };
-    // any entry may begin a run; large tiles are of runs of more than small_rows rows
+    // any entry may begin a run; small tiles are of runs of up to small_rows rows
     const int64_t runs = std::min<int64_t>(a.B, rows / (a.small_rows + (int64_t)1));
-    small_tiles = a.small_rows == kAllRows ? a.B * blocks : a.B;
+    small_tiles = a.small_rows == kAllRows ? a.B * blocks : group <= a.small_rows ? a.B : 0;
     large_tiles = runs * blocks;
     small = items(a.small, small_tiles);
     large = items(a.large, large_tiles);
@@ -255,27 +255,42 @@ struct SharedShape {
 };
 }  // namespace
 
-size_t kv_shared_shape(KvTileArgs& a) {
+// Whether runs of more than a small tile's rows take large tiles: bf16, from 3 * 2^30
+// multiply-adds of all queries with the whole context on.  32 heads on 8 of 128, us with small
+// tiles alone and with large ones: over a prompt of 4096 tokens 64 answers 56 and 70, 128
+// 80 and 91, 256 134 and 122, 1000 439 and 310; of 16,384 tokens 32 81 and 82, 64 116 and
+// 103, 128 183 and 132.  2 prompts of 64 answers, 16 heads on 2 of 64: 36 and 51; 8 of 4, 16 heads
+// of 128 over 2001: 50 and 57.  In fp32 the matrix instructions take as long from either.
+static bool shared_large(const KvTileArgs& a) {
+  return a.p.dtype == LLA_BF16 && (int64_t)a.B * a.H * a.p.d * a.n_ctx >= (int64_t)3 << 30;
+}
+static void shared_shape(KvTileArgs& a, bool large) {
   limits(a, 0);
-  const int group = a.H / a.p.Hkv;
   a.small_cols = small_cols_of(a, false);
-  const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(group, a.small_cols);
-  const bool all_small = a.p.dtype == LLA_F32;
-  a.small_rows = all_small ? kAllRows : a.small_cols;
-  a.prefix_cols = all_small ? a.small_cols : large_cols(a.p.d);
+  const int64_t units = (int64_t)a.B * a.p.Hkv * blocks_of(a.H / a.p.Hkv, a.small_cols);
+  a.small_rows = large ? a.small_cols : kAllRows;
+  a.prefix_cols = large ? large_cols(a.p.d) : a.small_cols;
   a.own_slices =
       (int)std::max<int64_t>(1, std::min<int64_t>(a.small.wgs / units, a.small.most));
+}
+size_t kv_shared_shape(KvTileArgs& a) {
+  shared_shape(a, shared_large(a));
   return SharedShape(a).bytes(a);
 }
-// Of any smaller batch: the partial tiles over prompts grow with the entries, and of own
-// ones there are no more than workgroups, or than entries have without a cut.
+// Of any smaller batch, which may have small tiles alone: the partial tiles over prompts grow with the entries,
+// and of own ones there are no more than workgroups, or than entries have without a cut.
 size_t kv_shared_workspace(const KvTileArgs& a) {
-  KvTileArgs x = a;
-  kv_shared_shape(x);
-  SharedShape s(x);
-  const int64_t units = s.own / x.own_slices;
-  s.own = std::min(std::max<int64_t>(x.small.wgs, units), units * x.small.most);
-  return s.bytes(x);
+  size_t most = 0;
+  for (const bool large : {false, true}) {
+    if (large && !shared_large(a)) continue;
+    KvTileArgs x = a;
+    shared_shape(x, large);
+    SharedShape s(x);
+    const int64_t units = s.own / x.own_slices;
+    s.own = std::min(std::max<int64_t>(x.small.wgs, units), units * x.small.most);
+    most = std::max(most, s.bytes(x));
+  }
+  return most;
 }
 
 hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
@@ -289,7 +304,9 @@ hipError_t launch_kv_shared(const KvTileArgs& args, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (s.large) e = launch_large_prefix(a, grid(s.large), stream);
   if (e != hipSuccess) return e;
-  e = launch_small_shared(a, grid(s.small + s.own), stream);
+  // (a workgroup has to count the tiles over prompts: no more of them than run at a time, however
+  // few of the tiles that there may be there are; 512 answers 178 -> 126 us)
+  e = launch_small_shared(a, (unsigned)std::min<int64_t>(s.small + s.own, a.small.wgs), stream);
   if (e != hipSuccess) return e;
   const int64_t joins = blocks_of((int64_t)a.B * a.H, join_rows(a.p.d));
   hipLaunchKernelGGL(join_shared_kernel, dim3((unsigned)std::min<int64_t>(joins, kMostJoins)), dim3(kThreads), 0, stream, a);

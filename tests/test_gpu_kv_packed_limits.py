@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from paper_2607_15456_amd import kv
+from tests import test_gpu_kv_packed as packed
 from tests.helpers import f64
 from tests.test_gpu_kv_packed import BF, DEV, F32, bounds, ints, near, normal, pages_for, places, pool, prefill_reference
 
@@ -179,3 +180,65 @@ def test_a_token_does_not_depend_on_its_batch(out_dtype):
     for total, offset, start in calls:
         out = kv.prefill_attn(q[:total], kp, vp, t, ints(offset), ints(start), n_ctx=1024, out_dtype=out_dtype)[:6]
         near(out, ref, tol if out_dtype == F32 else tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref), f"{total} {offset}")
+
+
+# ---------------------------------------------------------------------------
+# shared prompts under a bound far above the lengths, from which on their tiles are large ones
+# ---------------------------------------------------------------------------
+
+def far_bound(monkeypatch, entries, H, d):
+    """Tables that are wide enough for a bound at which the entries' products with all of it are past 3 * 2^30."""
+    pages = -(-(3 << 30) // (entries * H * d * 64)) + 1
+
+    def wide(ends, rng, spare=3):
+        table, n = pages_for(ends, rng, spare)
+        return np.concatenate((table, np.full((len(ends), max(0, pages - table.shape[1])), -1)), axis=1), n
+
+    monkeypatch.setattr(packed, "pages_for", wide)
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_shared_widths_under_a_far_bound(monkeypatch, out_dtype, d):
+    far_bound(monkeypatch, 6, 6, d)
+    packed.check_shared(BF, out_dtype, 6, 2, d, [(200, [5, 70, 1]), (0, [300]), (64, [0, 64])], seed=d)
+    far_bound(monkeypatch, 40, 8, d)
+    packed.check_shared(BF, out_dtype, 8, 1, d, [(900, [3] * 40)], seed=d)
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("H,H_kv,groups", [(4, 2, [(300, [i % 5 for i in range(100)]), (700, [2] * 33)]), (300, 1, [(130, [5, 0, 80])]),
+                                           (40, 2, [(130, [5, 0, 80]), (64, [1] * 9), (1, [1, 63])]), (4, 2, [(5000, [1, 100])]),
+                                           (2, 2, [(64 * i + 3, [1] * (i % 40 + 1)) for i in range(12)]), (64, 1, [(65, [1] * 70)])])
+def test_shared_runs_under_a_far_bound(monkeypatch, out_dtype, H, H_kv, groups):
+    """Runs of few and of many rows side by side, cut inside, of more heads than a tile has rows."""
+    far_bound(monkeypatch, sum(len(m) for _, m in groups), H, 64)
+    packed.check_shared(BF, out_dtype, H, H_kv, 64, groups, seed=len(groups))
+
+
+def test_shared_bad_indices_under_a_far_bound(monkeypatch):
+    """NaN for those whose prompt cannot be read, in runs of few rows and of many, and no harm to the others."""
+    far_bound(monkeypatch, 120, 4, 64)
+    table, n_pages = packed.pages_for([200] * 8, np.random.default_rng(1))
+    kp, vp = pool(1, n_pages, 2, 64, BF)
+    B = 120
+    q = normal((B, 4, 64), 2, BF)
+    rows, lead, shared = np.arange(B) % 7, np.repeat([0, 0, 40, B, 80, -1], 20), np.full(B, 100)
+    shared[45], rows[50], rows[51] = 201, -1, 8
+    bad_table = table.copy()
+    bad_table[rows[80], 1] = n_pages
+    out = kv.decode_attn_shared(q, kp, vp, ints(bad_table), ints([200] * 8), ints(lead), ints(shared), n_ctx=64 * table.shape[1],
+                                rows=ints(rows))
+    nan = (lead < 0) | (lead == B) | (lead == 80) | (shared > 200) | (rows == 8) | (rows == rows[80])
+    nan[50] = False
+    assert (out[50] == 0).all()
+    assert np.array_equal(out.isnan().all(2).all(1).cpu().numpy(), nan) and np.array_equal(out.isnan().any(2).any(1).cpu().numpy(), nan)
+    kn, vn, qn = f64(kp), f64(vp), f64(q)
+    for b in np.flatnonzero(~nan)[::7]:
+        if b == 50:
+            continue
+        for h in range(4):
+            k, v = places(table, rows[b], 200, kn, vn, h // 2)
+            k[:100], v[:100] = places(table, rows[lead[b]], 100, kn, vn, h // 2)
+            ref, _, tol, _ = bounds(qn[b, h:h + 1], k, v, np.ones((1, 200), dtype=bool), 1 / 8, BF, F32, 0.0)
+            near(out[b, h:h + 1], ref, tol, f"entry {b} head {h}")

@@ -1,0 +1,18 @@
+"""Workspaces of packed batches and shared prompts where the kind of tiles changes (no GPU needed)."""
+
+import pytest
+import torch
+
+from paper_2607_15456_amd import kv
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,H_kv,d", [(16, 16, 128), (16, 2, 64), (40, 2, 256), (300, 1, 32)])
+def test_a_workspace_serves_calls_of_the_other_kind_of_tiles(dtype, H, H_kv, d):
+    """Sizes on both sides of where a batch gets other tiles: what the larger one needs is enough."""
+    for B in (1, 2, 16, 100, 1024):
+        sizes = [kv.shared_workspace_bytes(dtype, B, H, H_kv, d, n) for n in (64, 4096, 20000, 100000, 1 << 20, 1 << 26)]
+        assert sizes == sorted(sizes), B
+    for n in (64, 5000, 100000, 1 << 24):
+        sizes = [kv.shared_workspace_bytes(dtype, B, H, H_kv, d, n) for B in range(1, 1025, 31)]
+        assert sizes == sorted(sizes), n
