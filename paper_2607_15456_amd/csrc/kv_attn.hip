@@ -185,8 +185,8 @@ struct PackedShape {
     const int64_t rows = (int64_t)a.total * (a.H / a.p.Hkv);
     const int cols = large_cols(a.p.d);
     // every entry may end inside a tile; large ones have more than small_rows rows
-    small_tiles = a.small_rows == 0 ? 0
-                  : a.small_rows == kAllRows ? std::min(rows / a.small_cols + a.B, rows) : std::min(a.B, a.total);
+    small_tiles = a.small_rows == 0 ? 0 : std::min(rows / a.small_cols + a.B, rows);
+    if (a.small_rows != kAllRows) small_tiles = std::min(small_tiles, a.B * blocks_of(a.small_rows, a.small_cols));
     large_tiles = rows > a.small_rows ? std::min(rows / cols + a.B, blocks_of(rows, a.small_rows + 1)) : 0;
     small_partial = partial_tiles(a, a.small, small_tiles);
     large_partial = partial_tiles(a, a.large, large_tiles);
@@ -198,20 +198,55 @@ struct PackedShape {
 
 }  // namespace
 
-// Large tiles are of bf16.  In fp32 the matrix units are the bound from few rows on, and
-// small tiles keep them as busy (3 entries of 301 .. 101 tokens over 1020 of a window, 24
-// heads on 8 of 96: 108 us; with large fp32 tiles 134).
-size_t kv_prefill_shape(KvTileArgs& a) {
+// Rows up to which an entry is of small tiles, by what the host knows.  fp32 has no large
+// ones: small tiles read a page again for every 16 or 32 rows of an entry, which bounds them well below the
+// matrix units' rate (3 entries of 301 .. 101 tokens over 1020 of a window, 24 heads on 8 of 96: 100 us, 57
+// TFLOP/s, 7.2 TB/s of pages), but the large fp32 tiles that were tried took 134 us.
+// bf16, us with small tiles alone and with both kinds; a batch of few rows is not worth a second launch:
+//   16 heads of 128 over 1000 tokens: 32 entries of 8 tokens 72 and 82, of 32 88 and 95, of 64 143 and 114
+//   16 heads on 2:                     8 entries of 16 27 and 33, of 32 43 and 41; 32 entries of 16 58 and 45
+//   24 heads on 8 of 64:               8 entries of 32 25 and 33; 32 entries of 16 37 and 42, of 32 54 and 44
+// An entry of up to 32 rows, two small tiles, leaves most of a large one's 256 empty (200
+// entries of 8 .. 1 tokens, 24 heads on 8 of 64: 80 and 133).  A single entry is of one
+// kind, so that one launch does: over 4000 tokens 16 heads of 128, 32 tokens 27 and 26, 64 40 and 31;
+// 16 heads on 2, 32 tokens 24 and 32, 64 38 and 35; on 4 of 256, 32 tokens 35 and 50, 64 56 and 57.
+constexpr int kFewRows = 32, kBatchRows = 1024, kSingleRows = 1024;  // the last: of all heads
+static int small_rows_of(const KvTileArgs& a) {
+  const int64_t rows = (int64_t)a.total * (a.H / a.p.Hkv);
+  if (a.p.dtype == LLA_F32 || rows <= kFewRows) return kAllRows;
+  if (a.B == 1) return (int64_t)a.total * a.H < kSingleRows ? kAllRows : 0;
+  return rows <= kBatchRows ? kAllRows : kFewRows;
+}
+static void packed_shape(KvTileArgs& a, int small_rows) {
   limits(a, large_cols(a.p.d));
   a.small_cols = small_cols_of(a, true);
-  // a single entry is of one kind of tile, so one launch does
-  const bool one_large = a.B == 1 && (int64_t)a.total * (a.H / a.p.Hkv) > a.small_cols;
-  a.small_rows = a.p.dtype == LLA_F32 ? kAllRows : one_large ? 0 : a.small_cols;
+  a.small_rows = small_rows;
+}
+size_t kv_prefill_shape(KvTileArgs& a) {
+  packed_shape(a, small_rows_of(a));
   return PackedShape(a).bytes(a);
 }
+// Of any smaller batch: of small tiles alone, of both kinds, and of one entry with large ones, where it has such.
 size_t kv_prefill_workspace(const KvTileArgs& a) {
-  KvTileArgs x = a;
-  return kv_prefill_shape(x);
+  size_t most = 0;
+  auto with = [&](int B, int64_t total, int small_rows) {
+    KvTileArgs x = a;
+    x.B = B;
+    x.total = (int)std::min<int64_t>(a.total, total);
+    packed_shape(x, small_rows);
+    most = std::max(most, PackedShape(x).bytes(x));
+  };
+  const int group = a.H / a.p.Hkv;
+  if (a.p.dtype == LLA_F32) {
+    with(a.B, a.total, kAllRows);
+    return most;
+  }
+  with(a.B, std::max(1, kBatchRows / group), kAllRows);
+  KvTileArgs one = a;
+  one.B = 1;
+  if (small_rows_of(one) == 0) with(1, a.total, 0);
+  if (small_rows_of(a) == kFewRows) with(a.B, a.total, kFewRows);
+  return most;
 }
 
 hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
@@ -225,7 +260,10 @@ hipError_t launch_kv_prefill(const KvTileArgs& args, hipStream_t stream) {
   auto grid = [&](int64_t tiles, int64_t partial) { return (unsigned)std::min<int64_t>(std::max(partial, tiles * a.p.Hkv), 1 << 16); };
   if (s.large_tiles) e = launch_large_packed(a, grid(s.large_tiles, s.large_partial), stream);
   if (e != hipSuccess) return e;
-  if (s.small_tiles) e = launch_small_packed(a, grid(s.small_tiles, std::min<int64_t>(s.small_partial, a.small.wgs)), stream);
+  // (a workgroup has to count the tiles: two rounds of those that run at a time; 200 entries of one
+  // token, 16 heads of 128, 348 -> 328 us.  With one round fp32 prompts wait for the last ones, 29 -> 35)
+  const unsigned small = grid(s.small_tiles, std::min<int64_t>(s.small_partial, a.small.wgs));
+  if (s.small_tiles) e = launch_small_packed(a, std::min(small, 2u * a.small.wgs), stream);
   if (e != hipSuccess || s.small_partial + s.large_partial == 0) return e;
   const int64_t joins = s.small_partial * join_chunks(a.p.d, a.small_cols) + s.large_partial * join_chunks(a.p.d, large_cols(a.p.d));
   hipLaunchKernelGGL(join_packed_kernel, dim3((unsigned)std::min<int64_t>(joins, kMostJoins)), dim3(kThreads), 0, stream, a,

@@ -242,3 +242,57 @@ def test_shared_bad_indices_under_a_far_bound(monkeypatch):
             k[:100], v[:100] = places(table, rows[lead[b]], 100, kn, vn, h // 2)
             ref, _, tol, _ = bounds(qn[b, h:h + 1], k, v, np.ones((1, 200), dtype=bool), 1 / 8, BF, F32, 0.0)
             near(out[b, h:h + 1], ref, tol, f"entry {b} head {h}")
+
+
+# ---------------------------------------------------------------------------
+# entries with room for more tokens, from 1024 rows of which on those of more than 32 rows take large tiles
+# ---------------------------------------------------------------------------
+
+ROOM = 2100
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_prefill_widths_with_room(out_dtype, d):
+    packed.check_prefill(BF, out_dtype, 3, 1, d, [70, 1, 200], [0, 300, 13], seed=d, spare=ROOM)
+    packed.check_prefill(BF, out_dtype, 2, 2, d, [300], [65], seed=d + 1, spare=ROOM)
+    packed.check_prefill(BF, out_dtype, 2, 1, d, [3, 10, 16, 17, 9], [400, 0, 65, 130, 250], seed=d, spare=ROOM)
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("H,H_kv", [(1, 1), (16, 16), (16, 2), (6, 2), (40, 2), (64, 1), (33, 1)])
+def test_prefill_groups_with_room(out_dtype, H, H_kv):
+    packed.check_prefill(BF, out_dtype, H, H_kv, 64, [5, 1, 37], [100, 0, 63], seed=H, spare=ROOM)
+    packed.check_prefill(BF, out_dtype, H, H_kv, 64, [5], [100], seed=H, spare=ROOM)
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("new,start", [([1], [0]), ([1], [64]), ([64], [0]), ([33], [31]), ([129], [4000]), ([0, 3, 0, 17, 1, 0], [5, 60, 0, 9, 700, 1]),
+                                       ([300, 1, 1, 64], [0, 5000, 1, 64]), ([16, 17, 15, 32, 33], [0, 1, 2, 3, 4])])
+def test_prefill_lengths_with_room(out_dtype, new, start):
+    packed.check_prefill(BF, out_dtype, 4, 2, 128, new, start, seed=sum(new), spare=ROOM, fused=True)
+    packed.check_prefill(BF, out_dtype, 4, 2, 96, new, start, seed=sum(new), spare=ROOM)
+
+
+@pytest.mark.parametrize("sink,window", [(0, 1), (0, 64), (4, 60), (70, 100), (4, 100000), (1, 31), (500, 3)])
+def test_prefill_windows_with_room(sink, window):
+    packed.check_prefill(BF, BF, 4, 2, 64, [150, 1, 1, 280], [0, 400, 63, 700], sink, window, seed=window % 97, spare=ROOM)
+    packed.check_prefill(BF, F32, 4, 2, 64, [14, 16, 1, 180], [0, 400, 63, 700], sink, window, seed=window % 97, spare=ROOM)
+
+
+@pytest.mark.parametrize("offsets", [[0, 1500, 0, 1500, 0, 1500], [1500, 0, 1500, 0], [-5, 1600, -(1 << 31), (1 << 31) - 1, 3], [7] * 6])
+def test_prefill_offsets_that_decrease_with_room(offsets):
+    """Which tokens are done is not defined; nothing but the results and the workspace is written, and a call after it is whole."""
+    B, total = len(offsets) - 1, 1500
+    table, n_pages = pages_for_all([2500] * B)
+    kp, vp = pool(1, n_pages, 2, 64, BF)
+    q = normal((total, 4, 64), 2, BF)
+    n_ctx = 64 * table.shape[1]
+    need = kv.prefill_workspace_bytes(BF, B, total, 4, 2, 64, n_ctx)
+    ws = torch.full((need + 65536,), 90, dtype=torch.uint8, device=DEV)
+    out = torch.full((total + 64, 4, 64), 7.0, device=DEV)
+    kv.prefill_attn(q, kp, vp, ints(table), ints(offsets), ints([800] * B), n_ctx=n_ctx, out=out[:total], workspace=ws[:need])
+    assert (ws[need:] == 90).all() and (out[total:] == 7).all()
+    kv.prefill_attn(q, kp, vp, ints(table[:1]), ints([0, total]), ints([900]), n_ctx=n_ctx, out=out[:total], workspace=ws[:need])
+    ref = prefill_reference(q[:, [0, 3]].contiguous(), kp, vp, table[:1], [0, total], [900], None, 1 / 8, 0, 0, BF, F32)
+    near(out[:total][:, [0, 3]], ref[0], ref[2], "after it")
