@@ -293,8 +293,8 @@ struct Tile {
       else if (row < 0 || row >= a.p.n_seqs) state = kNone;
       else {
         n = a.length[row];
-        if (n == 0) state = kZeros;
-        else if (n < 0 || n > a.n_ctx || a.shared[b] < 0 || a.shared[b] > n) state = kNone;
+        if (n < 0 || n > a.n_ctx || a.shared[b] < 0 || a.shared[b] > n) state = kNone;
+        else if (n == 0) state = kZeros;
       }
       keys.p_min = keys.p_max = state == kFine ? n - 1 : -1;
       keys.low_min = keys.low_max = state == kFine ? a.shared[b] : 0;

@@ -296,3 +296,25 @@ def test_prefill_offsets_that_decrease_with_room(offsets):
     kv.prefill_attn(q, kp, vp, ints(table[:1]), ints([0, total]), ints([900]), n_ctx=n_ctx, out=out[:total], workspace=ws[:need])
     ref = prefill_reference(q[:, [0, 3]].contiguous(), kp, vp, table[:1], [0, total], [900], None, 1 / 8, 0, 0, BF, F32)
     near(out[:total][:, [0, 3]], ref[0], ref[2], "after it")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("far", [False, True])
+def test_an_empty_entry_shares_nothing(monkeypatch, dtype, far):
+    """Places shared beyond a length of 0 are places shared beyond the length: NaN; with none shared, zeros."""
+    if far:
+        far_bound(monkeypatch, 40, 4, 64)
+    table, n_pages = packed.pages_for([200, 100], np.random.default_rng(0))
+    kp, vp = pool(1, n_pages, 2, 64, dtype)
+    q, lse = normal((40, 4, 64), 2, dtype), torch.zeros((40, 4), device=DEV)
+    rows, shared, lead = np.zeros(40, dtype=int), np.full(40, 90), np.zeros(40, dtype=int)
+    rows[5], rows[6], shared[6], rows[7], shared[7], rows[8] = 1, 1, 0, 1, -3, -1
+    out = kv.decode_attn_shared(q, kp, vp, ints(table), ints([200, 0]), ints(lead), ints(shared), n_ctx=64 * table.shape[1],
+                                rows=ints(rows), lse=lse)
+    for b in range(40):
+        if b in (5, 7):
+            assert out[b].isnan().all() and lse[b].isnan().all(), b
+        elif b in (6, 8):
+            assert (out[b] == 0).all() and (lse[b] == -np.inf).all(), b
+        else:
+            assert out[b].isfinite().all() and lse[b].isfinite().all(), b
