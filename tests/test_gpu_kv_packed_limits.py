@@ -318,3 +318,51 @@ def test_an_empty_entry_shares_nothing(monkeypatch, dtype, far):
             assert (out[b] == 0).all() and (lse[b] == -np.inf).all(), b
         else:
             assert out[b].isfinite().all() and lse[b].isfinite().all(), b
+
+
+# ---------------------------------------------------------------------------
+# two graphs of one pool
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_two_captured_steps_of_one_pool(dtype):
+    """A packed step and a step over shared prompts, each captured once, replayed in turn with the program's own work
+    between; both equal the eager ones of another pool.  The side stream waits for what the tensors hold."""
+    a, b = packed.Server(dtype), packed.Server(dtype)
+    width = a.H + 2 * a.H_kv
+    result = torch.empty(4, dtype=torch.int32, device=DEV)
+    first = normal((500, width, a.d), 30, dtype)
+    for s in (a, b):
+        s.step(ints([0, 2]), ints([200, 300]), first, 500)
+        kv.fork(s.pages, ints([0, 0, 2]), ints([1, 4, 3]), result)
+    rows, add = [ints([0, 1, 4, 2, 3, -1]), ints([2, 0, -1])], [ints([1] * 5 + [0]), ints([3, 7, 0])]
+    totals, shared = (6, 12), (True, False)
+    x = [torch.zeros((n, width, a.d), dtype=dtype, device=DEV) for n in totals]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(2):  # (loads kernels; the lengths grow alike in both)
+        with torch.cuda.stream(side):
+            a.step(rows[i], add[i], x[i], totals[i], shared[i])
+        torch.cuda.current_stream().wait_stream(side)
+        b.step(rows[i], add[i], x[i], totals[i], shared[i])
+        side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    for i in range(2):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(a.step(rows[i], add[i], x[i], totals[i], shared[i]))
+        graphs.append(g)
+    for turn in range(8):
+        i = turn % 2 if turn < 6 else 1
+        xs = normal(tuple(x[i].shape), 50 + turn, dtype)
+        if i:
+            add[1].copy_(ints([turn, 9 - turn, 0]))
+        x[i].copy_(xs)
+        graphs[i].replay()
+        want = b.step(rows[i], add[i], xs, totals[i], shared[i])
+        torch.cuda.synchronize()
+        used = totals[i] if shared[i] else int(add[i].clamp_min(0).sum())
+        assert outs[i][:used].isfinite().all() and torch.equal(outs[i][:used], want[:used]), turn
+        assert torch.equal(a.pages.length, b.pages.length) and torch.equal(a.pages.table, b.pages.table)
+        (xs.float() @ xs.float().transpose(1, 2)).sum().item()  # the program's own work
