@@ -381,7 +381,8 @@ lla_status lla_kv_prefill_attn(int dtype, int out_dtype, int B, int total, int H
  * entry b joins the group of b - 1 when both read the same pages at their first
  * c >= least places (c counts no place past either's length).  For all entries of a
  * group, lead[b] is its first entry and shared[b] the least c of its joins; an entry
- * alone has lead[b] = b and shared[b] = 0.  Sequences that lla_pages_fork made share the
+ * alone has lead[b] = b and shared[b] = 0.  Families behind one prompt that all have are one
+ * group of that prompt unless `least` is above its places.  Sequences that lla_pages_fork made share the
  * pages that they had, until lla_pages_reserve gives one a copy of its last.
  *   rows  int32 [B] or NULL (-1 or out of range: joins nobody);  length  int32 [n_seqs]
  *   lead, shared  int32 [B]
@@ -400,9 +401,12 @@ lla_status lla_kv_shared_workspace_bytes(int dtype, int B, int H, int H_kv, int 
 
 /*
  * lla_kv_decode_attn for entries of which neighbours share a long prompt: the keys and
- * values of entry b's places below shared[b] are those of entry lead[b], are read
- * through that entry's pages, and once for all neighbours with the same lead and shared;
- * the places from shared[b] to its length through its own pages.  (lla_pages_shared
+ * values of entry b's places below shared[b] are those of entry lead[b], and are read
+ * through that entry's pages by the queries of neighbours with the same lead and shared
+ * together: up to 16 rows (entries times H / H_kv; 32 where H / H_kv is more than 16) read a
+ * page at once, in bf16 up to 256 (128 above a d_head of 128) where the batch has enough to
+ * do; the places from shared[b] to its length through its own pages.  It pays where neighbours
+ * would read some 450 MB more without it; below that lla_kv_decode_attn is faster.  (lla_pages_shared
  * finds both; a program that knows its prompts may give other numbers, down to a place
  * inside a page.)  Arguments and results are otherwise those of lla_kv_decode_attn without
  * a window.

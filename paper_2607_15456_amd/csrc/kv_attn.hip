@@ -176,7 +176,9 @@ void limits(KvTileArgs& a, int cols) {
 
 // Rows of a small tile: two products' columns where a group of heads is more than one's, and
 // for packed tokens of wide heads: two wavefronts a SIMD, which one column leaves room
-// for, hold no more registers than the step takes, and its masks need some.
+// for, hold no more registers than the step takes, and its masks need some (32 drafts of 5 tokens
+// over 4001, 16 heads of 128: 264 us with one column, 188 with two; at a width of 64 24 heads
+// on 8, 32 entries of 4 tokens over 1000, 25 and 30).
 int small_cols_of(const KvTileArgs& a, bool packed) { return a.H / a.p.Hkv > 16 || (packed && a.p.d > 96) ? 32 : 16; }
 
 struct PackedShape {
@@ -199,9 +201,9 @@ struct PackedShape {
 }  // namespace
 
 // Rows up to which an entry is of small tiles, by what the host knows.  fp32 has no large
-// ones: small tiles read a page again for every 16 or 32 rows of an entry, which bounds them well below the
-// matrix units' rate (3 entries of 301 .. 101 tokens over 1020 of a window, 24 heads on 8 of 96: 100 us, 57
-// TFLOP/s, 7.2 TB/s of pages), but the large fp32 tiles that were tried took 134 us.
+// ones: small tiles read a page again for every 16 or 32 rows of an entry and keep the matrix units half busy
+// (3 entries of 301 .. 101 tokens over 1020 of a window, 24 heads on 8 of 96: 100 us, 57 TFLOP/s, 7.2 TB/s of
+// pages from the caches, units 51% busy), but the large fp32 tiles that were tried took 134 us.
 // bf16, us with small tiles alone and with both kinds; a batch of few rows is not worth a second launch:
 //   16 heads of 128 over 1000 tokens: 32 entries of 8 tokens 72 and 82, of 32 88 and 95, of 64 143 and 114
 //   16 heads on 2:                     8 entries of 16 27 and 33, of 32 43 and 41; 32 entries of 16 58 and 45
