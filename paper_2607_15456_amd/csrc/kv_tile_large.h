@@ -3,10 +3,11 @@
 // (kv_large_packed.hip) and the queries of many entries over one shared prompt
 // (kv_large_shared.hip).
 //
-// Bound by the matrix units: 4 d flops a pair of row and token, of which the weights' half is done three
-// times for all of their bits (4 prompts of 4096 tokens, 16 heads of 128, 539 us: 1.02 PFLOP/s of products with
-// those, 510 TFLOP/s without, where a large library product reaches 1.15).  A wavefront holds 32 rows, a workgroup eight of them (four); a step of
-// 64 tokens (32) is staged in LDS once for all, the next one on its way in registers.
+// Bound by the matrix units: 4 d flops a pair of row and token, of which the weights' half is
+// done three times for all of their bits (4 prompts of 4096 tokens, 16 heads of 128, 539 us: 510
+// TFLOP/s, 1.02 PFLOP/s with the three, where a large library product reaches 1.15).  A
+// wavefront holds 32 rows, a workgroup eight of them (four); a step of 64 tokens (32) is
+// staged in LDS once for all, the next one on its way in registers.
 // Both products are 32 x 32 tiles with the rows as columns:
 //
 //   S^T [tokens x rows] = K Q^T           A: 16 bytes of a key row (token-major)
